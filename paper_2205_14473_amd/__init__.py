@@ -3,6 +3,8 @@
 The work runs in ``libea.so`` (hand-written HIP kernels for gfx950 behind the
 C ABI of ``include/ea.h``); this package only binds it.  ``state`` allocates
 the device buffers one round needs (PyTorch provides memory and streams).
+Beside the round, ``include/ea_train.h`` holds AdamW over many tensors, the
+global gradient norm, and the embedding lookup with its gradient.
 
 The binding is loaded on first use of any of its names, so that the ``build``
 submodule can be imported (and the library compiled) before the library
@@ -19,15 +21,25 @@ _EXPORTS = (
     "ea_worker_apply", "ea_step", "ea_step_noalloc", "ea_schedule_at", "ea_step_scheduled", "ea_run", "ea_toy_workspace_bytes",
     "ea_toy_grad", "ea_toy_step",
 )
-__all__ = list(_EXPORTS)
+# The operators beside the round (include/ea_train.h).
+_TRAIN_EXPORTS = (
+    "EA_F32", "EA_BF16", "EA_F16", "EA_ROUND_NEAREST", "EA_ROUND_STOCHASTIC", "EA_STATE_BLOCK",
+    "Tensor", "AdamW", "Embed", "TensorList", "ea_type",
+    "ea_adamw_step", "ea_adamw_step_scheduled", "ea_grad_norm", "ea_grad_norm_workspace_bytes",
+    "ea_embed_lookup", "ea_embed_grad", "ea_embed_workspace_bytes",
+)
+__all__ = list(_EXPORTS + _TRAIN_EXPORTS)
 
 
 def __getattr__(name):
     if name in _EXPORTS:
         from . import _binding
         return getattr(_binding, name)
+    if name in _TRAIN_EXPORTS:
+        from . import _train
+        return getattr(_train, name)
     raise AttributeError(f"module {__name__!r} has no attribute {name!r}")
 
 
 def __dir__():
-    return sorted(list(globals()) + list(_EXPORTS))
+    return sorted(list(globals()) + list(_EXPORTS + _TRAIN_EXPORTS))

@@ -1,0 +1,251 @@
+"""ctypes binding of the operators beside the round (include/ea_train.h):
+AdamW over many tensors, the global gradient norm, the embedding lookup and
+its gradient.  Argument marshalling only, in the manner of ``_binding``: every
+function has the name of the C entry point it calls, tensors are device
+tensors of the documented types, streams are torch streams, raw hipStream_t
+integers, or None for torch's current stream.
+"""
+import ctypes as C
+
+from . import _binding as B
+from ._binding import _check, _ptr, _ptr_u32, _stream, lib
+
+EA_F32, EA_BF16, EA_F16 = 0, 1, 2
+EA_ROUND_NEAREST, EA_ROUND_STOCHASTIC = 0, 1
+EA_STATE_BLOCK = 256
+
+
+class Tensor(C.Structure):
+    """ea_tensor_t"""
+    _fields_ = [("g", C.c_void_p), ("p", C.c_void_p), ("m", C.c_void_p), ("v", C.c_void_p),
+                ("m_scale", C.c_void_p), ("v_scale", C.c_void_p), ("master", C.c_void_p), ("n", C.c_int64),
+                ("weight_decay", C.c_float), ("lr_scale", C.c_float)]
+
+
+class AdamW(C.Structure):
+    """ea_adamw_t"""
+    _fields_ = [("lr", C.c_float), ("beta1", C.c_float), ("beta2", C.c_float), ("eps", C.c_float),
+                ("param_type", C.c_int32), ("grad_type", C.c_int32), ("state_bits", C.c_int32),
+                ("rounding", C.c_int32), ("seed", C.c_uint64)]
+
+
+class Embed(C.Structure):
+    """ea_embed_t"""
+    _fields_ = [("tokens", C.c_int64), ("vocab", C.c_int64), ("dim", C.c_int64), ("table_stride", C.c_int64),
+                ("x_stride", C.c_int64), ("padding", C.c_int64), ("scale", C.c_float), ("table_type", C.c_int32),
+                ("x_type", C.c_int32), ("index_bits", C.c_int32)]
+
+
+assert C.sizeof(Tensor) == 72 and C.sizeof(AdamW) == 40 and C.sizeof(Embed) == 64
+
+_P, _I32, _I64 = C.c_void_p, C.c_int32, C.c_int64
+for _name, _res, _args in (
+        ("ea_adamw_step", C.c_int, [C.POINTER(AdamW), _I64, _I32, _P, _P, _P]),
+        ("ea_adamw_step_scheduled", C.c_int, [C.POINTER(AdamW), C.POINTER(B.Schedule), _P, _I32, _P, _P, _P]),
+        ("ea_grad_norm_workspace_bytes", _I64, [_I32, _P]),
+        ("ea_grad_norm", C.c_int, [_I32, _I32, _P, C.c_float, C.c_float, _P, _P, _P, _P]),
+        ("ea_embed_lookup", C.c_int, [C.POINTER(Embed), _P, _P, _P, _P]),
+        ("ea_embed_workspace_bytes", _I64, [C.POINTER(Embed)]),
+        ("ea_embed_grad", C.c_int, [C.POINTER(Embed), _P, _P, _P, _I32, _P, _P])):
+    getattr(lib, _name).restype, getattr(lib, _name).argtypes = _res, _args
+
+
+def ea_type(dtype) -> int:
+    """EA_F32, EA_BF16 or EA_F16 for a torch dtype."""
+    import torch
+    types = {torch.float32: EA_F32, torch.bfloat16: EA_BF16, torch.float16: EA_F16}
+    if dtype not in types:
+        raise ValueError(f"libea takes float32, bfloat16 or float16 here, got {dtype}")
+    return types[dtype]
+
+
+def _dense(t) -> bool:
+    """Whether the tensor fills its memory without gaps or overlaps, in any order."""
+    if t.is_contiguous():
+        return True
+    expect = 1
+    for stride, size in sorted((st, sz) for st, sz in zip(t.stride(), t.shape) if sz != 1):
+        if stride != expect:
+            return False
+        expect *= size
+    return True
+
+
+class TensorList:
+    """The tensors of an AdamW step or a gradient norm: an ea_tensor_t array and references to what it points
+    to.  A program makes it once and passes it every step; ``set_grads`` replaces the gradients.
+
+    g, p, m, v, m_scale, v_scale, master: lists of device tensors, one per parameter (all but g may be None;
+    entries of master too).  g, p and master of a parameter share its shape and strides and are dense; m and v
+    hold its number of elements in the same memory order, as float32, or as 8-bit codes (float8_e4m3fn or
+    uint8) with scales.  weight_decay, lr_scale: one number, or one per parameter.
+    """
+
+    def __init__(self, g, p=None, m=None, v=None, m_scale=None, v_scale=None, master=None, weight_decay=0.0,
+                 lr_scale=1.0):
+        n = len(g)
+        self.count = n
+        self.array = (Tensor * max(n, 1))()
+        self.param_type = self.grad_type = self.state_bits = None
+        self._p = p
+        for name, ts in (("p", p), ("m", m), ("v", v), ("m_scale", m_scale), ("v_scale", v_scale),
+                         ("master", master)):
+            if ts is not None and len(ts) != n:
+                raise ValueError(f"{len(ts)} tensors in {name}, and {n} in g")
+        self.set_grads(g)
+        if p is not None:
+            self.param_type = self._set("p", p, g, dtype=None)
+            if master is not None:
+                self._set("master", master, p, dtype="float32", optional=True)
+        if (m is None) != (v is None):
+            raise ValueError("m and v come together")
+        if m is not None:
+            self.state_bits = self._set_states(m, v, m_scale, v_scale)
+        for i in range(n):
+            self.array[i].weight_decay = weight_decay if isinstance(weight_decay, (int, float)) else weight_decay[i]
+            self.array[i].lr_scale = lr_scale if isinstance(lr_scale, (int, float)) else lr_scale[i]
+        self._held = (p, m, v, m_scale, v_scale, master)
+
+    def _set(self, name, ts, like, dtype, optional=False):
+        import torch
+        kind = None
+        for i, (t, e) in enumerate(zip(ts, like)):
+            if t is None and optional:
+                continue
+            if not t.is_cuda:
+                raise ValueError("libea needs device tensors")
+            if dtype is not None and t.dtype is not getattr(torch, dtype):
+                raise ValueError(f"{name}[{i}]: expected {dtype}, got {t.dtype}")
+            if kind is not None and t.dtype is not kind:
+                raise ValueError(f"{name}[{i}]: all of {name} share one type, got {t.dtype} after {kind}")
+            kind = t.dtype
+            if t.device != e.device:
+                raise ValueError(f"{name}[{i}] is on {t.device}, and others on {e.device}")
+            if t.shape != e.shape or (t.stride() != e.stride() and t.numel() > 1) or not _dense(t):
+                raise ValueError(f"{name}[{i}]: shape {tuple(t.shape)}, strides {t.stride()} do not match the "
+                                 f"parameter's {tuple(e.shape)}, {e.stride()}, or leave gaps")
+            setattr(self.array[i], name, t.data_ptr())
+        return None if kind is None or dtype is not None else ea_type(kind)
+
+    def _set_states(self, m, v, m_scale, v_scale):
+        import torch
+        codes = (torch.float8_e4m3fn, torch.uint8)
+        bits = 8 if self.count and m[0].dtype in codes else 32
+        if bits == 8 and (m_scale is None or v_scale is None):
+            raise ValueError("8-bit states come with m_scale and v_scale")
+        for name, ts in (("m", m), ("v", v), ("m_scale", m_scale), ("v_scale", v_scale)):
+            if ts is None or (bits == 32 and name.endswith("scale")):
+                continue
+            want = codes if bits == 8 and name in "mv" else (torch.float32,)
+            for i, t in enumerate(ts):
+                n = self.array[i].n
+                most = n if name in "mv" else (n + EA_STATE_BLOCK - 1) // EA_STATE_BLOCK
+                if not t.is_cuda:
+                    raise ValueError("libea needs device tensors")
+                if t.dtype not in want or t.numel() != most or not _dense(t) or t.device != self._g[i].device:
+                    raise ValueError(f"{name}[{i}]: expected {most} dense elements of {want[0]} on the gradient's "
+                                     f"device, got {t.numel()} of {t.dtype} on {t.device}")
+                setattr(self.array[i], name, t.data_ptr())
+        return bits
+
+    def set_grads(self, g):
+        """Points the list at other gradients of the same shapes."""
+        if len(g) != self.count:
+            raise ValueError(f"{len(g)} gradients for {self.count} tensors")
+        kind = self._set("g", g, g if self._p is None else self._p, dtype=None)
+        if self.grad_type is not None and kind != self.grad_type:
+            raise ValueError("the gradients' type changed")
+        for i, t in enumerate(g):
+            if self.array[i].p is not None and self.array[i].n != t.numel():
+                raise ValueError(f"g[{i}]: {t.numel()} elements, and the parameter has {self.array[i].n}")
+            self.array[i].n = t.numel()
+        self.grad_type = kind
+        self._g = g
+
+
+def _check_list(cfg, tensors):
+    if tensors.count and (tensors.param_type, tensors.grad_type, tensors.state_bits) != \
+            (cfg.param_type, cfg.grad_type, cfg.state_bits):
+        raise ValueError(f"the tensors' types (param {tensors.param_type}, grad {tensors.grad_type}, states "
+                         f"{tensors.state_bits} bits) are not the configuration's ({cfg.param_type}, "
+                         f"{cfg.grad_type}, {cfg.state_bits} bits)")
+
+
+def ea_adamw_step(cfg, t, tensors, gscale=None, stream=None):
+    _check_list(cfg, tensors)
+    return _check(lib.ea_adamw_step(C.byref(cfg), t, tensors.count, tensors.array, _ptr(gscale, B._f32()),
+                                    _stream(stream)))
+
+
+def ea_adamw_step_scheduled(cfg, sched, t_dev, tensors, gscale=None, stream=None):
+    _check_list(cfg, tensors)
+    return _check(lib.ea_adamw_step_scheduled(C.byref(cfg), C.byref(sched), _ptr_u32(t_dev), tensors.count,
+                                              tensors.array, _ptr(gscale, B._f32()), _stream(stream)))
+
+
+def ea_grad_norm_workspace_bytes(tensors) -> int:
+    return _check(lib.ea_grad_norm_workspace_bytes(tensors.count, tensors.array))
+
+
+def ea_grad_norm(tensors, scale, max_norm, norm, gscale, workspace, stream=None):
+    f = B._f32()
+    _room(workspace, lib.ea_grad_norm_workspace_bytes(tensors.count, tensors.array))
+    return _check(lib.ea_grad_norm(EA_F32 if tensors.grad_type is None else tensors.grad_type, tensors.count,
+                                   tensors.array, scale, max_norm, _ptr(norm, f), _ptr(gscale, f), _ptr(workspace),
+                                   _stream(stream)))
+
+
+def _room(workspace, need):
+    if need > 0 and hasattr(workspace, "numel") and workspace.numel() * workspace.element_size() < need:
+        raise ValueError(f"the workspace holds {workspace.numel() * workspace.element_size()} bytes, {need} are needed")
+
+
+def _rows(t, kind, rows, dim, stride, name):
+    """Pointer of a [rows, dim] tensor (leading dimensions may be split) with `stride` elements between rows."""
+    if t is None or isinstance(t, int):
+        return t
+    if not t.is_cuda:
+        raise ValueError("libea needs device tensors")
+    if ea_type(t.dtype) != kind:
+        raise ValueError(f"{name}: {t.dtype} is not the configuration's type {kind}")
+    if t.dim() < 1 or t.shape[-1] != dim or t.numel() != rows * dim:
+        raise ValueError(f"{name}: expected {rows} rows of {dim}, got shape {tuple(t.shape)}")
+    if t.numel() == 0:
+        return t.data_ptr()
+    step = stride
+    for k in range(t.dim() - 2, -1, -1):
+        if t.shape[k] != 1 and t.stride(k) != step:
+            raise ValueError(f"{name}: strides {t.stride()} are not those of rows {stride} elements apart")
+        step *= t.shape[k]
+    if dim > 1 and t.stride(-1) != 1:
+        raise ValueError(f"{name}: the elements of a row are not next to each other")
+    return t.data_ptr()
+
+
+def _ids(t, cfg):
+    if t is None or isinstance(t, int):
+        return t
+    if t.is_floating_point() or t.element_size() * 8 != cfg.index_bits:
+        raise ValueError(f"ids: expected {cfg.index_bits}-bit integers, got {t.dtype}")
+    if t.numel() != cfg.tokens:
+        raise ValueError(f"ids: expected {cfg.tokens}, got {t.numel()}")
+    return _ptr(t)
+
+
+def ea_embed_lookup(cfg, table, ids, x, stream=None):
+    return _check(lib.ea_embed_lookup(C.byref(cfg),
+                                      _rows(table, cfg.table_type, cfg.vocab, cfg.dim, cfg.table_stride, "table"),
+                                      _ids(ids, cfg), _rows(x, cfg.x_type, cfg.tokens, cfg.dim, cfg.x_stride, "x"),
+                                      _stream(stream)))
+
+
+def ea_embed_workspace_bytes(cfg) -> int:
+    return _check(lib.ea_embed_workspace_bytes(C.byref(cfg)))
+
+
+def ea_embed_grad(cfg, ids, dx, dtable, accumulate, workspace, stream=None):
+    _room(workspace, lib.ea_embed_workspace_bytes(C.byref(cfg)))
+    return _check(lib.ea_embed_grad(C.byref(cfg), _ids(ids, cfg),
+                                    _rows(dx, cfg.x_type, cfg.tokens, cfg.dim, cfg.x_stride, "dx"),
+                                    _rows(dtable, cfg.table_type, cfg.vocab, cfg.dim, cfg.table_stride, "dtable"),
+                                    1 if accumulate else 0, _ptr(workspace), _stream(stream)))

@@ -1,0 +1,142 @@
+// ea_train.hpp -- argument blocks, element types and launchers of the
+// operators beside the round (ea_train.h): AdamW over many tensors, gradient
+// norm, embedding.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "ea_train.h"
+
+namespace ea {
+
+// ---- element types ----------------------------------------------------------
+
+using bf16 = __bf16;
+using f16 = _Float16;
+using v4f = float __attribute__((ext_vector_type(4)));
+
+// Four consecutive elements of type T at an address aligned to one element:
+// gfx950 loads and stores vectors at any such address.
+template <class T>
+struct Quad {
+    typedef T vec __attribute__((ext_vector_type(4)));
+    typedef vec unaligned __attribute__((aligned(sizeof(T))));
+};
+
+template <class T>
+__device__ __forceinline__ typename Quad<T>::vec load4(const T* p)
+{
+    return *(const typename Quad<T>::unaligned*)p;
+}
+
+template <class T>
+__device__ __forceinline__ void store4(T* p, typename Quad<T>::vec v)
+{
+    *(typename Quad<T>::unaligned*)p = v;
+}
+
+template <class T>
+__device__ __forceinline__ v4f widen(T v)
+{
+    return __builtin_convertvector(v, v4f);
+}
+
+template <class T>
+__device__ __forceinline__ typename Quad<T>::vec narrow(v4f v)
+{
+    return __builtin_convertvector(v, typename Quad<T>::vec);
+}
+
+// The first `n` (0 to 3) of four elements; the rest read as zeros, and are not written.
+template <class T>
+__device__ __forceinline__ typename Quad<T>::vec load_some(const T* p, int n)
+{
+    typename Quad<T>::vec v = {(T)0.0f, (T)0.0f, (T)0.0f, (T)0.0f};
+    if (n > 0) v[0] = p[0];
+    if (n > 1) v[1] = p[1];
+    if (n > 2) v[2] = p[2];
+    return v;
+}
+
+template <class T>
+__device__ __forceinline__ void store_some(T* p, typename Quad<T>::vec v, int n)
+{
+    if (n > 0) p[0] = v[0];
+    if (n > 1) p[1] = v[1];
+    if (n > 2) p[2] = v[2];
+}
+
+// ---- AdamW ------------------------------------------------------------------
+
+// A tensor, or 2^30 consecutive elements of a larger one, as a launch sees it.
+struct TensorPart {
+    const void* g;
+    void* p;
+    void* m;
+    void* v;
+    float* m_scale;
+    float* v_scale;
+    float* master;
+    uint32_t n;                            // at most 2^30
+    float weight_decay, lr_scale;
+    uint32_t index;                        // of the tensor in the call's list
+    uint32_t piece;                        // its first element is piece * 2^30
+};
+constexpr int64_t kPartElements = (int64_t)1 << 30;
+
+// Parts of one launch: the table rides in the kernel's arguments, which hold
+// at most 4 KB, and a grid has fewer than 2^32 threads.
+constexpr int kListParts = 46;
+constexpr uint32_t kMostGroups = 1u << 23;
+
+struct AdamwArgs {
+    // The step's values from the host, or (t_dev) from the device's step and the schedule.
+    float lr, beta1, beta2, eps;
+    uint32_t t;
+    uint32_t k0, k1;                       // Philox key
+    int32_t count;                         // parts
+    const float* gscale;
+    const uint32_t* t_dev;
+    ea_schedule_t sched;
+    uint32_t first[kListParts + 1];        // first workgroup of each part
+    TensorPart part[kListParts];
+};
+static_assert(sizeof(AdamwArgs) <= 4096, "kernel arguments");
+
+// Elements per workgroup of a call of `total` elements: what `first` counts in.
+int64_t adamw_chunk(int64_t total);
+hipError_t launch_adamw(const AdamwArgs& a, const ea_adamw_t& c, int64_t chunk, hipStream_t s);
+
+// ---- gradient norm ------------------------------------------------------------
+
+constexpr int kNormParts = 160;
+
+struct NormArgs {
+    int32_t count;                         // parts
+    int64_t chunk;                         // elements per workgroup
+    double* sums;                          // one per workgroup of this launch
+    uint32_t first[kNormParts + 1];
+    struct {
+        const void* g;
+        int64_t n;
+    } part[kNormParts];
+};
+static_assert(sizeof(NormArgs) <= 4096, "kernel arguments");
+
+int64_t norm_chunk(int64_t total);
+hipError_t launch_norm(const NormArgs& a, int32_t grad_type, hipStream_t s);
+hipError_t launch_norm_finish(const double* part, int64_t parts, float scale, float max_norm, float* norm,
+                              float* gscale, hipStream_t s);
+
+// ---- embedding ----------------------------------------------------------------
+
+hipError_t launch_embed_lookup(const ea_embed_t& c, const void* table, const void* ids, void* x, hipStream_t s);
+int64_t embed_workspace_bytes(const ea_embed_t& c);
+hipError_t launch_embed_grad(const ea_embed_t& c, const void* ids, const void* dx, void* dtable, bool accumulate,
+                             void* workspace, hipStream_t s);
+
+// t_dev[0] <- t_dev[0] + 1 (ea_kernels.hip).
+hipError_t launch_advance(uint32_t* t_dev, hipStream_t s);
+
+}  // namespace ea

@@ -59,3 +59,27 @@ def allocate(cfg: B.Config, device="cuda", with_u: bool = False) -> RoundBuffers
 
 def init_state(cfg: B.Config, rb: RoundBuffers, stream=None):
     B.ea_state_init(cfg, rb.m, rb.v, rb.e_s, rb.e_w, rb.m_w, rb.v_w, stream)
+
+
+def adamw_list(params, grads, state_bits=32, masters=False, weight_decay=0.0, lr_scale=1.0):
+    """The tensors of ea_adamw_step for these parameters and gradients, with states (and, for 16-bit
+    parameters, binary32 masters) allocated at their start: zeros, and the parameters' values.  The states are
+    ``.states`` (first moments, then second ones) and ``.scales`` of the list returned."""
+    import torch
+    from . import _train as T
+    eight = state_bits == 8
+
+    def states(dtype, count):
+        return [torch.zeros(count(p.numel()), dtype=dtype, device=p.device) for p in params]
+
+    codes = torch.float8_e4m3fn if eight else torch.float32
+    m, v = states(codes, lambda n: n), states(codes, lambda n: n)
+    ms = vs = None
+    if eight:
+        blocks = lambda n: (n + T.EA_STATE_BLOCK - 1) // T.EA_STATE_BLOCK  # noqa: E731
+        ms, vs = states(torch.float32, blocks), states(torch.float32, blocks)
+    master = [p.detach().float() for p in params] if masters else None
+    got = T.TensorList(grads, p=params, m=m, v=v, m_scale=ms, v_scale=vs, master=master, weight_decay=weight_decay,
+                       lr_scale=lr_scale)
+    got.states, got.scales, got.masters = m + v, (ms + vs if eight else []), master
+    return got

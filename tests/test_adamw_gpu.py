@@ -1,0 +1,346 @@
+"""AdamW over many tensors against a plain step in 64 bits: element types, masters, sizes from
+nothing to several workgroups, alignments, orders, per-tensor factors, skipped steps, 8-bit states
+bit for bit, graphs and streams."""
+import math
+
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+if not torch.cuda.is_available():  # pragma: no cover - CPU-only host
+    pytest.skip("needs a GPU", allow_module_level=True)
+
+import paper_2205_14473_amd as E  # noqa: E402
+import train_util as R  # noqa: E402
+from paper_2205_14473_amd.state import adamw_list  # noqa: E402
+
+TYPES = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+HYPER = dict(lr=3e-3, beta1=0.9, beta2=0.95, eps=1e-8)
+SIZES = [1, 2, 3, 4, 5, 63, 255, 256, 257, 0, 1000, 1024, 1027, 4096, 4099, 20_001]
+
+
+def config(param=torch.float32, grad=torch.float32, bits=32, **kw):
+    return E.AdamW(**{**HYPER, **dict(param_type=E.ea_type(param), grad_type=E.ea_type(grad), state_bits=bits), **kw})
+
+
+class Problem:
+    """Tensors of the given sizes in one allocation per array, each `shift` elements off the last one's end."""
+
+    def __init__(self, sizes, param=torch.float32, grad=torch.float32, bits=32, master=False, shift=0, seed=1,
+                 t=7, **list_args):
+        rng = np.random.default_rng(seed)
+        self.sizes, self.t, self.bits = sizes, t, bits
+        self.p0, self.g0, self.m0, self.v0 = [], [], [], []
+        for n in sizes:
+            s = 10.0 ** rng.uniform(-4, 0)
+            self.p0.append(torch.from_numpy(rng.standard_normal(n).astype(np.float32) * 0.1).to(param))
+            self.g0.append(torch.from_numpy(rng.standard_normal(n).astype(np.float32) * np.float32(s)).to(grad))
+            self.m0.append((rng.standard_normal(n) * s * 0.3).astype(np.float32))
+            self.v0.append((np.exp(rng.standard_normal(n) * 2) * s * s).astype(np.float32))
+        lay = lambda ts: self._lay(ts, shift)  # noqa: E731
+        self.p, self.g = lay(self.p0), lay(self.g0)
+        self.w0 = [x.float() + 0.001 * torch.from_numpy(rng.standard_normal(x.numel()).astype(np.float32))
+                   for x in self.p0] if master else None
+        self.w = lay(self.w0) if master else None
+        if bits == 32:
+            self.m, self.v = lay([torch.from_numpy(x) for x in self.m0]), lay([torch.from_numpy(x) for x in self.v0])
+            self.ms = self.vs = None
+        else:
+            cm, cv = [R.encode32(x, False) for x in self.m0], [R.encode32(np.sqrt(x), True) for x in self.v0]
+            self.cm0, self.cv0 = cm, cv
+            self.m, self.v = lay([torch.from_numpy(c) for c, _ in cm]), lay([torch.from_numpy(c) for c, _ in cv])
+            self.ms, self.vs = lay([torch.from_numpy(s) for _, s in cm]), lay([torch.from_numpy(s) for _, s in cv])
+        self.list = E.TensorList(self.g, p=self.p, m=self.m, v=self.v, m_scale=self.ms, v_scale=self.vs,
+                                 master=self.w, **list_args)
+
+    def _lay(self, ts, shift):
+        total = sum(t.numel() + shift for t in ts) + shift
+        flat = torch.full((total,), 77, dtype=ts[0].dtype, device="cuda")
+        out, at = [], shift
+        for t in ts:
+            out.append(flat[at:at + t.numel()])
+            out[-1].copy_(t)
+            at += t.numel() + shift
+        self.__dict__.setdefault("flats", []).append((flat, out))
+        return out
+
+    def check_gaps(self):
+        for flat, views in self.flats:
+            left = torch.ones(flat.numel(), dtype=torch.bool, device="cuda")
+            for v in views:
+                a = v.storage_offset()
+                left[a:a + v.numel()] = False
+            assert bool((flat[left] == 77).all()), "a write outside the tensors"
+
+    def want(self, i, wd=0.0, lr_scale=1.0, gscale=1.0, t=None):
+        p = (self.p0[i] if self.w0 is None else self.w0[i]).double()
+        if self.bits == 32:
+            m, v = torch.from_numpy(self.m0[i]).double(), torch.from_numpy(self.v0[i]).double()
+        else:
+            m, v = R.decode(*self.cm0[i]), R.decode(*self.cv0[i]) ** 2
+        return R.Step(p, self.g0[i].double(), m, v, t or self.t, wd=wd, lr_scale=lr_scale, gscale=gscale, **HYPER)
+
+
+@pytest.mark.parametrize("shift", [0, 1, 3])
+@pytest.mark.parametrize("grad", TYPES)
+@pytest.mark.parametrize("param,master", [("f32", False), ("bf16", False), ("bf16", True), ("f16", False),
+                                          ("f16", True)])
+def test_states_in_32_bits(param, master, grad, shift):
+    P = Problem(SIZES, TYPES[param], TYPES[grad], master=master, shift=shift)
+    E.ea_adamw_step(config(TYPES[param], TYPES[grad]), P.t, P.list)
+    for i in range(len(SIZES)):
+        w = P.want(i)
+        R.within(P.m[i], w.m, w.m_bound, f"m[{i}]")
+        R.within(P.v[i], w.v, w.v_bound, f"v[{i}]")
+        if master:
+            R.within(P.w[i], w.p, w.p_bound, f"master[{i}]")
+            assert torch.equal(P.p[i], P.w[i].to(TYPES[param])), f"p[{i}] is not the master's rounding"
+        else:
+            R.within(P.p[i], w.p, w.p_bound + 2.0 ** -25, f"p[{i}]", extra=R.U16[TYPES[param]]) if param != "f32" \
+                else R.within(P.p[i], w.p, w.p_bound, f"p[{i}]")
+    P.check_gaps()
+
+
+@pytest.mark.parametrize("rounding", ["nearest", "stochastic"])
+@pytest.mark.parametrize("shift", [0, 1])
+@pytest.mark.parametrize("param,grad,master", [("f32", "f32", False), ("f32", "bf16", False), ("bf16", "bf16", True),
+                                               ("f16", "f32", False), ("bf16", "f16", False), ("f16", "f16", True)])
+def test_states_in_8_bits(param, grad, master, shift, rounding):
+    draws = rounding == "stochastic"
+    P = Problem(SIZES, TYPES[param], TYPES[grad], bits=8, master=master, shift=shift)
+    cfg = config(TYPES[param], TYPES[grad], 8, rounding=int(draws), seed=0x0123456789ABCDEF)
+    E.ea_adamw_step(cfg, P.t, P.list)
+    for i, n in enumerate(SIZES):
+        if n == 0:
+            continue
+        w = P.want(i)
+        # what is kept stands within one code step (draws) or half of one of the 64-bit values
+        code = (2.0 if draws else 1.0) * 2.0 ** -4
+        for name, kept, scale, want, bound, least in (("m", P.m, P.ms, w.m, w.m_bound, 2.0 ** -10),
+                                                      ("root", P.v, P.vs, w.root, w.root_bound, 2.0 ** -9)):
+            s = scale[i].cpu().numpy()
+            got = R.decode(kept[i].cpu().numpy(), s)
+            step = torch.from_numpy(np.repeat(s.astype(np.float64), 256)[:n]) * least * (2 if draws else 1)
+            R.within(got, want, 2 * bound + torch.maximum(step, code * want.abs()), f"{name}[{i}]")
+        target = P.w if master else P.p
+        R.within(target[i], w.p, w.p_bound + (0 if master or param == "f32" else 2.0 ** -25), f"p[{i}]",
+                 extra=0.0 if master else R.U16[TYPES[param]])
+        if master:
+            assert torch.equal(P.p[i], P.w[i].to(TYPES[param]))
+        # and, the operations being fixed, bit for bit
+        dec = lambda c: (R.VALUES[c[0]].astype(np.float32) * np.repeat(c[1], 256)[:n])  # noqa: E731
+        r0 = dec(P.cv0[i])
+        p0 = (P.p0[i] if P.w0 is None else P.w0[i]).float().numpy()
+        m, r, _, p = R.adamw32(p0, P.g0[i].float().numpy(), dec(P.cm0[i]), r0 * r0, P.t, **HYPER)
+        word = R.philox_words(cfg.seed, P.t, i, n) if draws else None
+        for name, kept, scale, x, u in (("m", P.m, P.ms, m, None if word is None else word >> 16),
+                                        ("v", P.v, P.vs, r, None if word is None else word & 0xFFFF)):
+            codes, scales = R.encode32(x, name == "v", u)
+            assert np.array_equal(scale[i].cpu().numpy(), scales), f"{name}_scale[{i}]"
+            assert np.array_equal(kept[i].cpu().numpy(), codes), f"{name}[{i}] codes"
+    P.check_gaps()
+
+
+def test_every_code_is_read_by_the_format():
+    """Gradients of zero: the states decay from every code, under scales of very different sizes."""
+    codes = np.array([c for c in range(256) if c & 127 != 127], np.uint8)
+    for scale in (1.0, 2.0 ** -60, 3.7e15):
+        n = codes.size
+        m = torch.from_numpy(codes).cuda()
+        v = torch.from_numpy(codes & 127).cuda()
+        ms, vs = (torch.full((1,), scale, device="cuda") for _ in range(2))
+        p, g = torch.zeros(n, device="cuda"), torch.zeros(n, device="cuda")
+        cfg = config(bits=8, beta1=0.5, beta2=0.25)
+        E.ea_adamw_step(cfg, 3, E.TensorList([g], p=[p], m=[m], v=[v], m_scale=[ms], v_scale=[vs]))
+        # halving a value halves the scale and keeps the code, but for -0 and 0
+        assert np.array_equal(R.VALUES[m.cpu().numpy()], R.VALUES[codes])
+        assert np.array_equal(v.cpu().numpy(), codes & 127)
+        assert abs(ms.item() - scale / 2) <= 2 * R.U32 * scale and abs(vs.item() - scale / 2) <= 2 * R.U32 * scale
+
+
+def test_many_tensors_with_factors_of_their_own():
+    """More tensors than one launch takes, each with its weight decay and learning-rate factor."""
+    rng = np.random.default_rng(3)
+    sizes = [int(x) for x in rng.integers(1, 600, 173)] + [70_001]
+    wd, ls = [0.1 * (i % 3) for i in range(len(sizes))], [1.0 / (1 + i % 4) for i in range(len(sizes))]
+    gscale = torch.full((1,), 0.125, device="cuda")
+    for bits in (32, 8):
+        P = Problem(sizes, bits=bits, shift=1, weight_decay=wd, lr_scale=ls)
+        E.ea_adamw_step(config(bits=bits), P.t, P.list, gscale)
+        for i in range(len(sizes)):
+            w = P.want(i, wd[i], ls[i], 0.125)
+            R.within(P.p[i], w.p, w.p_bound, f"p[{i}] ({bits} bits)")
+        P.check_gaps()
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_several_steps_follow_the_64_bit_ones(bits):
+    """From zeroed states, ten steps; 32-bit states stay within the accumulated rounding, 8-bit ones near."""
+    n, steps, rng = 5000, 10, np.random.default_rng(5)
+    p = torch.from_numpy(rng.standard_normal(n).astype(np.float32)).cuda()
+    want, m, v = p.cpu().double(), torch.zeros(n).double(), torch.zeros(n).double()
+    g = torch.empty(n, device="cuda")
+    tl = adamw_list([p], [g], state_bits=bits)
+    cfg = config(bits=bits, rounding=E.EA_ROUND_STOCHASTIC if bits == 8 else 0, seed=9)
+    for t in range(1, steps + 1):
+        grad = torch.from_numpy(rng.standard_normal(n).astype(np.float32))
+        g.copy_(grad)
+        E.ea_adamw_step(cfg, t, tl)
+        s = R.Step(want, grad.double(), m, v, t, **HYPER)
+        want, m, v = s.p, s.m, s.v
+    off = (p.cpu().double() - want).abs().max().item()
+    # 32 bits: each step rounds p and its update, of size <= 3 lr sqrt(20), a few times; 8 bits: an update's
+    # relative error stays under two code steps
+    move = steps * HYPER["lr"] * math.sqrt(1 / (1 - HYPER["beta2"]))
+    assert off <= (steps * 40 * R.U32 * (5 + move) if bits == 32 else 0.25 * move), off
+
+
+def test_stochastic_rounding_keeps_the_average():
+    """A state that decays by 1% a step under a block maximum that does not: to nearest it never moves,
+    with draws its mean over many elements follows."""
+    n, steps = 256 * 64, 40
+    res = {}
+    for rounding in (E.EA_ROUND_NEAREST, E.EA_ROUND_STOCHASTIC):
+        g = torch.zeros(n, device="cuda")
+        g[::256] = 1.0
+        p = torch.zeros(n, device="cuda")
+        tl = adamw_list([p], [g], state_bits=8)
+        cfg = config(bits=8, rounding=rounding, seed=77, beta1=0.99, beta2=0.99)
+        x = np.full((64, 256), 0.3, np.float32)
+        x[:, 0] = 1.0
+        codes, scales = R.encode32(x, False)
+        tl.states[0].view(torch.uint8).copy_(torch.from_numpy(codes))
+        tl.scales[0].copy_(torch.from_numpy(scales))
+        start = R.decode(codes, scales).view(64, 256)[:, 1:].mean().item()
+        for t in range(1, steps + 1):
+            E.ea_adamw_step(cfg, t, tl)
+        end = R.decode(tl.states[0].view(torch.uint8).cpu().numpy(), tl.scales[0].cpu().numpy())
+        res[rounding] = end.view(64, 256)[:, 1:].mean().item() / start
+    assert res[E.EA_ROUND_NEAREST] == pytest.approx(1.0, rel=1e-3)
+    # standard deviation of the mean: 40 steps, each at most a code step of 1/8 over sqrt(16320) elements
+    assert res[E.EA_ROUND_STOCHASTIC] == pytest.approx(0.99 ** steps, abs=6 * 0.125 * math.sqrt(40 / 16320))
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("factor", [float("nan"), float("inf"), -float("inf")])
+def test_a_factor_that_is_not_finite_changes_nothing(bits, factor):
+    P = Problem([5, 300, 1024], bits=bits)
+    before = [flat.clone() for flat, _ in P.flats]
+    E.ea_adamw_step(config(bits=bits), P.t, P.list, torch.full((1,), factor, device="cuda"))
+    for (flat, _), b in zip(P.flats, before):
+        assert torch.equal(flat.view(torch.uint8), b.view(torch.uint8))
+
+
+def test_gradients_that_are_not_finite_show():
+    """32 bits: in the element alone.  8 bits: in the whole block's states, and in no other block."""
+    for bad in (float("nan"), float("inf")):
+        P = Problem([1000], bits=32)
+        P.g[0][300] = bad
+        E.ea_adamw_step(config(), P.t, P.list)
+        odd = torch.zeros(1000, dtype=torch.bool)
+        odd[300] = True
+        for x in (P.m, P.v, P.p):
+            assert torch.equal(~torch.isfinite(x[0].cpu()), odd) or x is P.p
+        assert torch.equal(torch.isnan(P.p[0].cpu()), odd)
+        P = Problem([1000], bits=8)
+        P.g[0][300] = bad
+        E.ea_adamw_step(config(bits=8), P.t, P.list)
+        assert torch.equal(torch.isnan(P.p[0].cpu()), odd)
+        for s in (P.ms, P.vs):
+            assert torch.isnan(s[0].cpu()).tolist() == [False, True, False, False]
+        E.ea_adamw_step(config(bits=8), P.t + 1, P.list)
+        assert torch.isnan(P.p[0].cpu()).nonzero().view(-1).tolist() == list(range(256, 512))
+
+
+def test_small_and_large_blocks():
+    """Blocks of zeros, of values under the smallest normal scale, and a root far under its block's largest."""
+    n = 1024
+    g = torch.zeros(n, device="cuda")
+    g[256:512] = 1e-38
+    g[512] = 1e5
+    g[513] = 1e-6
+    g[768:] = 1e-30
+    p = torch.ones(n, device="cuda")
+    tl = adamw_list([p], [g], state_bits=8)
+    E.ea_adamw_step(config(bits=8), 1, tl)
+    m, v = (x.view(torch.uint8).cpu().numpy() for x in tl.states)
+    assert not m[:512].any() and not v[:512].any() and tl.scales[0][:2].tolist() == [0.0, 0.0]
+    assert v[513] == 1 and v[514] == 0 and m[513] == 0
+    assert torch.isfinite(p).all()
+    # the element with the small root moves by no more than lr times the bound of m / root
+    E.ea_adamw_step(config(bits=8), 2, tl)
+    assert (p - 1).abs().max().item() <= 2 * HYPER["lr"] * math.sqrt(1 / (1 - HYPER["beta2"]))
+
+
+def test_transposed_parameters():
+    """Parameters that are dense in another order: gradient and states in the same memory order."""
+    w = torch.randn(37, 53, device="cuda").t()
+    g = torch.randn(37, 53, device="cuda").t()
+    a, b = w.clone(memory_format=torch.contiguous_format), g.contiguous()
+    la, lb = adamw_list([w], [g]), adamw_list([a], [b])
+    E.ea_adamw_step(config(), 1, la)
+    E.ea_adamw_step(config(), 1, lb)
+    assert torch.equal(w, a)
+
+
+def test_same_bits_from_run_to_run_and_on_another_stream():
+    outs = []
+    for stream in (None, torch.cuda.Stream(), None):
+        P = Problem([12_345, 77, 9], bits=8, seed=4)
+        torch.cuda.synchronize()
+        cfg = config(bits=8, rounding=E.EA_ROUND_STOCHASTIC, seed=5)
+        E.ea_adamw_step(cfg, 3, P.list, stream=stream)
+        torch.cuda.synchronize()
+        outs.append([flat.clone() for flat, _ in P.flats])
+    for o in outs[1:]:
+        for x, y in zip(o, outs[0]):
+            assert torch.equal(x.view(torch.uint8), y.view(torch.uint8))
+
+
+SCHEDULES = [E.Schedule(kind=E.EA_SCHED_CONSTANT),
+             E.Schedule(kind=E.EA_SCHED_ASSUMPTION2, alpha=0.05, theta=20.0, T=400),
+             E.Schedule(kind=E.EA_SCHED_STEP_DECAY, alpha=0.01, factor=0.5, period=2)]
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("sched", SCHEDULES, ids=["constant", "assumption2", "decay"])
+def test_scheduled_steps_in_a_graph_equal_the_host_s(sched, bits):
+    """The step read on the device, captured once and replayed, against ea_adamw_step with the
+    schedule's values at each step."""
+    kw = dict(rounding=E.EA_ROUND_STOCHASTIC, seed=5) if bits == 8 else {}
+    a, b = Problem([700, 3], bits=bits), Problem([700, 3], bits=bits)
+    cfg = config(bits=bits, **kw)
+    t_dev = torch.ones(1, dtype=torch.int32, device="cuda")
+    side = torch.cuda.Stream()
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=side):
+        E.ea_adamw_step_scheduled(cfg, sched, t_dev, a.list)
+    round_cfg = E.Config(d=1, N=1, lr=cfg.lr, beta2=cfg.beta2)
+    for t in range(1, 7):
+        graph.replay()
+        lr, beta2 = E.ea_schedule_at(round_cfg, sched, t)
+        E.ea_adamw_step(config(bits=bits, **{**kw, "lr": lr, "beta2": beta2}), t, b.list)
+        torch.cuda.synchronize()
+        for (x, _), (y, _) in zip(a.flats, b.flats):
+            assert torch.equal(x.view(torch.uint8), y.view(torch.uint8)), f"step {t}"
+    assert t_dev.item() == 7
+
+
+def test_new_gradients_in_the_same_list():
+    P = Problem([100, 2000])
+    other = [torch.full_like(g, 0.5) for g in P.g]
+    P.list.set_grads(other)
+    E.ea_adamw_step(config(), P.t, P.list)
+    P.g0 = [g.cpu() for g in other]
+    for i in range(2):
+        w = P.want(i)
+        R.within(P.p[i], w.p, w.p_bound, f"p[{i}]")
+
+
+def test_no_tensors():
+    E.ea_adamw_step(config(), 1, E.TensorList([], p=[], m=[], v=[]))
+    e = torch.empty(0, device="cuda")
+    E.ea_adamw_step(config(), 1, adamw_list([e], [e.clone()]))
