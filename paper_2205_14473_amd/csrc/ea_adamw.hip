@@ -17,17 +17,6 @@ namespace {
 constexpr float kCodeMax = 448.0f;        // largest E4M3 value
 constexpr float kLeastNormal = 0x1p-126f;
 
-// b^t by square-and-multiply from the lowest bit.
-__device__ __forceinline__ double ipow(double b, uint32_t t)
-{
-    double r = 1.0;
-    for (; t; t >>= 1) {
-        if (t & 1) r = r * b;
-        b = b * b;
-    }
-    return r;
-}
-
 // lr and beta2 of the schedule at step t (as defined with ea_schedule_t).
 __device__ __forceinline__ void schedule_at(const ea_schedule_t& s, uint32_t t, float& lr, float& beta2)
 {
@@ -70,24 +59,26 @@ struct Factors {
 
 __device__ __forceinline__ Factors factors_of(const AdamwArgs& a, const TensorPart& e, float gs)
 {
-    float lr = a.lr, beta2 = a.beta2;
-    uint32_t t = a.t;
-    if (a.t_dev) {
-        t = *a.t_dev;
-        schedule_at(a.sched, t, lr, beta2);
-    }
-    const double lri = (double)lr * (double)e.lr_scale;
     Factors f;
-    f.t = t;
+    float lr = a.lr, beta2 = a.beta2;
+    f.t = a.t;
+    f.root = a.root;
+    f.step = e.step;
+    f.keep = e.keep;
+    if (a.t_dev) {
+        f.t = *a.t_dev;
+        schedule_at(a.sched, f.t, lr, beta2);
+        const double lri = (double)lr * (double)e.step;
+        f.root = uniform(adamw_root(beta2, f.t));
+        f.keep = uniform(adamw_keep(lri, e.keep));
+        f.step = uniform(adamw_step_size(lri, a.beta1, f.t));
+    }
     f.gs = gs;
     f.b1 = a.beta1;
-    f.a1 = (float)(1.0 - (double)a.beta1);
+    f.a1 = uniform(1.0f - a.beta1);      // the exact difference, rounded once
     f.b2 = beta2;
-    f.a2 = (float)(1.0 - (double)beta2);
+    f.a2 = uniform(1.0f - beta2);
     f.eps = a.eps;
-    f.root = (float)(1.0 / sqrt(1.0 - ipow((double)beta2, t)));
-    f.step = (float)(lri / (1.0 - ipow((double)a.beta1, t)));
-    f.keep = (float)(1.0 - lri * (double)e.weight_decay);
     return f;
 }
 
@@ -105,23 +96,26 @@ __device__ __forceinline__ void adamw_element(const Factors& f, float g, float& 
 
 constexpr int kAdamwBlock = 256;
 
+// One quad a thread.  With two or four a thread, loads ahead of the arithmetic,
+// the step of 355M parameters took 1689 and 1705 us against 1653; the caches
+// left out of loads and stores are the larger part (1834 with them, one quad).
 template <class P, class G>
-__device__ __forceinline__ void adamw32_quad(const Factors& f, const TensorPart& e, int64_t i, int n)
+__device__ __forceinline__ void adamw32_quad(const Factors& f, const TensorPart& e, uint32_t i, int n)
 {
     const G* gp = (const G*)e.g + i;
     P* pp = (P*)e.p + i;
     float* mp = (float*)e.m + i;
     float* vp = (float*)e.v + i;
     float* wp = e.master ? e.master + i : nullptr;
-    const bool whole = n >= 4;
-    const v4f g = widen(whole ? load4(gp) : load_some(gp, n));
-    v4f m = whole ? load4(mp) : load_some(mp, n);
-    v4f v = whole ? load4(vp) : load_some(vp, n);
+    const bool four = n == 4;
+    const v4f g = widen(four ? load4_once(gp) : load_some(gp, n));
+    v4f m = four ? load4_once(mp) : load_some(mp, n);
+    v4f v = four ? load4_once(vp) : load_some(vp, n);
     v4f p;
     if (wp)
-        p = whole ? load4(wp) : load_some(wp, n);
+        p = four ? load4_once(wp) : load_some(wp, n);
     else
-        p = widen(whole ? load4(pp) : load_some(pp, n));
+        p = widen(four ? load4_once(pp) : load_some(pp, n));
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
         float mk = m[k], vk = v[k], pk = p[k], r;
@@ -130,11 +124,11 @@ __device__ __forceinline__ void adamw32_quad(const Factors& f, const TensorPart&
         v[k] = vk;
         p[k] = pk;
     }
-    if (whole) {
-        store4(mp, m);
-        store4(vp, v);
-        if (wp) store4(wp, p);
-        store4(pp, narrow<P>(p));
+    if (four) {
+        store4_once(mp, m);
+        store4_once(vp, v);
+        if (wp) store4_once(wp, p);
+        store4_once(pp, narrow<P>(p));
     } else {
         store_some(mp, m, n);
         store_some(vp, v, n);
@@ -151,25 +145,20 @@ __global__ void __launch_bounds__(kAdamwBlock) adamw32_kernel(AdamwArgs a)
     const int at = __builtin_amdgcn_readfirstlane(part_of<kListParts>(a.first, a.count, blockIdx.x));
     const TensorPart& e = a.part[at];
     const Factors f = factors_of(a, e, gs);
-    const int64_t i = (int64_t)(blockIdx.x - a.first[at]) * (kAdamwBlock * 4) + threadIdx.x * 4;
+    const uint32_t i = ((blockIdx.x - a.first[at]) * kAdamwBlock + threadIdx.x) * 4;
     if (i < e.n) adamw32_quad<P, G>(f, e, i, e.n - i < 4 ? (int)(e.n - i) : 4);
 }
 
 // ---- states in 8 bits ------------------------------------------------------------
 
-// Largest bit pattern of the wave: the largest magnitude of patterns without
-// sign, an infinity above every number and a NaN above that.
-__device__ __forceinline__ uint32_t wave_umax(uint32_t v)
+// Largest bit pattern of a row of 16 lanes: of patterns without sign, an
+// infinity stands above every number and a NaN above that.
+__device__ __forceinline__ uint32_t row_umax(uint32_t v)
 {
     v = max(v, dpp<kDppXor1>(v));
     v = max(v, dpp<kDppXor2>(v));
     v = max(v, dpp<kDppHalfMirror>(v));
-    v = max(v, dpp<kDppRowMirror>(v));
-    uint32_t a, b;
-    row_swap16(v, a, b);
-    v = max(a, b);
-    row_swap32(v, a, b);
-    return max(a, b);
+    return max(v, dpp<kDppRowMirror>(v));
 }
 
 __device__ __forceinline__ uint32_t magnitude(float x)
@@ -178,37 +167,48 @@ __device__ __forceinline__ uint32_t magnitude(float x)
 }
 
 // The block's scale from its largest magnitude: 0 below the normal numbers
-// (the block is kept as zeros), NaN for an infinity or NaN (as is every value then).
-__device__ __forceinline__ float block_scale(uint32_t top)
+// (the block is kept as zeros), NaN for an infinity or NaN (as is every value
+// then).  `inv` is 1 / scale, and 0 in both those cases.
+__device__ __forceinline__ float block_scale(uint32_t top, float& inv)
 {
-    const float s = __uint_as_float(top) * (1.0f / kCodeMax);
-    if (top >= 0x7F800000u) return __uint_as_float(0x7FC00000u);
-    return s < kLeastNormal ? 0.0f : s;
+    float s = __uint_as_float(top) * (1.0f / kCodeMax);
+    s = s < kLeastNormal ? 0.0f : s;
+    const bool odd = top >= 0x7F800000u;
+    inv = s > 0.0f && !odd ? 1.0f / s : 0.0f;
+    return odd ? __uint_as_float(0x7FC00000u) : s;
 }
 
-// |y| rounded by the 16-bit draw u to one of its two neighbours in E4M3, whose
+// y >= 0 rounded by the 16-bit draw u to one of its two neighbours in E4M3, whose
 // quantum is 2^-9 below 2^-6 and three fraction bits above.
 __device__ __forceinline__ float round_by(float y, uint32_t u)
 {
     const uint32_t up = (__float_as_uint(y) + ((u << 4) | 8u)) & ~0xFFFFFu;
     const float low = floorf(y * 512.0f + ((float)u + 0.5f) * 0x1p-16f) * 0x1p-9f;
-    return y < 0x1p-6f ? low : __uint_as_float(up);
+    return fminf(y < 0x1p-6f ? low : __uint_as_float(up), kCodeMax);
 }
 
-// Four values over the scale as E4M3 codes, one a byte.
+// A value over its block's scale, on or between E4M3 numbers: with a finite
+// value at most 448 and a few units in the last place, which the conversion
+// rounds to 448.  (With inv = 0 an infinity or NaN becomes a NaN: the scale says so.)
 template <bool DRAWS>
-__device__ __forceinline__ uint32_t codes_of(v4f x, float scale, const uint32_t* u)
+__device__ __forceinline__ float over_scale(float x, float inv, uint32_t u)
 {
-    if (!(scale > 0.0f)) return 0;
-    const float inv = 1.0f / scale;
-    float y[4];
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        float a = fabsf(x[k] * inv);
-        if (DRAWS) a = round_by(a, u[k]);
-        y[k] = __builtin_copysignf(fminf(a, kCodeMax), x[k]);
-    }
-    uint32_t c = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
+    const float y = x * inv;
+    return DRAWS ? __builtin_copysignf(round_by(fabsf(y), u), y) : y;
+}
+
+// The same of a root.  A positive one is at least `least`, 2^-9 (0 where inv
+// is 0): below it, to nearest, are 0 and that code only.
+template <bool DRAWS>
+__device__ __forceinline__ float root_over_scale(float x, float inv, float least, uint32_t u)
+{
+    const float y = fmaxf(x * inv, x > 0.0f ? least : 0.0f);
+    return DRAWS ? round_by(y, u) : y;
+}
+
+__device__ __forceinline__ uint32_t pack_codes(const float* y)
+{
+    const uint32_t c = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
     return __builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], c, true);
 }
 
@@ -219,20 +219,10 @@ __device__ __forceinline__ v4f values_of(uint32_t c, float scale)
     return v4f{a[0] * scale, a[1] * scale, b[0] * scale, b[1] * scale};
 }
 
-// A positive root's code 0 becomes 1 (2^-9 of the scale).
-__device__ __forceinline__ uint32_t lift_zeros(uint32_t c, v4f r, float scale)
-{
-    if (!(scale > 0.0f)) return c;
-#pragma unroll
-    for (int k = 0; k < 4; ++k)
-        if (r[k] > 0.0f && ((c >> (8 * k)) & 0x7Fu) == 0) c |= 1u << (8 * k);
-    return c;
-}
-
 __device__ __forceinline__ uint32_t load_codes(const uint8_t* p, int n)
 {
     typedef uint32_t word __attribute__((aligned(1)));
-    if (n >= 4) return *(const word*)p;
+    if (n >= 4) return __builtin_nontemporal_load((const word*)p);
     uint32_t c = 0;
     if (n > 0) c |= p[0];
     if (n > 1) c |= (uint32_t)p[1] << 8;
@@ -244,7 +234,7 @@ __device__ __forceinline__ void store_codes(uint8_t* p, uint32_t c, int n)
 {
     typedef uint32_t word __attribute__((aligned(1)));
     if (n >= 4) {
-        *(word*)p = c;
+        __builtin_nontemporal_store(c, (word*)p);
         return;
     }
     if (n > 0) p[0] = (uint8_t)c;
@@ -252,7 +242,195 @@ __device__ __forceinline__ void store_codes(uint8_t* p, uint32_t c, int n)
     if (n > 2) p[2] = (uint8_t)(c >> 16);
 }
 
-// One wave, one block of 256 elements; lane l holds elements 4l to 4l+3.
+constexpr int kRowLanes = 16;            // lanes that share a block of the 8-bit states
+constexpr int kRowQuads = EA_STATE_BLOCK / 4 / kRowLanes;
+constexpr uint32_t kWaveElements = (kWave / kRowLanes) * EA_STATE_BLOCK;
+
+// Root and quotient by one correction step on the hardware's approximations:
+// rounded as sqrtf and the division do but for about one value in a million,
+// which is one unit in the last place off.  Those two check for operands that
+// the approximations do not take (29 instructions an element together, of 45;
+// here 12), which is left to plain_square below.
+__device__ __forceinline__ float root_of(float v)
+{
+    const float y = __builtin_amdgcn_rsqf(fmaxf(v, kLeastNormal));
+    const float s = v * y;
+    return fmaf(fmaf(-s, s, v), 0.5f * y, s);
+}
+
+__device__ __forceinline__ float quotient(float a, float b)
+{
+    float y = __builtin_amdgcn_rcpf(b);
+    y = fmaf(fmaf(-b, y, 1.0f), y, y);
+    const float q = a * y;
+    return fmaf(fmaf(-b, q, a), y, q);
+}
+
+// Neither subnormal, infinite nor NaN.
+__device__ __forceinline__ bool plain_square(float v)
+{
+    return !__builtin_amdgcn_classf(v, 0x003 | 0x004 | 0x010 | 0x080 | 0x200);
+}
+
+constexpr float kLeastEps = 0x1p-100f;   // below, quotient's reciprocal could leave the normal numbers
+
+// The codes of a quad of first moments and roots, in place of the old ones.
+template <bool DRAWS>
+__device__ __forceinline__ void store_states(const AdamwArgs& a, const Factors& f, const TensorPart& e, uint32_t at,
+                                             uint8_t* mp, uint8_t* vp, v4f m, v4f r, float minv, float rinv, int n)
+{
+    const float least = rinv > 0.0f ? 0x1p-9f : 0.0f;
+    uint4 w = {0, 0, 0, 0};
+    if (DRAWS) {
+        const uint64_t quad = ((uint64_t)e.piece * kPartElements + at) >> 2;
+        w = philox10(make_uint4((uint32_t)quad, (uint32_t)(quad >> 32), f.t, e.index), a.k0, a.k1);
+    }
+    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+    float ym[4], yr[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        ym[k] = over_scale<DRAWS>(m[k], minv, u[k] >> 16);
+        yr[k] = root_over_scale<DRAWS>(r[k], rinv, least, u[k] & 0xFFFFu);
+    }
+    store_codes(mp, pack_codes(ym), n);
+    store_codes(vp, pack_codes(yr), n);
+}
+
+// One wave, four blocks of 256 elements: each row of 16 lanes has one, a lane
+// its quads j, j + 16, j + 32, j + 48, so that the block's largest magnitude
+// takes four steps within the row, and its scale serves 16 elements a lane.
+// The form for any values and any number of elements.
+template <class P, class G, bool DRAWS>
+__device__ __forceinline__ void adamw8_any(const AdamwArgs& a, const Factors& f, const TensorPart& e, uint32_t begin)
+{
+    const int lane = lane_id(), row = lane / kRowLanes;
+    const uint32_t block = begin / EA_STATE_BLOCK + row;
+    if (block * (uint64_t)EA_STATE_BLOCK >= e.n) return;
+    const float ms0 = e.m_scale[block], rs0 = e.v_scale[block];
+    v4f m[kRowQuads], r[kRowQuads];
+    uint32_t mtop = 0, rtop = 0;
+#pragma unroll
+    for (int q = 0; q < kRowQuads; ++q) {
+        const uint32_t i = block * EA_STATE_BLOCK + (q * kRowLanes + lane % kRowLanes) * 4;
+        const int n = i >= e.n ? 0 : e.n - i < 4 ? (int)(e.n - i) : 4;
+        const G* gp = (const G*)e.g + i;
+        P* pp = (P*)e.p + i;
+        float* wp = e.master ? e.master + i : nullptr;
+        const v4f g = widen(n == 4 ? load4_once(gp) : load_some(gp, n));
+        v4f p;
+        if (wp)
+            p = n == 4 ? load4_once(wp) : load_some(wp, n);
+        else
+            p = widen(n == 4 ? load4_once(pp) : load_some(pp, n));
+        m[q] = values_of(load_codes((uint8_t*)e.m + i, n), ms0);
+        r[q] = values_of(load_codes((uint8_t*)e.v + i, n), rs0);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            float mk = m[q][k], vk = r[q][k] * r[q][k], rk, pk = p[k];
+            adamw_element(f, g[k], mk, vk, rk, pk);
+            m[q][k] = mk;
+            r[q][k] = rk;
+            p[k] = pk;
+            if (k < n) {
+                mtop = max(mtop, magnitude(mk));
+                rtop = max(rtop, magnitude(rk));
+            }
+        }
+        if (n == 4) {
+            if (wp) store4_once(wp, p);
+            store4_once(pp, narrow<P>(p));
+        } else {
+            if (wp) store_some(wp, p, n);
+            store_some(pp, narrow<P>(p), n);
+        }
+    }
+    float minv, rinv;
+    const float ms = block_scale(row_umax(mtop), minv), rs = block_scale(row_umax(rtop), rinv);
+#pragma unroll
+    for (int q = 0; q < kRowQuads; ++q) {
+        const uint32_t i = block * EA_STATE_BLOCK + (q * kRowLanes + lane % kRowLanes) * 4;
+        const int n = i >= e.n ? 0 : e.n - i < 4 ? (int)(e.n - i) : 4;
+        store_states<DRAWS>(a, f, e, i, (uint8_t*)e.m + i, (uint8_t*)e.v + i, m[q], r[q], minv, rinv, n);
+    }
+    if (lane % kRowLanes == 0) {
+        e.m_scale[block] = ms;
+        e.v_scale[block] = rs;
+    }
+}
+
+// The same for four whole blocks and values that root_of and quotient take,
+// as nearly all are; false, with nothing written, where one is not.
+template <class P, class G, bool DRAWS, bool MASTER>
+__device__ __forceinline__ bool adamw8_four(const AdamwArgs& a, const Factors& f, const TensorPart& e, uint32_t begin)
+{
+    const int lane = lane_id(), row = lane / kRowLanes;
+    const uint32_t block = begin / EA_STATE_BLOCK;
+    const uint32_t first = (row * EA_STATE_BLOCK + (lane % kRowLanes) * 4);
+    const G* gp = (const G*)e.g + begin;
+    P* pp = (P*)e.p + begin;
+    float* wp = MASTER ? e.master + begin : nullptr;
+    uint8_t* mp = (uint8_t*)e.m + begin;
+    uint8_t* vp = (uint8_t*)e.v + begin;
+    v4f p[kRowQuads], m[kRowQuads], r[kRowQuads];
+    typename Quad<G>::vec g[kRowQuads];
+    typename Quad<P>::vec pn[kRowQuads];
+    uint32_t cm[kRowQuads], cr[kRowQuads];
+    const float ms0 = (e.m_scale + block)[row], rs0 = (e.v_scale + block)[row];
+#pragma unroll
+    for (int q = 0; q < kRowQuads; ++q) {
+        const uint32_t at = first + q * kRowLanes * 4;
+        cm[q] = load_codes(mp + at, 4);
+        cr[q] = load_codes(vp + at, 4);
+        g[q] = load4_once(gp + at);
+        if (MASTER)
+            p[q] = load4_once(wp + at);
+        else
+            pn[q] = load4_once(pp + at);
+    }
+    float mtop = 0.0f, rtop = 0.0f;
+    bool fine = ms0 == ms0;
+#pragma unroll
+    for (int q = 0; q < kRowQuads; ++q) {
+        m[q] = values_of(cm[q], ms0);
+        r[q] = values_of(cr[q], rs0);
+        if (!MASTER) p[q] = widen(pn[q]);
+        const v4f gq = widen(g[q]);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const float gk = gq[k] * f.gs;
+            const float mk = m[q][k] * f.b1 + gk * f.a1;
+            const float vk = (r[q][k] * r[q][k]) * f.b2 + (gk * gk) * f.a2;
+            const float rk = root_of(vk);
+            fine &= plain_square(vk);
+            p[q][k] = p[q][k] * f.keep - quotient(mk, rk * f.root + f.eps) * f.step;
+            m[q][k] = mk;
+            r[q][k] = rk;
+            mtop = fmaxf(mtop, fabsf(mk));
+            rtop = fmaxf(rtop, rk);
+        }
+    }
+    if (__ballot(!fine)) return false;
+#pragma unroll
+    for (int q = 0; q < kRowQuads; ++q) {
+        const uint32_t at = first + q * kRowLanes * 4;
+        if (MASTER) store4_once(wp + at, p[q]);
+        store4_once(pp + at, narrow<P>(p[q]));
+    }
+    float minv, rinv;
+    const float ms = block_scale(row_umax(__float_as_uint(mtop)), minv);
+    const float rs = block_scale(row_umax(__float_as_uint(rtop)), rinv);
+#pragma unroll
+    for (int q = 0; q < kRowQuads; ++q) {
+        const uint32_t at = first + q * kRowLanes * 4;
+        store_states<DRAWS>(a, f, e, begin + at, mp + at, vp + at, m[q], r[q], minv, rinv, 4);
+    }
+    if (lane % kRowLanes == 0) {
+        (e.m_scale + block)[row] = ms;
+        (e.v_scale + block)[row] = rs;
+    }
+    return true;
+}
+
 template <class P, class G, bool DRAWS>
 __global__ void __launch_bounds__(kAdamwBlock) adamw8_kernel(AdamwArgs a)
 {
@@ -260,65 +438,15 @@ __global__ void __launch_bounds__(kAdamwBlock) adamw8_kernel(AdamwArgs a)
     if (!__builtin_isfinite(gs)) return;
     const int at = __builtin_amdgcn_readfirstlane(part_of<kListParts>(a.first, a.count, blockIdx.x));
     const TensorPart& e = a.part[at];
+    const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const uint32_t begin = ((blockIdx.x - a.first[at]) * kWavesPerBlock + wave) * kWaveElements;
+    if (begin >= e.n) return;
     const Factors f = factors_of(a, e, gs);
-    const int64_t block = (int64_t)(blockIdx.x - a.first[at]) * kWavesPerBlock + threadIdx.x / kWave;
-    const int64_t i = block * EA_STATE_BLOCK + lane_id() * 4;
-    if (block * EA_STATE_BLOCK >= e.n) return;
-    const int n = i >= e.n ? 0 : e.n - i < 4 ? (int)(e.n - i) : 4;
-    const bool whole = n == 4;
-    const G* gp = (const G*)e.g + i;
-    P* pp = (P*)e.p + i;
-    uint8_t* mp = (uint8_t*)e.m + i;
-    uint8_t* vp = (uint8_t*)e.v + i;
-    float* wp = e.master ? e.master + i : nullptr;
-    const v4f g = widen(whole ? load4(gp) : load_some(gp, n));
-    v4f m = values_of(load_codes(mp, n), e.m_scale[block]);
-    v4f r = values_of(load_codes(vp, n), e.v_scale[block]);
-    v4f p;
-    if (wp)
-        p = whole ? load4(wp) : load_some(wp, n);
-    else
-        p = widen(whole ? load4(pp) : load_some(pp, n));
-    uint32_t mtop = 0, rtop = 0;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        float mk = m[k], vk = r[k] * r[k], rk, pk = p[k];
-        adamw_element(f, g[k], mk, vk, rk, pk);
-        m[k] = mk;
-        r[k] = rk;
-        p[k] = pk;
-        if (k < n) {
-            mtop = max(mtop, magnitude(mk));
-            rtop = max(rtop, magnitude(rk));
-        }
-    }
-    const float ms = block_scale(wave_umax(mtop)), rs = block_scale(wave_umax(rtop));
-    uint32_t um[4] = {0, 0, 0, 0}, ur[4] = {0, 0, 0, 0};
-    if (DRAWS) {
-        const uint64_t quad = ((uint64_t)e.piece * kPartElements + (uint64_t)i) >> 2;
-        const uint4 w = philox10(make_uint4((uint32_t)quad, (uint32_t)(quad >> 32), f.t, e.index), a.k0, a.k1);
-        const uint32_t x[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            um[k] = x[k] >> 16;
-            ur[k] = x[k] & 0xFFFFu;
-        }
-    }
-    const uint32_t cm = codes_of<DRAWS>(m, ms, um);
-    const uint32_t cv = lift_zeros(codes_of<DRAWS>(r, rs, ur), r, rs);
-    store_codes(mp, cm, n);
-    store_codes(vp, cv, n);
-    if (whole) {
-        if (wp) store4(wp, p);
-        store4(pp, narrow<P>(p));
-    } else {
-        if (wp) store_some(wp, p, n);
-        store_some(pp, narrow<P>(p), n);
-    }
-    if (lane_id() == 0) {
-        e.m_scale[block] = ms;
-        e.v_scale[block] = rs;
-    }
+    bool done = false;
+    if (e.n - begin >= kWaveElements && f.eps >= kLeastEps)
+        done = sizeof(P) == 2 && e.master ? adamw8_four<P, G, DRAWS, true>(a, f, e, begin)
+                                          : adamw8_four<P, G, DRAWS, false>(a, f, e, begin);
+    if (!done) adamw8_any<P, G, DRAWS>(a, f, e, begin);
 }
 
 template <class P, class G>
@@ -371,7 +499,7 @@ __global__ void __launch_bounds__(kNormBlock) norm_kernel(NormArgs a)
     const G* g = (const G*)a.part[at].g;
     double sum = 0.0;
     for (int64_t i = begin + threadIdx.x * 4; i < end; i += kNormBlock * 4) {
-        const v4f x = widen(end - i >= 4 ? load4(g + i) : load_some(g + i, (int)(end - i)));
+        const v4f x = widen(end - i >= 4 ? load4_once(g + i) : load_some(g + i, (int)(end - i)));
 #pragma unroll
         for (int k = 0; k < 4; ++k) sum = fma((double)x[k], (double)x[k], sum);
     }
@@ -401,12 +529,12 @@ __global__ void __launch_bounds__(kFinishBlock) norm_finish_kernel(const double*
 
 }  // namespace
 
-int64_t adamw_chunk(int64_t)
+int64_t adamw_chunk(const ea_adamw_t& c)
 {
-    return kAdamwBlock * 4;
+    return c.state_bits == 8 ? kWavesPerBlock * kWaveElements : kAdamwBlock * 4;
 }
 
-hipError_t launch_adamw(const AdamwArgs& a, const ea_adamw_t& c, int64_t, hipStream_t s)
+hipError_t launch_adamw(const AdamwArgs& a, const ea_adamw_t& c, hipStream_t s)
 {
     if (a.count < 1 || a.first[a.count] == 0) return hipSuccess;
     if (c.param_type == EA_F32)

@@ -36,6 +36,19 @@ __device__ __forceinline__ void store4(T* p, typename Quad<T>::vec v)
     *(typename Quad<T>::unaligned*)p = v;
 }
 
+// The same for data that a pass reads or writes once: it leaves the caches to others.
+template <class T>
+__device__ __forceinline__ typename Quad<T>::vec load4_once(const T* p)
+{
+    return __builtin_nontemporal_load((const typename Quad<T>::unaligned*)p);
+}
+
+template <class T>
+__device__ __forceinline__ void store4_once(T* p, typename Quad<T>::vec v)
+{
+    __builtin_nontemporal_store(v, (typename Quad<T>::unaligned*)p);
+}
+
 template <class T>
 __device__ __forceinline__ v4f widen(T v)
 {
@@ -79,7 +92,9 @@ struct TensorPart {
     float* v_scale;
     float* master;
     uint32_t n;                            // at most 2^30
-    float weight_decay, lr_scale;
+    // The factors of a step known to the host: 1 - lr_i wd and lr_i / (1 - beta1^t); of one read on the
+    // device (t_dev): wd and the factor on the learning rate.
+    float keep, step;
     uint32_t index;                        // of the tensor in the call's list
     uint32_t piece;                        // its first element is piece * 2^30
 };
@@ -93,6 +108,7 @@ constexpr uint32_t kMostGroups = 1u << 23;
 struct AdamwArgs {
     // The step's values from the host, or (t_dev) from the device's step and the schedule.
     float lr, beta1, beta2, eps;
+    float root;                            // 1 / sqrt(1 - beta2^t) (t_dev: unset)
     uint32_t t;
     uint32_t k0, k1;                       // Philox key
     int32_t count;                         // parts
@@ -104,9 +120,32 @@ struct AdamwArgs {
 };
 static_assert(sizeof(AdamwArgs) <= 4096, "kernel arguments");
 
-// Elements per workgroup of a call of `total` elements: what `first` counts in.
-int64_t adamw_chunk(int64_t total);
-hipError_t launch_adamw(const AdamwArgs& a, const ea_adamw_t& c, int64_t chunk, hipStream_t s);
+// The step's factors, formed in binary64 and rounded once, on the host or on the device alike.
+__host__ __device__ inline double adamw_power(double b, uint32_t t)
+{
+    double r = 1.0;
+    for (; t; t >>= 1) {
+        if (t & 1) r = r * b;
+        b = b * b;
+    }
+    return r;
+}
+__host__ __device__ inline float adamw_root(float beta2, uint32_t t)
+{
+    return (float)(1.0 / sqrt(1.0 - adamw_power((double)beta2, t)));
+}
+__host__ __device__ inline float adamw_step_size(double lri, float beta1, uint32_t t)
+{
+    return (float)(lri / (1.0 - adamw_power((double)beta1, t)));
+}
+__host__ __device__ inline float adamw_keep(double lri, float wd)
+{
+    return (float)(1.0 - lri * (double)wd);
+}
+
+// Elements per workgroup: what `first` counts in.
+int64_t adamw_chunk(const ea_adamw_t& c);
+hipError_t launch_adamw(const AdamwArgs& a, const ea_adamw_t& c, hipStream_t s);
 
 // ---- gradient norm ------------------------------------------------------------
 

@@ -113,8 +113,9 @@ int adamw_impl(const char* name, const ea_adamw_t* c, const ea_schedule_t* s, in
     a.k1 = (uint32_t)(c->seed >> 32);
     a.gscale = gscale;
     a.t_dev = t_dev;
+    if (!t_dev) a.root = ea::adamw_root(c->beta2, a.t);
     if (s) a.sched = *s;
-    const int64_t chunk = ea::adamw_chunk(total);
+    const int64_t chunk = ea::adamw_chunk(*c);
     const int64_t state = c->state_bits / 8;
     const int64_t gb = (int64_t)type_bytes(c->grad_type), pb = (int64_t)type_bytes(c->param_type);
     const hipStream_t st = (hipStream_t)stream;
@@ -124,7 +125,7 @@ int adamw_impl(const char* name, const ea_adamw_t* c, const ea_schedule_t* s, in
             const int64_t left = tensors[i].n - at, n = left < ea::kPartElements ? left : ea::kPartElements;
             const uint32_t groups = (uint32_t)((n + chunk - 1) / chunk);
             if (a.count == ea::kListParts || a.first[a.count] + groups > ea::kMostGroups) {
-                e = ea::launch_adamw(a, *c, chunk, st);
+                e = ea::launch_adamw(a, *c, st);
                 a.count = 0;
                 if (e != hipSuccess) break;
             }
@@ -137,14 +138,20 @@ int adamw_impl(const char* name, const ea_adamw_t* c, const ea_schedule_t* s, in
             p.v_scale = state == 1 ? past(tensors[i].v_scale, at / EA_STATE_BLOCK, 4) : nullptr;
             p.master = past(tensors[i].master, at, 4);
             p.n = (uint32_t)n;
-            p.weight_decay = tensors[i].weight_decay;
-            p.lr_scale = tensors[i].lr_scale;
+            if (t_dev) {
+                p.keep = tensors[i].weight_decay;
+                p.step = tensors[i].lr_scale;
+            } else {
+                const double lri = (double)c->lr * (double)tensors[i].lr_scale;
+                p.keep = ea::adamw_keep(lri, tensors[i].weight_decay);
+                p.step = ea::adamw_step_size(lri, c->beta1, a.t);
+            }
             p.index = (uint32_t)i;
             p.piece = (uint32_t)(at / ea::kPartElements);
             a.first[a.count + 1] = a.first[a.count] + groups;
             ++a.count;
         }
-    if (e == hipSuccess) e = ea::launch_adamw(a, *c, chunk, st);
+    if (e == hipSuccess) e = ea::launch_adamw(a, *c, st);
     if (e == hipSuccess && t_dev) e = ea::launch_advance(t_dev, st);
     return hip_status(e, name);
 }
