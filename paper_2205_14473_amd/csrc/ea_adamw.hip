@@ -151,6 +151,8 @@ __global__ void __launch_bounds__(kAdamwBlock) adamw32_kernel(AdamwArgs a)
 
 // ---- states in 8 bits ------------------------------------------------------------
 
+constexpr int kRowLanes = 32;            // lanes that share a block of the 8-bit states
+
 // Largest bit pattern of a row of 16 lanes: of patterns without sign, an
 // infinity stands above every number and a NaN above that.
 __device__ __forceinline__ uint32_t row_umax(uint32_t v)
@@ -158,7 +160,17 @@ __device__ __forceinline__ uint32_t row_umax(uint32_t v)
     v = max(v, dpp<kDppXor1>(v));
     v = max(v, dpp<kDppXor2>(v));
     v = max(v, dpp<kDppHalfMirror>(v));
-    return max(v, dpp<kDppRowMirror>(v));
+    v = max(v, dpp<kDppRowMirror>(v));
+    uint32_t a, b;
+    if (kRowLanes >= 32) {
+        row_swap16(v, a, b);
+        v = max(a, b);
+    }
+    if (kRowLanes >= 64) {
+        row_swap32(v, a, b);
+        v = max(a, b);
+    }
+    return v;
 }
 
 __device__ __forceinline__ uint32_t magnitude(float x)
@@ -242,7 +254,6 @@ __device__ __forceinline__ void store_codes(uint8_t* p, uint32_t c, int n)
     if (n > 2) p[2] = (uint8_t)(c >> 16);
 }
 
-constexpr int kRowLanes = 16;            // lanes that share a block of the 8-bit states
 constexpr int kRowQuads = EA_STATE_BLOCK / 4 / kRowLanes;
 constexpr uint32_t kWaveElements = (kWave / kRowLanes) * EA_STATE_BLOCK;
 
@@ -272,6 +283,7 @@ __device__ __forceinline__ bool plain_square(float v)
     return !__builtin_amdgcn_classf(v, 0x003 | 0x004 | 0x010 | 0x080 | 0x200);
 }
 
+constexpr int64_t kShortRuns = 1 << 25;  // elements of a call below which a wave takes one group
 constexpr float kLeastEps = 0x1p-100f;   // below, quotient's reciprocal could leave the normal numbers
 
 // The codes of a quad of first moments and roots, in place of the old ones.
@@ -296,9 +308,8 @@ __device__ __forceinline__ void store_states(const AdamwArgs& a, const Factors& 
     store_codes(vp, pack_codes(yr), n);
 }
 
-// One wave, four blocks of 256 elements: each row of 16 lanes has one, a lane
-// its quads j, j + 16, j + 32, j + 48, so that the block's largest magnitude
-// takes four steps within the row, and its scale serves 16 elements a lane.
+// One wave, two blocks of 256 elements: each row of 32 lanes has one, a lane
+// its quads j and j + 32.
 // The form for any values and any number of elements.
 template <class P, class G, bool DRAWS>
 __device__ __forceinline__ void adamw8_any(const AdamwArgs& a, const Factors& f, const TensorPart& e, uint32_t begin)
@@ -358,46 +369,60 @@ __device__ __forceinline__ void adamw8_any(const AdamwArgs& a, const Factors& f,
     }
 }
 
-// The same for four whole blocks and values that root_of and quotient take,
-// as nearly all are; false, with nothing written, where one is not.
-template <class P, class G, bool DRAWS, bool MASTER>
-__device__ __forceinline__ bool adamw8_four(const AdamwArgs& a, const Factors& f, const TensorPart& e, uint32_t begin)
-{
-    const int lane = lane_id(), row = lane / kRowLanes;
-    const uint32_t block = begin / EA_STATE_BLOCK;
-    const uint32_t first = (row * EA_STATE_BLOCK + (lane % kRowLanes) * 4);
-    const G* gp = (const G*)e.g + begin;
-    P* pp = (P*)e.p + begin;
-    float* wp = MASTER ? e.master + begin : nullptr;
-    uint8_t* mp = (uint8_t*)e.m + begin;
-    uint8_t* vp = (uint8_t*)e.v + begin;
-    v4f p[kRowQuads], m[kRowQuads], r[kRowQuads];
-    typename Quad<G>::vec g[kRowQuads];
-    typename Quad<P>::vec pn[kRowQuads];
+// What a lane reads of its block, as it is kept.
+template <class P, class G, bool MASTER>
+struct Held {
     uint32_t cm[kRowQuads], cr[kRowQuads];
-    const float ms0 = (e.m_scale + block)[row], rs0 = (e.v_scale + block)[row];
+    typename Quad<G>::vec g[kRowQuads];
+    typename Quad<P>::vec p[kRowQuads];
+    v4f w[kRowQuads];
+    float ms, rs;
+};
+
+// First of a lane's elements among its wave's; its others follow 4 kRowLanes apart.
+__device__ __forceinline__ uint32_t first_of_lane()
+{
+    return (lane_id() / kRowLanes) * EA_STATE_BLOCK + (lane_id() % kRowLanes) * 4;
+}
+
+template <class P, class G, bool MASTER>
+__device__ __forceinline__ void fetch(const TensorPart& e, uint32_t begin, Held<P, G, MASTER>& h)
+{
+    const int row = lane_id() / kRowLanes;
+    h.ms = (e.m_scale + begin / EA_STATE_BLOCK)[row];
+    h.rs = (e.v_scale + begin / EA_STATE_BLOCK)[row];
 #pragma unroll
     for (int q = 0; q < kRowQuads; ++q) {
-        const uint32_t at = first + q * kRowLanes * 4;
-        cm[q] = load_codes(mp + at, 4);
-        cr[q] = load_codes(vp + at, 4);
-        g[q] = load4_once(gp + at);
+        const uint32_t at = first_of_lane() + q * kRowLanes * 4;
+        h.cm[q] = load_codes((const uint8_t*)e.m + begin + at, 4);
+        h.cr[q] = load_codes((const uint8_t*)e.v + begin + at, 4);
+        h.g[q] = load4_once((const G*)e.g + begin + at);
         if (MASTER)
-            p[q] = load4_once(wp + at);
+            h.w[q] = load4_once(e.master + begin + at);
         else
-            pn[q] = load4_once(pp + at);
+            h.p[q] = load4_once((const P*)e.p + begin + at);
     }
+}
+
+// The same for whole blocks, fetched before, and values that root_of and
+// quotient take, as nearly all are; false, with nothing written, where one is not.
+template <class P, class G, bool DRAWS, bool MASTER>
+__device__ __forceinline__ bool adamw8_whole(const AdamwArgs& a, const Factors& f, const TensorPart& e, uint32_t begin,
+                                             const Held<P, G, MASTER>& h)
+{
+    const uint32_t first = first_of_lane();
+    v4f p[kRowQuads], m[kRowQuads], r[kRowQuads];
     float mtop = 0.0f, rtop = 0.0f;
-    bool fine = ms0 == ms0;
+    bool fine = h.ms == h.ms;
 #pragma unroll
     for (int q = 0; q < kRowQuads; ++q) {
-        m[q] = values_of(cm[q], ms0);
-        r[q] = values_of(cr[q], rs0);
-        if (!MASTER) p[q] = widen(pn[q]);
-        const v4f gq = widen(g[q]);
+        m[q] = values_of(h.cm[q], h.ms);
+        r[q] = values_of(h.cr[q], h.rs);
+        p[q] = MASTER ? h.w[q] : widen(h.p[q]);
+        const v4f g = widen(h.g[q]);
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-            const float gk = gq[k] * f.gs;
+            const float gk = g[k] * f.gs;
             const float mk = m[q][k] * f.b1 + gk * f.a1;
             const float vk = (r[q][k] * r[q][k]) * f.b2 + (gk * gk) * f.a2;
             const float rk = root_of(vk);
@@ -412,23 +437,45 @@ __device__ __forceinline__ bool adamw8_four(const AdamwArgs& a, const Factors& f
     if (__ballot(!fine)) return false;
 #pragma unroll
     for (int q = 0; q < kRowQuads; ++q) {
-        const uint32_t at = first + q * kRowLanes * 4;
-        if (MASTER) store4_once(wp + at, p[q]);
-        store4_once(pp + at, narrow<P>(p[q]));
+        const uint32_t at = begin + first + q * kRowLanes * 4;
+        if (MASTER) store4_once(e.master + at, p[q]);
+        store4_once((P*)e.p + at, narrow<P>(p[q]));
     }
     float minv, rinv;
     const float ms = block_scale(row_umax(__float_as_uint(mtop)), minv);
     const float rs = block_scale(row_umax(__float_as_uint(rtop)), rinv);
 #pragma unroll
     for (int q = 0; q < kRowQuads; ++q) {
-        const uint32_t at = first + q * kRowLanes * 4;
-        store_states<DRAWS>(a, f, e, begin + at, mp + at, vp + at, m[q], r[q], minv, rinv, 4);
+        const uint32_t at = begin + first + q * kRowLanes * 4;
+        store_states<DRAWS>(a, f, e, at, (uint8_t*)e.m + at, (uint8_t*)e.v + at, m[q], r[q], minv, rinv, 4);
     }
-    if (lane % kRowLanes == 0) {
-        (e.m_scale + block)[row] = ms;
-        (e.v_scale + block)[row] = rs;
+    if (lane_id() % kRowLanes == 0) {
+        (e.m_scale + begin / EA_STATE_BLOCK)[lane_id() / kRowLanes] = ms;
+        (e.v_scale + begin / EA_STATE_BLOCK)[lane_id() / kRowLanes] = rs;
     }
     return true;
+}
+
+// A wave's run of its part: whole groups of blocks, each fetched before the
+// last one is worked on, then what is left of the part.
+template <class P, class G, bool DRAWS, bool MASTER>
+__device__ __forceinline__ void adamw8_run(const AdamwArgs& a, const Factors& f, const TensorPart& e, uint32_t begin,
+                                           uint32_t end)
+{
+    Held<P, G, MASTER> h, next;
+    if (f.eps >= kLeastEps && end - begin >= kWaveElements) {
+        fetch<P, G, MASTER>(e, begin, h);
+        for (;;) {
+            const uint32_t then = begin + kWaveElements;
+            const bool more = end - then >= kWaveElements;
+            if (more) fetch<P, G, MASTER>(e, then, next);
+            if (!adamw8_whole<P, G, DRAWS, MASTER>(a, f, e, begin, h)) adamw8_any<P, G, DRAWS>(a, f, e, begin);
+            begin = then;
+            if (!more) break;
+            h = next;
+        }
+    }
+    for (; begin < end; begin += kWaveElements) adamw8_any<P, G, DRAWS>(a, f, e, begin);
 }
 
 template <class P, class G, bool DRAWS>
@@ -438,15 +485,15 @@ __global__ void __launch_bounds__(kAdamwBlock) adamw8_kernel(AdamwArgs a)
     if (!__builtin_isfinite(gs)) return;
     const int at = __builtin_amdgcn_readfirstlane(part_of<kListParts>(a.first, a.count, blockIdx.x));
     const TensorPart& e = a.part[at];
-    const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-    const uint32_t begin = ((blockIdx.x - a.first[at]) * kWavesPerBlock + wave) * kWaveElements;
+    const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), run = a.chunk / kWavesPerBlock;
+    const uint32_t begin = ((blockIdx.x - a.first[at]) * kWavesPerBlock + wave) * run;
     if (begin >= e.n) return;
+    const uint32_t end = e.n - begin < run ? e.n : begin + run;
     const Factors f = factors_of(a, e, gs);
-    bool done = false;
-    if (e.n - begin >= kWaveElements && f.eps >= kLeastEps)
-        done = sizeof(P) == 2 && e.master ? adamw8_four<P, G, DRAWS, true>(a, f, e, begin)
-                                          : adamw8_four<P, G, DRAWS, false>(a, f, e, begin);
-    if (!done) adamw8_any<P, G, DRAWS>(a, f, e, begin);
+    if (sizeof(P) == 2 && e.master)
+        adamw8_run<P, G, DRAWS, true>(a, f, e, begin, end);
+    else
+        adamw8_run<P, G, DRAWS, false>(a, f, e, begin, end);
 }
 
 template <class P, class G>
@@ -490,21 +537,63 @@ __device__ __forceinline__ double block_sum(double v)
     return r;
 }
 
+// Squares of n elements summed over the workgroup's threads, in 16-byte loads,
+// up to eight in flight a thread.
+template <class G, int THREADS>
+__device__ __forceinline__ double squares(const G* g, uint32_t n)
+{
+    constexpr int kEach = 16 / sizeof(G), kAhead = 8;
+    typedef G vec __attribute__((ext_vector_type(kEach)));
+    typedef vec unaligned __attribute__((aligned(sizeof(G))));
+    constexpr uint32_t kStride = THREADS * kEach;
+    double sum = 0.0;
+    const auto add = [&sum](float x) { sum = fma((double)x, (double)x, sum); };
+    uint32_t i = threadIdx.x * kEach;
+    for (; (uint64_t)i + (kAhead - 1) * kStride + kEach <= n; i += kAhead * kStride) {
+        vec x[kAhead];
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) x[u] = __builtin_nontemporal_load((const unaligned*)(g + i + u * kStride));
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u)
+#pragma unroll
+            for (int k = 0; k < kEach; ++k) add((float)x[u][k]);
+    }
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+        if (i < n && n - i >= kEach) {
+            const vec x = *(const unaligned*)(g + i);
+#pragma unroll
+            for (int k = 0; k < kEach; ++k) add((float)x[k]);
+            i += kStride;
+        }
+    }
+    if (i < n)
+        for (uint32_t k = 0; k < kEach && k < n - i; ++k) add((float)g[i + k]);
+    return sum;
+}
+
 template <class G>
 __global__ void __launch_bounds__(kNormBlock) norm_kernel(NormArgs a)
 {
     const int at = __builtin_amdgcn_readfirstlane(part_of<kNormParts>(a.first, a.count, blockIdx.x));
-    const int64_t begin = (int64_t)(blockIdx.x - a.first[at]) * a.chunk;
-    const int64_t n = a.part[at].n, end = begin + a.chunk < n ? begin + a.chunk : n;
-    const G* g = (const G*)a.part[at].g;
-    double sum = 0.0;
-    for (int64_t i = begin + threadIdx.x * 4; i < end; i += kNormBlock * 4) {
-        const v4f x = widen(end - i >= 4 ? load4_once(g + i) : load_some(g + i, (int)(end - i)));
-#pragma unroll
-        for (int k = 0; k < 4; ++k) sum = fma((double)x[k], (double)x[k], sum);
-    }
-    sum = block_sum<kNormBlock / kWave>(sum);
+    const int64_t begin = (int64_t)(blockIdx.x - a.first[at]) * a.chunk, left = a.part[at].n - begin;
+    const uint32_t n = (uint32_t)(left < a.chunk ? left : a.chunk);
+    const double sum =
+        block_sum<kNormBlock / kWave>(squares<G, kNormBlock>((const G*)a.part[at].g + begin, n));
     if (threadIdx.x == 0) a.sums[blockIdx.x] = sum;
+}
+
+// Norm and factor from the sum of squares.
+__device__ __forceinline__ void norm_out(double sum, float scale, float max_norm, float* norm, float* gscale)
+{
+    const float n = (float)((double)scale * sqrt(sum));
+    float f = scale;
+    if (!__builtin_isfinite(n))
+        f = __uint_as_float(0x7FC00000u);
+    else if (max_norm < n)
+        f = (float)((double)scale * ((double)max_norm / (double)n));
+    *norm = n;
+    if (gscale) *gscale = f;
 }
 
 constexpr int kFinishBlock = 1024;
@@ -513,25 +602,29 @@ __global__ void __launch_bounds__(kFinishBlock) norm_finish_kernel(const double*
                                                                    float max_norm, float* norm, float* gscale)
 {
     double sum = 0.0;
+#pragma unroll 4
     for (int64_t i = threadIdx.x; i < parts; i += kFinishBlock) sum = sum + part[i];
     sum = block_sum<kFinishBlock / kWave>(sum);
-    if (threadIdx.x == 0) {
-        const float n = (float)((double)scale * sqrt(sum));
-        float f = scale;
-        if (!__builtin_isfinite(n))
-            f = __uint_as_float(0x7FC00000u);
-        else if (max_norm < n)
-            f = (float)((double)scale * ((double)max_norm / (double)n));
-        *norm = n;
-        if (gscale) *gscale = f;
-    }
+    if (threadIdx.x == 0) norm_out(sum, scale, max_norm, norm, gscale);
+}
+
+// Few elements: one launch of one workgroup.
+template <class G>
+__global__ void __launch_bounds__(kFinishBlock) norm_small_kernel(NormArgs a, float scale, float max_norm, float* norm,
+                                                                  float* gscale)
+{
+    double sum = 0.0;
+    for (int k = 0; k < a.count; ++k) sum = sum + squares<G, kFinishBlock>((const G*)a.part[k].g, (uint32_t)a.part[k].n);
+    sum = block_sum<kFinishBlock / kWave>(sum);
+    if (threadIdx.x == 0) norm_out(sum, scale, max_norm, norm, gscale);
 }
 
 }  // namespace
 
-int64_t adamw_chunk(const ea_adamw_t& c)
+uint32_t adamw_chunk(const ea_adamw_t& c, int64_t total)
 {
-    return c.state_bits == 8 ? kWavesPerBlock * kWaveElements : kAdamwBlock * 4;
+    if (c.state_bits == 32) return kAdamwBlock * 4;
+    return kWavesPerBlock * kWaveElements * (total < kShortRuns ? 1 : 4);
 }
 
 hipError_t launch_adamw(const AdamwArgs& a, const ea_adamw_t& c, hipStream_t s)
@@ -549,7 +642,7 @@ hipError_t launch_adamw(const AdamwArgs& a, const ea_adamw_t& c, hipStream_t s)
 int64_t norm_chunk(int64_t total)
 {
     int64_t c = 4096;
-    while (total / c > 4096) c *= 2;
+    while (total / c > 8192) c *= 2;
     return c;
 }
 
@@ -563,6 +656,24 @@ hipError_t launch_norm(const NormArgs& a, int32_t grad_type, hipStream_t s)
         hipLaunchKernelGGL(norm_kernel<bf16>, grid, block, 0, s, a);
     else
         hipLaunchKernelGGL(norm_kernel<f16>, grid, block, 0, s, a);
+    return hipGetLastError();
+}
+
+bool norm_in_one(const NormArgs& a, int64_t total)
+{
+    return a.count <= kSmallParts && total <= kSmallTotal;
+}
+
+hipError_t launch_norm_small(const NormArgs& a, int32_t grad_type, float scale, float max_norm, float* norm,
+                             float* gscale, hipStream_t s)
+{
+    const dim3 grid(1), block(kFinishBlock);
+    if (grad_type == EA_F32)
+        hipLaunchKernelGGL(norm_small_kernel<float>, grid, block, 0, s, a, scale, max_norm, norm, gscale);
+    else if (grad_type == EA_BF16)
+        hipLaunchKernelGGL(norm_small_kernel<bf16>, grid, block, 0, s, a, scale, max_norm, norm, gscale);
+    else
+        hipLaunchKernelGGL(norm_small_kernel<f16>, grid, block, 0, s, a, scale, max_norm, norm, gscale);
     return hipGetLastError();
 }
 

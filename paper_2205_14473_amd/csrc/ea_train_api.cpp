@@ -115,7 +115,7 @@ int adamw_impl(const char* name, const ea_adamw_t* c, const ea_schedule_t* s, in
     a.t_dev = t_dev;
     if (!t_dev) a.root = ea::adamw_root(c->beta2, a.t);
     if (s) a.sched = *s;
-    const int64_t chunk = ea::adamw_chunk(*c);
+    a.chunk = ea::adamw_chunk(*c, total);
     const int64_t state = c->state_bits / 8;
     const int64_t gb = (int64_t)type_bytes(c->grad_type), pb = (int64_t)type_bytes(c->param_type);
     const hipStream_t st = (hipStream_t)stream;
@@ -123,7 +123,7 @@ int adamw_impl(const char* name, const ea_adamw_t* c, const ea_schedule_t* s, in
     for (int32_t i = 0; i < ntensors && e == hipSuccess; ++i)
         for (int64_t at = 0; at < tensors[i].n && e == hipSuccess; at += ea::kPartElements) {
             const int64_t left = tensors[i].n - at, n = left < ea::kPartElements ? left : ea::kPartElements;
-            const uint32_t groups = (uint32_t)((n + chunk - 1) / chunk);
+            const uint32_t groups = (uint32_t)((n + a.chunk - 1) / a.chunk);
             if (a.count == ea::kListParts || a.first[a.count] + groups > ea::kMostGroups) {
                 e = ea::launch_adamw(a, *c, st);
                 a.count = 0;
@@ -235,6 +235,7 @@ int ea_grad_norm(int32_t grad_type, int32_t ntensors, const ea_tensor_t* tensors
     if (pc.rc) return pc.rc;
     const hipStream_t st = (hipStream_t)stream;
     hipError_t e = hipSuccess;
+    bool flushed = false;
     a.sums = (double*)workspace;
     for (int32_t i = 0; i < ntensors && e == hipSuccess; ++i) {
         if (tensors[i].n == 0) continue;
@@ -242,6 +243,7 @@ int ea_grad_norm(int32_t grad_type, int32_t ntensors, const ea_tensor_t* tensors
             e = ea::launch_norm(a, grad_type, st);
             a.sums += a.first[a.count];
             a.count = 0;
+            flushed = true;
             if (e != hipSuccess) break;
         }
         a.part[a.count].g = tensors[i].g;
@@ -249,9 +251,13 @@ int ea_grad_norm(int32_t grad_type, int32_t ntensors, const ea_tensor_t* tensors
         a.first[a.count + 1] = a.first[a.count] + (uint32_t)((tensors[i].n + a.chunk - 1) / a.chunk);
         ++a.count;
     }
-    if (e == hipSuccess) e = ea::launch_norm(a, grad_type, st);
-    if (e == hipSuccess)
-        e = ea::launch_norm_finish((const double*)workspace, groups, scale, max_norm, norm, gscale, st);
+    if (e == hipSuccess && !flushed && ea::norm_in_one(a, total)) {
+        e = ea::launch_norm_small(a, grad_type, scale, max_norm, norm, gscale, st);
+    } else if (e == hipSuccess) {
+        e = ea::launch_norm(a, grad_type, st);
+        if (e == hipSuccess)
+            e = ea::launch_norm_finish((const double*)workspace, groups, scale, max_norm, norm, gscale, st);
+    }
     return hip_status(e, "ea_grad_norm");
 }
 
