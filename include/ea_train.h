@@ -94,8 +94,8 @@ typedef struct ea_adamw {
  *     applied to counter {lo(n>>2), hi(n>>2), t, i} with key {lo(seed),
  *     hi(seed)} (see ea.h): the high 16 bits for m, the low ones for r.
  *
- * tensors (host, ntensors) is read during the call.  ntensors >= 0; at most
- * 2^31 - 1 elements times 1024 in all.  gscale (device, one float, or NULL). */
+ * tensors (host, ntensors) is read during the call.  ntensors >= 0; fewer
+ * than 2^40 elements in all.  gscale (device, one float, or NULL). */
 int ea_adamw_step(const ea_adamw_t *c, int64_t t, int32_t ntensors, const ea_tensor_t *tensors, const float *gscale,
                   void *stream);
 
@@ -125,9 +125,9 @@ int ea_grad_norm(int32_t grad_type, int32_t ntensors, const ea_tensor_t *tensors
 /* ---- embedding ------------------------------------------------------------ */
 
 typedef struct ea_embed {
-    int64_t tokens;          /* ids, 0 <= tokens < 2^31 - 2^16                        */
+    int64_t tokens;          /* ids, 0 <= tokens < 2^30                               */
     int64_t vocab;           /* rows of the table, 1 <= vocab < 2^31 - 1              */
-    int64_t dim;             /* columns, 1 <= dim < 2^24                              */
+    int64_t dim;             /* columns, 1 <= dim <= 2^20                             */
     int64_t table_stride;    /* elements from one row of the table (gradient) to the
                                 next, >= dim, < 2^32                                  */
     int64_t x_stride;        /* the same for the tokens' rows                         */

@@ -35,35 +35,88 @@ __device__ __forceinline__ int64_t id_at(const void* ids, int bits, int64_t i)
 
 // ---- lookup -------------------------------------------------------------------
 
-template <class T, class X>
+// R consecutive tokens a group of lanes: their ids first, then a quad of each row.
+template <class T, class X, int R>
 __global__ void __launch_bounds__(kRowBlock) lookup_kernel(ea_embed_t c, const T* table, const void* ids, X* x, int gbits)
 {
-    const int64_t rows = (int64_t)gridDim.x << (8 - gbits);
+    const int64_t step = ((int64_t)gridDim.x << (8 - gbits)) * R;
     const int lane = threadIdx.x & ((1 << gbits) - 1);
-    for (int64_t i = ((int64_t)blockIdx.x << (8 - gbits)) + (threadIdx.x >> gbits); i < c.tokens; i += rows) {
-        const int64_t id = id_at(ids, c.index_bits, i);
-        const bool known = id >= 0 && id < c.vocab;
-        const T* from = table + (known ? id : 0) * c.table_stride;
-        X* to = x + i * c.x_stride;
+    for (int64_t i = (((int64_t)blockIdx.x << (8 - gbits)) + (threadIdx.x >> gbits)) * R; i < c.tokens; i += step) {
+        const T* from[R];
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const int64_t id = i + r < c.tokens ? id_at(ids, c.index_bits, i + r) : -1;
+            const bool known = id >= 0 && id < c.vocab;
+            from[r] = known ? table + id * c.table_stride : nullptr;
+        }
         for (int64_t k = lane * 4; k < c.dim; k += (int64_t)4 << gbits) {
             const int n = c.dim - k < 4 ? (int)(c.dim - k) : 4;
-            v4f v = {0.0f, 0.0f, 0.0f, 0.0f};
-            if (known) v = widen(n == 4 ? load4(from + k) : load_some(from + k, n)) * c.scale;
-            if (n == 4)
-                store4(to + k, narrow<X>(v));
-            else
-                store_some(to + k, narrow<X>(v), n);
+            v4f v[R];
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                v[r] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+                if (from[r]) v[r] = widen(n == 4 ? load4(from[r] + k) : load_some(from[r] + k, n)) * c.scale;
+            }
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                X* to = x + (i + r) * c.x_stride + k;
+                if (i + r < c.tokens) {
+                    if (n == 4)
+                        store4(to, narrow<X>(v[r]));
+                    else
+                        store_some(to, narrow<X>(v[r]), n);
+                }
+            }
         }
     }
 }
 
+// ---- zeros ----------------------------------------------------------------------
+
+// The table's rows as lines of bytes (one line where no elements lie between
+// rows), zeroed in units of 16 by workgroups that ride along with the sort's:
+// the sort is latency, and the zeros are bandwidth.
+struct Fill {
+    char* base;
+    int64_t line, pitch;                 // bytes of a line, and to the next
+    int64_t units;                       // 16-byte units of one line
+    int64_t begin, end;                  // units of this launch, over all lines
+};
+
+template <int THREADS>
+__device__ __forceinline__ void fill_zeros(const Fill& f, uint32_t group, uint32_t groups)
+{
+    typedef uint32_t vec __attribute__((ext_vector_type(4)));
+    typedef vec unaligned __attribute__((aligned(2)));
+    for (int64_t u = f.begin + (int64_t)group * THREADS + threadIdx.x; u < f.end; u += (int64_t)groups * THREADS) {
+        const int64_t line = u < f.units ? 0 : u / f.units, off = (u - line * f.units) * 16;
+        char* to = f.base + line * f.pitch + off;
+        const int64_t left = f.line - off;
+        if (left >= 16)
+            *(unaligned*)to = vec{0, 0, 0, 0};
+        else
+            for (int k = 0; k < (int)left; k += 2) *(uint16_t*)(to + k) = 0;
+    }
+}
+
+constexpr unsigned kFillGroups = 512;    // two workgroups of 1024 for each CU
+
+__global__ void __launch_bounds__(1024) fill_kernel16(Fill f)
+{
+    fill_zeros<1024>(f, blockIdx.x, gridDim.x);
+}
+
 // ---- sort -----------------------------------------------------------------------
 
-constexpr int kSortBlock = 512;
+constexpr int kSortBlock = 1024;
 constexpr int kSortWaves = kSortBlock / kWave;
-constexpr int kMostBits = 9;             // of one pass's digit: a thread for each value
+constexpr int kMostBits = 9;             // of one pass's digit
+constexpr int kMostValues = 1 << kMostBits;
 constexpr int64_t kLeastTile = 2048;     // items of one workgroup
 constexpr int64_t kMostTiles = 128;
+constexpr int kBatch = 4;                // items a lane loads ahead
+constexpr int kOneRounds = 4;            // items a lane holds where one workgroup sorts all
+constexpr int64_t kOneTile = kSortBlock * kOneRounds;
 
 struct SortPlan {
     int64_t n, tile, tiles;
@@ -101,19 +154,6 @@ __device__ __forceinline__ uint32_t key_of(const Items& t, int64_t i)
     return id >= 0 && id < t.vocab && id != t.padding ? (uint32_t)id : (uint32_t)t.vocab;
 }
 
-__global__ void __launch_bounds__(kSortBlock) digits_kernel(Items t, SortPlan p, int shift, uint32_t* counts)
-{
-    __shared__ uint32_t count[1 << kMostBits];
-    const int values = 1 << p.bits;
-    if ((int)threadIdx.x < values) count[threadIdx.x] = 0;
-    __syncthreads();
-    const int64_t begin = blockIdx.x * p.tile, end = begin + p.tile < p.n ? begin + p.tile : p.n;
-    for (int64_t i = begin + threadIdx.x; i < end; i += kSortBlock)
-        atomicAdd(&count[(key_of(t, i) >> shift) & (values - 1)], 1u);
-    __syncthreads();
-    if ((int)threadIdx.x < values) counts[(int64_t)blockIdx.x * values + threadIdx.x] = count[threadIdx.x];
-}
-
 __device__ __forceinline__ void wave_sync()
 {
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
@@ -121,40 +161,172 @@ __device__ __forceinline__ void wave_sync()
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
 
-// Each wave owns a run of its tile's items.  Their digits are counted once to
-// place the waves, then walked in order, 64 at a time: a lane's place is its
-// digit's running count plus the equal digits in lower lanes.
-__global__ void __launch_bounds__(kSortBlock) scatter_kernel(Items t, SortPlan p, int shift, const uint32_t* counts,
-                                                             uint32_t* keys, uint32_t* at)
+// A lane's place among its wave's items of one digit: `count` holds the digits'
+// running counts, which move on by the 64 lanes' items.
+__device__ __forceinline__ uint32_t take_place(uint32_t* count, uint32_t digit, int bits, bool here)
 {
-    __shared__ uint32_t place[kSortWaves][1 << kMostBits];
-    __shared__ uint32_t sums[kSortWaves];
-    const int values = 1 << p.bits, wave = threadIdx.x / kWave, lane = lane_id();
-    for (int k = threadIdx.x; k < kSortWaves * values; k += kSortBlock) place[k / values][k % values] = 0;
-    __syncthreads();
-    const int64_t run = p.tile / kSortWaves, begin = blockIdx.x * p.tile + wave * run;
-    for (int64_t k = lane; k < run; k += kWave)
-        if (begin + k < p.n) atomicAdd(&place[wave][(key_of(t, begin + k) >> shift) & (values - 1)], 1u);
-    __syncthreads();
+    uint64_t same = __ballot(here);
+    for (int b = 0; b < bits; ++b) {
+        const uint64_t ones = __ballot((digit >> b) & 1);
+        same &= (digit >> b) & 1 ? ones : ~ones;
+    }
+    const uint64_t lower = same & ((1ull << lane_id()) - 1);
+    const uint32_t first = here ? count[digit] : 0;
+    wave_sync();
+    if (here && !lower) count[digit] = first + (uint32_t)__popcll(same);
+    wave_sync();
+    return first + (uint32_t)__popcll(lower);
+}
 
-    // thread v: items with digit v in all tiles, and in the tiles before this one
-    uint32_t all = 0, before = 0;
-    if ((int)threadIdx.x < values)
-        for (int64_t b = 0; b < p.tiles; ++b) {
-            const uint32_t k = counts[b * values + threadIdx.x];
-            all += k;
-            before += b < (int64_t)blockIdx.x ? k : 0;
-        }
-    // exclusive sum of `all` over the digits
-    uint32_t upto = all;
+// Exclusive sum over the workgroup's threads.
+__device__ __forceinline__ uint32_t sum_before(uint32_t x, uint32_t* sums)
+{
+    const int lane = lane_id(), wave = threadIdx.x / kWave;
+    uint32_t upto = x;
     for (int d = 1; d < kWave; d *= 2) {
         const uint32_t k = __shfl_up(upto, d);
         upto += lane >= d ? k : 0;
     }
     if (lane == kWave - 1) sums[wave] = upto;
     __syncthreads();
-    uint32_t base = upto - all + before;
+    uint32_t base = upto - x;
     for (int w = 0; w < wave; ++w) base += sums[w];
+    return base;
+}
+
+// Tokens that one workgroup sorts in its registers and LDS, every pass in one
+// launch; the other workgroups zero the table.
+__global__ void __launch_bounds__(kSortBlock) sort_one_kernel(Items t, SortPlan p, uint32_t* keys, uint32_t* at, Fill f)
+{
+    __shared__ uint32_t place[kSortWaves][kMostValues];
+    __shared__ uint32_t skey[kOneTile];
+    __shared__ uint16_t sat[kOneTile];
+    __shared__ uint32_t sums[kSortWaves];
+    if (blockIdx.x > 0) {
+        fill_zeros<kSortBlock>(f, blockIdx.x - 1, gridDim.x - 1);
+        return;
+    }
+    const int values = 1 << p.bits, wave = threadIdx.x / kWave, lane = lane_id(), n = (int)p.n;
+    const int rounds = (n + kSortBlock - 1) / kSortBlock, begin = wave * rounds * kWave + lane;
+    uint32_t key[kOneRounds], from[kOneRounds], rank[kOneRounds];
+#pragma unroll
+    for (int r = 0; r < kOneRounds; ++r) {
+        const int i = begin + r * kWave;
+        from[r] = (uint32_t)i;
+        key[r] = r < rounds && i < n ? key_of(t, i) : 0;
+    }
+    for (int pass = 0; pass < p.passes; ++pass) {
+        const int shift = pass * p.bits;
+        for (int k = threadIdx.x; k < kSortWaves * values; k += kSortBlock) place[k / values][k % values] = 0;
+        __syncthreads();
+#pragma unroll
+        for (int r = 0; r < kOneRounds; ++r)
+            if (r < rounds)
+                rank[r] = take_place(place[wave], (key[r] >> shift) & (values - 1), p.bits, begin + r * kWave < n);
+        __syncthreads();
+        uint32_t all = 0;
+        if ((int)threadIdx.x < values)
+            for (int w = 0; w < kSortWaves; ++w) all += place[w][threadIdx.x];
+        uint32_t base = sum_before(all, sums);
+        if ((int)threadIdx.x < values)
+            for (int w = 0; w < kSortWaves; ++w) {
+                const uint32_t k = place[w][threadIdx.x];
+                place[w][threadIdx.x] = base;
+                base += k;
+            }
+        __syncthreads();
+#pragma unroll
+        for (int r = 0; r < kOneRounds; ++r)
+            if (r < rounds && begin + r * kWave < n) {
+                const uint32_t to = place[wave][(key[r] >> shift) & (values - 1)] + rank[r];
+                skey[to] = key[r];
+                sat[to] = (uint16_t)from[r];
+            }
+        __syncthreads();
+#pragma unroll
+        for (int r = 0; r < kOneRounds; ++r) {
+            const int i = begin + r * kWave;
+            if (r < rounds && i < n) {
+                key[r] = skey[i];
+                from[r] = sat[i];
+            }
+        }
+    }
+#pragma unroll
+    for (int r = 0; r < kOneRounds; ++r) {
+        const int i = begin + r * kWave;
+        if (r < rounds && i < n) {
+            keys[i] = key[r];
+            at[i] = from[r];
+        }
+    }
+}
+
+__global__ void __launch_bounds__(kSortBlock) digits_kernel(Items t, SortPlan p, int shift, uint32_t* counts, Fill f)
+{
+    __shared__ uint32_t count[kMostValues];
+    if (blockIdx.x >= p.tiles) {
+        fill_zeros<kSortBlock>(f, blockIdx.x - (uint32_t)p.tiles, gridDim.x - (uint32_t)p.tiles);
+        return;
+    }
+    const int values = 1 << p.bits;
+    if ((int)threadIdx.x < values) count[threadIdx.x] = 0;
+    __syncthreads();
+    const int64_t begin = blockIdx.x * p.tile, end = begin + p.tile < p.n ? begin + p.tile : p.n;
+#pragma unroll 2
+    for (int64_t i = begin + threadIdx.x; i < end; i += kSortBlock)
+        atomicAdd(&count[(key_of(t, i) >> shift) & (values - 1)], 1u);
+    __syncthreads();
+    if ((int)threadIdx.x < values) counts[(int64_t)blockIdx.x * values + threadIdx.x] = count[threadIdx.x];
+}
+
+// Each wave owns a run of its tile's items.  Their digits are counted once to
+// place the waves, then walked in order, 64 at a time.
+__global__ void __launch_bounds__(kSortBlock) scatter_kernel(Items t, SortPlan p, int shift, const uint32_t* counts,
+                                                             uint32_t* keys, uint32_t* at, Fill f)
+{
+    __shared__ uint32_t place[kSortWaves][kMostValues];
+    __shared__ uint32_t sums[kSortWaves];
+    if (blockIdx.x >= p.tiles) {
+        fill_zeros<kSortBlock>(f, blockIdx.x - (uint32_t)p.tiles, gridDim.x - (uint32_t)p.tiles);
+        return;
+    }
+    const int values = 1 << p.bits, wave = threadIdx.x / kWave, lane = lane_id();
+    for (int k = threadIdx.x; k < kSortWaves * values; k += kSortBlock) place[k / values][k % values] = 0;
+    __syncthreads();
+    const int64_t run = p.tile / kSortWaves, begin = blockIdx.x * p.tile + wave * run;
+    const int64_t end = begin + run < p.n ? begin + run : p.n;
+    for (int64_t k = begin + lane; k < end; k += kBatch * kWave) {
+        uint32_t key[kBatch];
+#pragma unroll
+        for (int r = 0; r < kBatch; ++r) key[r] = k + r * kWave < end ? key_of(t, k + r * kWave) : 0;
+#pragma unroll
+        for (int r = 0; r < kBatch; ++r)
+            if (k + r * kWave < end) atomicAdd(&place[wave][(key[r] >> shift) & (values - 1)], 1u);
+    }
+
+    // thread v: items with digit v in all tiles, and in the tiles before this one
+    uint32_t all = 0, before = 0;
+    if ((int)threadIdx.x < values) {
+        const uint32_t* c = counts + threadIdx.x;
+        int64_t b = 0;
+        for (; b + 8 <= p.tiles; b += 8) {
+            uint32_t k[8];
+#pragma unroll
+            for (int r = 0; r < 8; ++r) k[r] = c[(b + r) * values];
+#pragma unroll
+            for (int r = 0; r < 8; ++r) {
+                all += k[r];
+                before += b + r < (int64_t)blockIdx.x ? k[r] : 0;
+            }
+        }
+        for (; b < p.tiles; ++b) {
+            const uint32_t k = c[b * values];
+            all += k;
+            before += b < (int64_t)blockIdx.x ? k : 0;
+        }
+    }
+    uint32_t base = sum_before(all, sums) + before;
     if ((int)threadIdx.x < values)
         for (int w = 0; w < kSortWaves; ++w) {
             const uint32_t k = place[w][threadIdx.x];
@@ -163,25 +335,24 @@ __global__ void __launch_bounds__(kSortBlock) scatter_kernel(Items t, SortPlan p
         }
     __syncthreads();
 
-    for (int64_t k = 0; k < run && begin + k < p.n; k += kWave) {
-        const int64_t i = begin + k + lane;
-        const bool here = i < p.n;
-        const uint32_t key = here ? key_of(t, i) : 0, digit = (key >> shift) & (values - 1);
-        uint64_t same = __ballot(here);
-        for (int b = 0; b < p.bits; ++b) {
-            const uint64_t ones = __ballot((digit >> b) & 1);
-            same &= (digit >> b) & 1 ? ones : ~ones;
+    for (int64_t k = begin; k < end; k += kBatch * kWave) {
+        uint32_t key[kBatch], from[kBatch];
+#pragma unroll
+        for (int r = 0; r < kBatch; ++r) {
+            const int64_t i = k + r * kWave + lane;
+            key[r] = i < end ? key_of(t, i) : 0;
+            from[r] = t.ids || i >= end ? (uint32_t)i : t.at[i];
         }
-        const uint64_t lower = same & ((1ull << lane) - 1);
-        const uint32_t first = here ? place[wave][digit] : 0;
-        wave_sync();
-        if (here) {
-            const uint32_t to = first + (uint32_t)__popcll(lower);
-            keys[to] = key;
-            at[to] = t.ids ? (uint32_t)i : t.at[i];
-            if (!lower) place[wave][digit] = first + (uint32_t)__popcll(same);
+#pragma unroll
+        for (int r = 0; r < kBatch; ++r) {
+            if (k + r * kWave >= end) break;
+            const bool here = k + r * kWave + lane < end;
+            const uint32_t to = take_place(place[wave], (key[r] >> shift) & (values - 1), p.bits, here);
+            if (here) {
+                keys[to] = key[r];
+                at[to] = from[r];
+            }
         }
-        wave_sync();
     }
 }
 
@@ -196,6 +367,9 @@ struct SumArgs {
     float scale;
     int gbits, accumulate;
 };
+
+constexpr int kMostChunk = kWave;        // a lane for each position of a chunk
+constexpr int kAhead = 8;                // rows a lane loads ahead
 
 template <class T>
 __device__ __forceinline__ void finish_row(const SumArgs& a, T* table, uint32_t key, int64_t col, int n, v4f sum)
@@ -212,33 +386,106 @@ __device__ __forceinline__ void finish_row(const SumArgs& a, T* table, uint32_t 
 // A group of lanes sums one chunk of the sorted order over its slice of the
 // columns.  A row is finished here where its run lies within the chunk; a run
 // that came from the chunk before goes to partial row 0, one that goes on in
-// the chunk after to partial row 1.
+// the chunk after to partial row 1.  Groups are whole waves here: a lane holds
+// one position's key and row, from which the wave takes the next rows' addresses
+// and the ends of the runs without a branch of its own.
 template <class T, class X>
 __global__ void __launch_bounds__(kRowBlock) sum_kernel(SumArgs a, const X* dx, T* table)
 {
-    const int64_t c = ((int64_t)blockIdx.x << (8 - a.gbits)) + (threadIdx.x >> a.gbits);
+    const int lane = lane_id();
+    const int64_t c = ((int64_t)blockIdx.x << (8 - a.gbits)) +
+                      __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> a.gbits));
     const int64_t col = (((int64_t)blockIdx.y << a.gbits) + (threadIdx.x & ((1 << a.gbits) - 1))) * 4;
+    if (c >= a.chunks) return;
+    const int64_t begin = c * a.chunk;
+    const int count = (int)(a.n - begin < a.chunk ? a.n - begin : a.chunk);
+    // lane l: position l; lane `count`'s key ends the last run
+    const uint32_t none = 0xFFFFFFFFu;
+    const int64_t mine = begin + (lane < count ? lane : count - 1);
+    const uint32_t key = a.keys[mine], at = a.at[mine];
+    const uint32_t last_key = begin > 0 ? a.keys[begin - 1] : none;
+    const uint32_t next_key = begin + count < a.n ? a.keys[begin + count] : none;
+    uint32_t left = __shfl_up(key, 1);
+    if (lane == 0) left = last_key;
+    const uint64_t starts = __ballot(lane < count && key != left);
+    const int used = __popcll(__ballot(lane < count && key < a.vocab));   // the others sort last
+    if (used == 0) return;
+    const int n = a.dim - col >= 4 ? 4 : a.dim > col ? (int)(a.dim - col) : 0;
+    float* part = a.part + c * 2 * a.part_row + col;
+    bool open = !(starts & 1);                             // the first run began before this chunk
+    v4f sum = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int k = 0; k < used; k += kAhead) {
+        typename Quad<X>::vec x[kAhead];
+#pragma unroll
+        for (int r = 0; r < kAhead; ++r) {
+            const int i = k + r < used ? k + r : used - 1;
+            const X* from = dx + (int64_t)(uint32_t)__builtin_amdgcn_readlane((int)at, i) * a.x_stride + col;
+            x[r] = n == 4 ? load4_once(from) : load_some(from, n);
+        }
+#pragma unroll
+        for (int r = 0; r < kAhead; ++r) {
+            if (k + r >= used) break;
+            if (k + r > 0 && ((starts >> (k + r)) & 1)) {
+                if (n > 0) {
+                    if (open)
+                        store4(part, sum);
+                    else
+                        finish_row(a, table, (uint32_t)__builtin_amdgcn_readlane((int)key, k + r - 1), col, n, sum);
+                }
+                open = false;
+                sum = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+            }
+            sum = sum + widen(x[r]);
+        }
+    }
+    const uint32_t end_key = (uint32_t)__builtin_amdgcn_readlane((int)key, used - 1);
+    if (n == 0) return;
+    if (open)
+        store4(part, sum);
+    else if (used == count && next_key == end_key)
+        store4(part + a.part_row, sum);
+    else
+        finish_row(a, table, end_key, col, n, sum);
+}
+
+// The same for narrow rows, several groups a wave, each lane for itself.
+template <class T, class X>
+__global__ void __launch_bounds__(kRowBlock) sum_narrow_kernel(SumArgs a, const X* dx, T* table)
+{
+    const int64_t c = ((int64_t)blockIdx.x << (8 - a.gbits)) + (threadIdx.x >> a.gbits);
+    const int64_t col = (threadIdx.x & ((1 << a.gbits) - 1)) * 4;
     if (c >= a.chunks || col >= a.dim) return;
     const int n = a.dim - col < 4 ? (int)(a.dim - col) : 4;
     const int64_t begin = c * a.chunk, end = begin + a.chunk < a.n ? begin + a.chunk : a.n;
     float* part = a.part + c * 2 * a.part_row + col;
     uint32_t key = a.keys[begin];
-    bool open = begin > 0 && a.keys[begin - 1] == key;     // the first run began before this chunk
+    bool open = begin > 0 && a.keys[begin - 1] == key;
     v4f sum = {0.0f, 0.0f, 0.0f, 0.0f};
-    for (int64_t i = begin; i < end; ++i) {
-        const uint32_t k = a.keys[i];
-        if (k != key) {
-            if (open)
-                store4(part, sum);
-            else
-                finish_row(a, table, key, col, n, sum);
-            open = false;
-            key = k;
-            sum = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+    for (int64_t k = begin; k < end; k += kAhead) {
+        uint32_t keys[kAhead];
+        typename Quad<X>::vec x[kAhead];
+#pragma unroll
+        for (int r = 0; r < kAhead; ++r) {
+            const int64_t i = k + r < end ? k + r : end - 1;
+            keys[r] = a.keys[i];
+            const X* from = dx + (int64_t)a.at[i] * a.x_stride + col;
+            if (keys[r] < a.vocab) x[r] = n == 4 ? load4(from) : load_some(from, n);
         }
-        if (k >= a.vocab) return;                           // sorted last: no row of the table
-        const X* from = dx + (int64_t)a.at[i] * a.x_stride + col;
-        sum = sum + widen(n == 4 ? load4(from) : load_some(from, n));
+#pragma unroll
+        for (int r = 0; r < kAhead; ++r) {
+            if (k + r >= end) break;
+            if (keys[r] != key) {
+                if (open)
+                    store4(part, sum);
+                else
+                    finish_row(a, table, key, col, n, sum);
+                open = false;
+                key = keys[r];
+                sum = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+            }
+            if (key >= a.vocab) return;
+            sum = sum + widen(x[r]);
+        }
     }
     if (open)
         store4(part, sum);
@@ -248,44 +495,56 @@ __global__ void __launch_bounds__(kRowBlock) sum_kernel(SumArgs a, const X* dx, 
         finish_row(a, table, key, col, n, sum);
 }
 
-// The runs that cross chunks: the group of the chunk in which one begins adds
-// up its partial rows in order.
+constexpr int kJoinWaves = kRowBlock / kWave;
+constexpr int kJoinCols = kWave * 4;
+
+// The runs that cross chunks: the workgroup of the chunk in which one begins
+// adds up its partial rows, a quarter of them to each wave, in an order that
+// their number fixes.
 template <class T>
 __global__ void __launch_bounds__(kRowBlock) join_kernel(SumArgs a, T* table)
 {
-    const int64_t c = ((int64_t)blockIdx.x << (8 - a.gbits)) + (threadIdx.x >> a.gbits);
-    const int64_t col = (((int64_t)blockIdx.y << a.gbits) + (threadIdx.x & ((1 << a.gbits) - 1))) * 4;
-    if (c >= a.chunks || col >= a.dim) return;
-    const int n = a.dim - col < 4 ? (int)(a.dim - col) : 4;
-    const int64_t begin = c * a.chunk;
-    int64_t end = begin + a.chunk;
+    __shared__ v4f sums[kJoinWaves][kWave];
+    const int lane = lane_id(), wave = threadIdx.x / kWave;
+    const int64_t c = blockIdx.x, begin = c * a.chunk, end = begin + a.chunk;
     if (end >= a.n) return;
     const uint32_t key = a.keys[end - 1];
     if (key >= a.vocab || a.keys[end] != key) return;                              // ends here
-    if (a.keys[begin] == key && begin > 0 && a.keys[begin - 1] == key) return;    // began before
-    const float* part = a.part + c * 2 * a.part_row + col;
-    v4f sum = load4(part + a.part_row);
-    do {
-        part += 2 * a.part_row;
-        sum = sum + load4(part);
-        end += a.chunk;
-    } while (end < a.n && a.keys[end] == key);
-    finish_row(a, table, key, col, n, sum);
-}
-
-template <class T>
-__global__ void __launch_bounds__(kRowBlock) zero_rows_kernel(T* table, int64_t vocab, int64_t dim, int64_t stride, int gbits)
-{
-    const int64_t rows = (int64_t)gridDim.x << (8 - gbits);
-    const int lane = threadIdx.x & ((1 << gbits) - 1);
-    const typename Quad<T>::vec zero = narrow<T>(v4f{0.0f, 0.0f, 0.0f, 0.0f});
-    for (int64_t i = ((int64_t)blockIdx.x << (8 - gbits)) + (threadIdx.x >> gbits); i < vocab; i += rows)
-        for (int64_t k = lane * 4; k < dim; k += (int64_t)4 << gbits) {
-            if (dim - k >= 4)
-                store4(table + i * stride + k, zero);
-            else
-                store_some(table + i * stride + k, zero, (int)(dim - k));
+    if (begin > 0 && a.keys[begin] == key && a.keys[begin - 1] == key) return;    // began before
+    // the chunks after this one whose first key is still `key`: a 64-way search
+    int64_t rows = 0, range = a.chunks - 1 - c;
+    while (range > 0) {
+        const int64_t step = (range + kWave - 1) / kWave, probe = lane * step;
+        const bool still = probe < range && a.keys[end + (rows + probe) * a.chunk] == key;
+        const int hits = __popcll(__ballot(still));
+        if (hits == 0) break;
+        const int64_t known = (hits - 1) * step + 1;
+        range = range - known < step - 1 ? range - known : step - 1;
+        rows += known;
+    }
+    const int64_t col = (int64_t)blockIdx.y * kJoinCols + lane * 4;
+    const int64_t each = (rows + kJoinWaves - 1) / kJoinWaves;
+    const int64_t from = wave * each, upto = from + each < rows ? from + each : rows;
+    const float* part = a.part + (c + 1) * 2 * a.part_row + col;
+    v4f sum = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (col < a.dim) {
+        int64_t k = from;
+        for (; k + 2 * kAhead <= upto; k += 2 * kAhead) {
+            v4f x[2 * kAhead];
+#pragma unroll
+            for (int r = 0; r < 2 * kAhead; ++r) x[r] = load4(part + (k + r) * 2 * a.part_row);
+#pragma unroll
+            for (int r = 0; r < 2 * kAhead; ++r) sum = sum + x[r];
         }
+        for (; k < upto; ++k) sum = sum + load4(part + k * 2 * a.part_row);
+    }
+    sums[wave][lane] = sum;
+    __syncthreads();
+    if (wave == 0 && col < a.dim) {
+        sum = load4(part - a.part_row);                                            // this chunk's
+        for (int w = 0; w < kJoinWaves; ++w) sum = sum + sums[w][lane];
+        finish_row(a, table, key, col, a.dim - col < 4 ? (int)(a.dim - col) : 4, sum);
+    }
 }
 
 struct GradPlan {
@@ -299,15 +558,22 @@ int64_t align16(int64_t x)
     return (x + 15) / 16 * 16;
 }
 
+constexpr int64_t kEnoughWaves = 8192;   // 32 for each CU
+constexpr int64_t kLeastChunk = 8;
+
 GradPlan grad_plan(const ea_embed_t& c)
 {
     GradPlan p{};
     if (c.tokens == 0) return p;
     p.sort = sort_plan(c);
-    p.chunk = 32;
-    while (c.tokens / p.chunk >= 65536) p.chunk *= 2;
+    const int gbits = group_bits(c.dim);
+    const int64_t quads = (c.dim + 3) / 4;
+    p.chunk = kMostChunk;
+    while (p.chunk > kLeastChunk &&
+           (c.tokens / p.chunk) * (gbits < 6 ? 1 : (quads + kWave - 1) / kWave) < kEnoughWaves)
+        p.chunk /= 2;
     p.chunks = (c.tokens + p.chunk - 1) / p.chunk;
-    p.part_row = (c.dim + 3) / 4 * 4;
+    p.part_row = quads * 4;
     int64_t off = 0;
     for (int k = 0; k < 2; ++k) {
         p.off_keys[k] = off;
@@ -330,27 +596,57 @@ unsigned row_groups(int64_t rows, int gbits)
     return (unsigned)(blocks < (1 << 22) ? blocks : (1 << 22));
 }
 
+// The part of the zeros that goes with launch k of `of`.
+Fill fill_part(Fill f, int64_t units, int k, int of)
+{
+    f.begin = units / of * k;
+    f.end = k == of - 1 ? units : units / of * (k + 1);
+    return f;
+}
+
 template <class T, class X>
 hipError_t start_grad(const ea_embed_t& c, const GradPlan& p, const void* ids, const X* dx, T* table, bool accumulate,
                       char* ws, hipStream_t s)
 {
-    const int gbits = group_bits(c.dim);
-    if (!accumulate)
-        hipLaunchKernelGGL(zero_rows_kernel<T>, dim3(row_groups(c.vocab, gbits)), dim3(kRowBlock), 0, s, table, c.vocab,
-                           c.dim, c.table_stride, gbits);
-    if (c.tokens == 0) return hipGetLastError();
+    Fill f{};
+    f.base = (char*)table;
+    f.line = c.dim * (int64_t)sizeof(T);
+    f.pitch = c.table_stride * (int64_t)sizeof(T);
+    int64_t lines = accumulate ? 0 : c.vocab;
+    if (f.line == f.pitch || lines == 1) {
+        f.line = lines * f.line;
+        lines = lines > 0 ? 1 : 0;
+    }
+    f.units = (f.line + 15) / 16;
+    const int64_t units = f.units * lines;
+    const unsigned groups = units == 0 ? 0 : (unsigned)(units / kSortBlock < kFillGroups ? units / kSortBlock + 1 : kFillGroups);
+    if (c.tokens == 0) {
+        if (groups)
+            hipLaunchKernelGGL(fill_kernel16, dim3(groups), dim3(kSortBlock), 0, s, fill_part(f, units, 0, 1));
+        return hipGetLastError();
+    }
     Items t{ids, nullptr, nullptr, c.index_bits, c.vocab, c.padding};
     uint32_t* counts = (uint32_t*)(ws + p.off_counts);
-    for (int k = 0; k < p.sort.passes; ++k) {
-        uint32_t* keys = (uint32_t*)(ws + p.off_keys[k & 1]);
-        uint32_t* at = (uint32_t*)(ws + p.off_at[k & 1]);
-        const int shift = k * p.sort.bits;
-        hipLaunchKernelGGL(digits_kernel, dim3((unsigned)p.sort.tiles), dim3(kSortBlock), 0, s, t, p.sort, shift, counts);
-        hipLaunchKernelGGL(scatter_kernel, dim3((unsigned)p.sort.tiles), dim3(kSortBlock), 0, s, t, p.sort, shift, counts,
-                           keys, at);
-        t.ids = nullptr;
-        t.keys = keys;
-        t.at = at;
+    const auto keys = [&](int k) { return (uint32_t*)(ws + p.off_keys[k & 1]); };
+    const auto at = [&](int k) { return (uint32_t*)(ws + p.off_at[k & 1]); };
+    if (c.tokens <= kOneTile) {
+        hipLaunchKernelGGL(sort_one_kernel, dim3(1 + groups), dim3(kSortBlock), 0, s, t, p.sort, keys(0), at(0),
+                           fill_part(f, units, 0, 1));
+        t.keys = keys(0);
+        t.at = at(0);
+    } else {
+        const unsigned tiles = (unsigned)p.sort.tiles;
+        const int of = 2 * p.sort.passes;
+        for (int k = 0; k < p.sort.passes; ++k) {
+            const int shift = k * p.sort.bits;
+            hipLaunchKernelGGL(digits_kernel, dim3(tiles + groups), dim3(kSortBlock), 0, s, t, p.sort, shift, counts,
+                               fill_part(f, units, 2 * k, of));
+            hipLaunchKernelGGL(scatter_kernel, dim3(tiles + groups), dim3(kSortBlock), 0, s, t, p.sort, shift, counts,
+                               keys(k), at(k), fill_part(f, units, 2 * k + 1, of));
+            t.ids = nullptr;
+            t.keys = keys(k);
+            t.at = at(k);
+        }
     }
     SumArgs a{};
     a.n = c.tokens;
@@ -365,13 +661,22 @@ hipError_t start_grad(const ea_embed_t& c, const GradPlan& p, const void* ids, c
     a.part = (float*)(ws + p.off_part);
     a.part_row = p.part_row;
     a.scale = c.scale;
-    a.gbits = gbits;
+    a.gbits = group_bits(c.dim);
     a.accumulate = accumulate ? 1 : 0;
-    const dim3 grid(row_groups(p.chunks, gbits), (unsigned)((c.dim + ((int64_t)4 << gbits) - 1) >> (2 + gbits)));
-    hipLaunchKernelGGL((sum_kernel<T, X>), grid, dim3(kRowBlock), 0, s, a, dx, table);
-    if (p.chunks > 1) hipLaunchKernelGGL(join_kernel<T>, grid, dim3(kRowBlock), 0, s, a, table);
+    const int64_t per = (int64_t)1 << (8 - a.gbits);
+    const dim3 grid((unsigned)((p.chunks + per - 1) / per),
+                    (unsigned)((c.dim + ((int64_t)4 << a.gbits) - 1) >> (2 + a.gbits)));
+    if (a.gbits < 6)
+        hipLaunchKernelGGL((sum_narrow_kernel<T, X>), grid, dim3(kRowBlock), 0, s, a, dx, table);
+    else
+        hipLaunchKernelGGL((sum_kernel<T, X>), grid, dim3(kRowBlock), 0, s, a, dx, table);
+    if (p.chunks > 1)
+        hipLaunchKernelGGL(join_kernel<T>, dim3((unsigned)(p.chunks - 1), (unsigned)((c.dim + kJoinCols - 1) / kJoinCols)),
+                           dim3(kRowBlock), 0, s, a, table);
     return hipGetLastError();
 }
+
+constexpr int64_t kFewTokens = 8192;
 
 // f(table element, row element) with the types that c names.
 template <class F, class T>
@@ -399,8 +704,12 @@ hipError_t launch_embed_lookup(const ea_embed_t& c, const void* table, const voi
     return with_types(c, [&](auto t, auto e) {
         using T = decltype(t);
         using X = decltype(e);
-        hipLaunchKernelGGL((lookup_kernel<T, X>), dim3(row_groups(c.tokens, gbits)), dim3(kRowBlock), 0, s, c,
-                           (const T*)table, ids, (X*)x, gbits);
+        if (c.tokens < kFewTokens)
+            hipLaunchKernelGGL((lookup_kernel<T, X, 1>), dim3(row_groups(c.tokens, gbits)), dim3(kRowBlock), 0, s, c,
+                               (const T*)table, ids, (X*)x, gbits);
+        else
+            hipLaunchKernelGGL((lookup_kernel<T, X, 4>), dim3(row_groups((c.tokens + 3) / 4, gbits)), dim3(kRowBlock), 0, s,
+                               c, (const T*)table, ids, (X*)x, gbits);
         return hipGetLastError();
     });
 }

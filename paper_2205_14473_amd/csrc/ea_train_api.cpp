@@ -167,12 +167,12 @@ int64_t norm_groups(int32_t ntensors, const ea_tensor_t* tensors, int64_t chunk)
 int check_embed(const ea_embed_t* c)
 {
     if (!c) return fail(EA_ERR_ARG, "config is NULL");
-    if (c->tokens < 0 || c->tokens >= ((int64_t)1 << 31) - ((int64_t)1 << 16))
-        return fail(EA_ERR_ARG, "tokens must be in [0, 2^31 - 2^16) (got %lld)", (long long)c->tokens);
+    if (c->tokens < 0 || c->tokens >= (int64_t)1 << 30)
+        return fail(EA_ERR_ARG, "tokens must be in [0, 2^30) (got %lld)", (long long)c->tokens);
     if (c->vocab < 1 || c->vocab >= ((int64_t)1 << 31) - 1)
         return fail(EA_ERR_ARG, "vocab must be in [1, 2^31 - 1) (got %lld)", (long long)c->vocab);
-    if (c->dim < 1 || c->dim >= ((int64_t)1 << 24))
-        return fail(EA_ERR_ARG, "dim must be in [1, 2^24) (got %lld)", (long long)c->dim);
+    if (c->dim < 1 || c->dim > (int64_t)1 << 20)
+        return fail(EA_ERR_ARG, "dim must be in [1, 2^20] (got %lld)", (long long)c->dim);
     if (c->table_stride < c->dim || c->table_stride >= ((int64_t)1 << 32))
         return fail(EA_ERR_ARG, "table_stride must be in [dim, 2^32) (got %lld)", (long long)c->table_stride);
     if (c->x_stride < c->dim || c->x_stride >= ((int64_t)1 << 32))
