@@ -50,13 +50,22 @@ for _name, _res, _args in (
     getattr(lib, _name).restype, getattr(lib, _name).argtypes = _res, _args
 
 
+_types = None        # torch's dtypes by EA_F32, EA_BF16, EA_F16; looked up on first use
+
+
+def _dtypes():
+    global _types
+    if _types is None:
+        import torch
+        _types = (torch.float32, torch.bfloat16, torch.float16)
+    return _types
+
+
 def ea_type(dtype) -> int:
     """EA_F32, EA_BF16 or EA_F16 for a torch dtype."""
-    import torch
-    types = {torch.float32: EA_F32, torch.bfloat16: EA_BF16, torch.float16: EA_F16}
-    if dtype not in types:
+    if dtype not in _dtypes():
         raise ValueError(f"libea takes float32, bfloat16 or float16 here, got {dtype}")
-    return types[dtype]
+    return _types.index(dtype)
 
 
 def _dense(t) -> bool:
@@ -96,7 +105,7 @@ class TensorList:
         if p is not None:
             self.param_type = self._set("p", p, g, dtype=None)
             if master is not None:
-                self._set("master", master, p, dtype="float32", optional=True)
+                self._set("master", master, p, dtype=_dtypes()[EA_F32], optional=True)
         if (m is None) != (v is None):
             raise ValueError("m and v come together")
         if m is not None:
@@ -107,24 +116,28 @@ class TensorList:
         self._held = (p, m, v, m_scale, v_scale, master)
 
     def _set(self, name, ts, like, dtype, optional=False):
-        import torch
-        kind = None
-        for i, (t, e) in enumerate(zip(ts, like)):
+        kind, array, field = None, self.array, getattr(Tensor, name)
+        for i, t in enumerate(ts):
             if t is None and optional:
                 continue
+            if dtype is not None and t.dtype is not dtype:
+                raise ValueError(f"{name}[{i}]: expected {dtype}, got {t.dtype}")
+            if kind is None:
+                kind = t.dtype
+            elif t.dtype is not kind:
+                raise ValueError(f"{name}[{i}]: all of {name} share one type, got {t.dtype} after {kind}")
             if not t.is_cuda:
                 raise ValueError("libea needs device tensors")
-            if dtype is not None and t.dtype is not getattr(torch, dtype):
-                raise ValueError(f"{name}[{i}]: expected {dtype}, got {t.dtype}")
-            if kind is not None and t.dtype is not kind:
-                raise ValueError(f"{name}[{i}]: all of {name} share one type, got {t.dtype} after {kind}")
-            kind = t.dtype
-            if t.device != e.device:
-                raise ValueError(f"{name}[{i}] is on {t.device}, and others on {e.device}")
-            if t.shape != e.shape or (t.stride() != e.stride() and t.numel() > 1) or not _dense(t):
-                raise ValueError(f"{name}[{i}]: shape {tuple(t.shape)}, strides {t.stride()} do not match the "
-                                 f"parameter's {tuple(e.shape)}, {e.stride()}, or leave gaps")
-            setattr(self.array[i], name, t.data_ptr())
+            e = like[i]
+            if e is not t:
+                if t.device != e.device:
+                    raise ValueError(f"{name}[{i}] is on {t.device}, and others on {e.device}")
+                if t.shape != e.shape or (t.stride() != e.stride() and t.numel() > 1):
+                    raise ValueError(f"{name}[{i}]: shape {tuple(t.shape)}, strides {t.stride()} are not the "
+                                     f"parameter's {tuple(e.shape)}, {e.stride()}")
+            if not t.is_contiguous() and not _dense(t):
+                raise ValueError(f"{name}[{i}]: strides {t.stride()} leave gaps in shape {tuple(t.shape)}")
+            field.__set__(array[i], t.data_ptr())
         return None if kind is None or dtype is not None else ea_type(kind)
 
     def _set_states(self, m, v, m_scale, v_scale):
@@ -137,15 +150,16 @@ class TensorList:
             if ts is None or (bits == 32 and name.endswith("scale")):
                 continue
             want = codes if bits == 8 and name in "mv" else (torch.float32,)
+            per, array, field = (1 if name in "mv" else EA_STATE_BLOCK), self.array, getattr(Tensor, name)
             for i, t in enumerate(ts):
-                n = self.array[i].n
-                most = n if name in "mv" else (n + EA_STATE_BLOCK - 1) // EA_STATE_BLOCK
+                most = (array[i].n + per - 1) // per
                 if not t.is_cuda:
                     raise ValueError("libea needs device tensors")
-                if t.dtype not in want or t.numel() != most or not _dense(t) or t.device != self._g[i].device:
+                if t.dtype not in want or t.numel() != most or t.device != self._g[i].device or \
+                        not (t.is_contiguous() or _dense(t)):
                     raise ValueError(f"{name}[{i}]: expected {most} dense elements of {want[0]} on the gradient's "
                                      f"device, got {t.numel()} of {t.dtype} on {t.device}")
-                setattr(self.array[i], name, t.data_ptr())
+                field.__set__(array[i], t.data_ptr())
         return bits
 
     def set_grads(self, g):
@@ -204,6 +218,8 @@ def _rows(t, kind, rows, dim, stride, name):
     """Pointer of a [rows, dim] tensor (leading dimensions may be split) with `stride` elements between rows."""
     if t is None or isinstance(t, int):
         return t
+    if t.is_cuda and t.shape == (rows, dim) and t.stride() == (stride, 1) and t.dtype is _dtypes()[kind]:
+        return t.data_ptr()
     if not t.is_cuda:
         raise ValueError("libea needs device tensors")
     if ea_type(t.dtype) != kind:

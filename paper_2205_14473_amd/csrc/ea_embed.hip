@@ -35,7 +35,10 @@ __device__ __forceinline__ int64_t id_at(const void* ids, int bits, int64_t i)
 
 // ---- lookup -------------------------------------------------------------------
 
-// R consecutive tokens a group of lanes: their ids first, then a quad of each row.
+// R consecutive tokens a group of lanes: their ids first, then a quad of each
+// row.  With more than one the rows written pass the caches by, which stay with
+// the table's frequent rows (65,536 tokens, 1024 columns: 62 us with plain
+// stores, 42 without).
 template <class T, class X, int R>
 __global__ void __launch_bounds__(kRowBlock) lookup_kernel(ea_embed_t c, const T* table, const void* ids, X* x, int gbits)
 {
@@ -61,10 +64,12 @@ __global__ void __launch_bounds__(kRowBlock) lookup_kernel(ea_embed_t c, const T
             for (int r = 0; r < R; ++r) {
                 X* to = x + (i + r) * c.x_stride + k;
                 if (i + r < c.tokens) {
-                    if (n == 4)
-                        store4(to, narrow<X>(v[r]));
-                    else
+                    if (n != 4)
                         store_some(to, narrow<X>(v[r]), n);
+                    else if (R > 1)
+                        store4_once(to, narrow<X>(v[r]));
+                    else
+                        store4(to, narrow<X>(v[r]));
                 }
             }
         }
@@ -99,7 +104,7 @@ __device__ __forceinline__ void fill_zeros(const Fill& f, uint32_t group, uint32
     }
 }
 
-constexpr unsigned kFillGroups = 512;    // two workgroups of 1024 for each CU
+constexpr unsigned kFillGroups = 1024;   // of 1024 threads: 512 and 256 a little slower
 
 __global__ void __launch_bounds__(1024) fill_kernel16(Fill f)
 {
@@ -112,14 +117,16 @@ constexpr int kSortBlock = 1024;
 constexpr int kSortWaves = kSortBlock / kWave;
 constexpr int kMostBits = 9;             // of one pass's digit
 constexpr int kMostValues = 1 << kMostBits;
-constexpr int64_t kLeastTile = 2048;     // items of one workgroup
-constexpr int64_t kMostTiles = 128;
-constexpr int kBatch = 4;                // items a lane loads ahead
-constexpr int kOneRounds = 4;            // items a lane holds where one workgroup sorts all
-constexpr int64_t kOneTile = kSortBlock * kOneRounds;
+constexpr int kRounds = 4;               // items a lane holds, at most
+constexpr int64_t kMostTile = kSortBlock * kRounds;
+constexpr int64_t kLeastTile = kSortBlock * 2;
+constexpr int64_t kFewTiles = 128;       // whose counts every workgroup of a scatter adds up itself
+constexpr int kTilesAhead = 16;          // tiles' counts a thread loads ahead
+static_assert(kSortBlock >= 2 * kMostValues, "a digit has threads to share its tiles");
 
 struct SortPlan {
-    int64_t n, tile, tiles;
+    int64_t n, tiles;
+    int tile;                            // items of one workgroup
     int passes, bits;                    // digit width of each pass
 };
 
@@ -127,9 +134,7 @@ SortPlan sort_plan(const ea_embed_t& c)
 {
     SortPlan p;
     p.n = c.tokens;
-    p.tile = (c.tokens + kMostTiles - 1) / kMostTiles;
-    p.tile = (p.tile + kSortBlock - 1) / kSortBlock * kSortBlock;
-    if (p.tile < kLeastTile) p.tile = kLeastTile;
+    p.tile = (int)(c.tokens <= kLeastTile * kFewTiles ? kLeastTile : kMostTile);
     p.tiles = (c.tokens + p.tile - 1) / p.tile;
     int need = 1;
     while (c.vocab >> need) ++need;      // keys are 0 to vocab
@@ -194,13 +199,35 @@ __device__ __forceinline__ uint32_t sum_before(uint32_t x, uint32_t* sums)
     return base;
 }
 
+// Offsets of every wave's items of every digit, in place of its counts: `base`
+// is the first item of thread v's digit.
+__device__ __forceinline__ void place_waves(uint32_t (*place)[kMostValues], int values, uint32_t base)
+{
+    if ((int)threadIdx.x < values) {
+        uint32_t k[kSortWaves];
+#pragma unroll
+        for (int w = 0; w < kSortWaves; ++w) k[w] = place[w][threadIdx.x];
+#pragma unroll
+        for (int w = 0; w < kSortWaves; ++w) {
+            place[w][threadIdx.x] = base;
+            base += k[w];
+        }
+    }
+    __syncthreads();
+}
+
+__device__ __forceinline__ void no_places(uint32_t (*place)[kMostValues], int bits)
+{
+    for (int k = threadIdx.x; k < kSortWaves << bits; k += kSortBlock) place[k >> bits][k & ((1 << bits) - 1)] = 0;
+}
+
 // Tokens that one workgroup sorts in its registers and LDS, every pass in one
 // launch; the other workgroups zero the table.
 __global__ void __launch_bounds__(kSortBlock) sort_one_kernel(Items t, SortPlan p, uint32_t* keys, uint32_t* at, Fill f)
 {
     __shared__ uint32_t place[kSortWaves][kMostValues];
-    __shared__ uint32_t skey[kOneTile];
-    __shared__ uint16_t sat[kOneTile];
+    __shared__ uint32_t skey[kMostTile];
+    __shared__ uint16_t sat[kMostTile];
     __shared__ uint32_t sums[kSortWaves];
     if (blockIdx.x > 0) {
         fill_zeros<kSortBlock>(f, blockIdx.x - 1, gridDim.x - 1);
@@ -208,35 +235,30 @@ __global__ void __launch_bounds__(kSortBlock) sort_one_kernel(Items t, SortPlan 
     }
     const int values = 1 << p.bits, wave = threadIdx.x / kWave, lane = lane_id(), n = (int)p.n;
     const int rounds = (n + kSortBlock - 1) / kSortBlock, begin = wave * rounds * kWave + lane;
-    uint32_t key[kOneRounds], from[kOneRounds], rank[kOneRounds];
+    uint32_t key[kRounds], from[kRounds], rank[kRounds];
 #pragma unroll
-    for (int r = 0; r < kOneRounds; ++r) {
+    for (int r = 0; r < kRounds; ++r) {
         const int i = begin + r * kWave;
         from[r] = (uint32_t)i;
         key[r] = r < rounds && i < n ? key_of(t, i) : 0;
     }
     for (int pass = 0; pass < p.passes; ++pass) {
         const int shift = pass * p.bits;
-        for (int k = threadIdx.x; k < kSortWaves * values; k += kSortBlock) place[k / values][k % values] = 0;
+        no_places(place, p.bits);
         __syncthreads();
 #pragma unroll
-        for (int r = 0; r < kOneRounds; ++r)
+        for (int r = 0; r < kRounds; ++r)
             if (r < rounds)
                 rank[r] = take_place(place[wave], (key[r] >> shift) & (values - 1), p.bits, begin + r * kWave < n);
         __syncthreads();
         uint32_t all = 0;
-        if ((int)threadIdx.x < values)
-            for (int w = 0; w < kSortWaves; ++w) all += place[w][threadIdx.x];
-        uint32_t base = sum_before(all, sums);
-        if ((int)threadIdx.x < values)
-            for (int w = 0; w < kSortWaves; ++w) {
-                const uint32_t k = place[w][threadIdx.x];
-                place[w][threadIdx.x] = base;
-                base += k;
-            }
-        __syncthreads();
+        if ((int)threadIdx.x < values) {
 #pragma unroll
-        for (int r = 0; r < kOneRounds; ++r)
+            for (int w = 0; w < kSortWaves; ++w) all += place[w][threadIdx.x];
+        }
+        place_waves(place, values, sum_before(all, sums));
+#pragma unroll
+        for (int r = 0; r < kRounds; ++r)
             if (r < rounds && begin + r * kWave < n) {
                 const uint32_t to = place[wave][(key[r] >> shift) & (values - 1)] + rank[r];
                 skey[to] = key[r];
@@ -244,7 +266,7 @@ __global__ void __launch_bounds__(kSortBlock) sort_one_kernel(Items t, SortPlan 
             }
         __syncthreads();
 #pragma unroll
-        for (int r = 0; r < kOneRounds; ++r) {
+        for (int r = 0; r < kRounds; ++r) {
             const int i = begin + r * kWave;
             if (r < rounds && i < n) {
                 key[r] = skey[i];
@@ -253,7 +275,7 @@ __global__ void __launch_bounds__(kSortBlock) sort_one_kernel(Items t, SortPlan 
         }
     }
 #pragma unroll
-    for (int r = 0; r < kOneRounds; ++r) {
+    for (int r = 0; r < kRounds; ++r) {
         const int i = begin + r * kWave;
         if (r < rounds && i < n) {
             keys[i] = key[r];
@@ -262,98 +284,118 @@ __global__ void __launch_bounds__(kSortBlock) sort_one_kernel(Items t, SortPlan 
     }
 }
 
-__global__ void __launch_bounds__(kSortBlock) digits_kernel(Items t, SortPlan p, int shift, uint32_t* counts, Fill f)
+// Larger batches: the digits of each tile counted, then the tile's items put in place.
+__global__ void __launch_bounds__(kSortBlock) digits_kernel(Items t, SortPlan p, int shift, uint32_t* counts)
 {
     __shared__ uint32_t count[kMostValues];
-    if (blockIdx.x >= p.tiles) {
-        fill_zeros<kSortBlock>(f, blockIdx.x - (uint32_t)p.tiles, gridDim.x - (uint32_t)p.tiles);
-        return;
-    }
     const int values = 1 << p.bits;
+    const int64_t begin = (int64_t)blockIdx.x * p.tile + threadIdx.x;
+    uint32_t key[kRounds];
+#pragma unroll
+    for (int r = 0; r < kRounds; ++r) {
+        const int64_t i = begin + r * kSortBlock;
+        key[r] = r * kSortBlock < p.tile && i < p.n ? key_of(t, i) : 0;
+    }
     if ((int)threadIdx.x < values) count[threadIdx.x] = 0;
     __syncthreads();
-    const int64_t begin = blockIdx.x * p.tile, end = begin + p.tile < p.n ? begin + p.tile : p.n;
-#pragma unroll 2
-    for (int64_t i = begin + threadIdx.x; i < end; i += kSortBlock)
-        atomicAdd(&count[(key_of(t, i) >> shift) & (values - 1)], 1u);
+#pragma unroll
+    for (int r = 0; r < kRounds; ++r)
+        if (r * kSortBlock < p.tile && begin + r * kSortBlock < p.n)
+            atomicAdd(&count[(key[r] >> shift) & (values - 1)], 1u);
     __syncthreads();
     if ((int)threadIdx.x < values) counts[(int64_t)blockIdx.x * values + threadIdx.x] = count[threadIdx.x];
 }
 
-// Each wave owns a run of its tile's items.  Their digits are counted once to
-// place the waves, then walked in order, 64 at a time.
+// Many tiles: workgroup v turns digit v's counts into sums over the tiles
+// before each, and their total into the row after the last tile's.
+__global__ void __launch_bounds__(kSortBlock) prefix_kernel(SortPlan p, uint32_t* counts)
+{
+    __shared__ uint32_t sums[kSortWaves];
+    const int64_t values = (int64_t)1 << p.bits;
+    uint32_t* c = counts + blockIdx.x;
+    uint32_t base = 0;
+    for (int64_t b = 0; b < p.tiles; b += kSortBlock) {
+        const int64_t tile = b + threadIdx.x;
+        const uint32_t k = tile < p.tiles ? c[tile * values] : 0;
+        const uint32_t upto = sum_before(k, sums);
+        if (tile < p.tiles) c[tile * values] = base + upto;
+        uint32_t all = 0;
+        for (int w = 0; w < kSortWaves; ++w) all += sums[w];
+        base += all;
+        __syncthreads();
+    }
+    if (threadIdx.x == 0) c[p.tiles * values] = base;
+}
+
+// Each wave owns a run of its tile's items and ranks them among its own, 64 at
+// a time, in order; waves, tiles and digits before then add their counts.
 __global__ void __launch_bounds__(kSortBlock) scatter_kernel(Items t, SortPlan p, int shift, const uint32_t* counts,
                                                              uint32_t* keys, uint32_t* at, Fill f)
 {
     __shared__ uint32_t place[kSortWaves][kMostValues];
+    __shared__ uint32_t totals[2][kMostValues];
     __shared__ uint32_t sums[kSortWaves];
     if (blockIdx.x >= p.tiles) {
         fill_zeros<kSortBlock>(f, blockIdx.x - (uint32_t)p.tiles, gridDim.x - (uint32_t)p.tiles);
         return;
     }
-    const int values = 1 << p.bits, wave = threadIdx.x / kWave, lane = lane_id();
-    for (int k = threadIdx.x; k < kSortWaves * values; k += kSortBlock) place[k / values][k % values] = 0;
-    __syncthreads();
-    const int64_t run = p.tile / kSortWaves, begin = blockIdx.x * p.tile + wave * run;
-    const int64_t end = begin + run < p.n ? begin + run : p.n;
-    for (int64_t k = begin + lane; k < end; k += kBatch * kWave) {
-        uint32_t key[kBatch];
+    const int values = 1 << p.bits, wave = threadIdx.x / kWave, rounds = p.tile / kSortBlock;
+    const int64_t begin = (int64_t)blockIdx.x * p.tile + wave * rounds * kWave + lane_id();
+    uint32_t key[kRounds], from[kRounds], rank[kRounds];
 #pragma unroll
-        for (int r = 0; r < kBatch; ++r) key[r] = k + r * kWave < end ? key_of(t, k + r * kWave) : 0;
-#pragma unroll
-        for (int r = 0; r < kBatch; ++r)
-            if (k + r * kWave < end) atomicAdd(&place[wave][(key[r] >> shift) & (values - 1)], 1u);
+    for (int r = 0; r < kRounds; ++r) {
+        const int64_t i = begin + r * kWave;
+        const bool here = r < rounds && i < p.n;
+        key[r] = here ? key_of(t, i) : 0;
+        from[r] = here && !t.ids ? t.at[i] : (uint32_t)i;
     }
 
-    // thread v: items with digit v in all tiles, and in the tiles before this one
-    uint32_t all = 0, before = 0;
-    if ((int)threadIdx.x < values) {
-        const uint32_t* c = counts + threadIdx.x;
-        int64_t b = 0;
-        for (; b + 8 <= p.tiles; b += 8) {
-            uint32_t k[8];
+    // items with each digit in all tiles, and in the tiles before this one: the
+    // tiles' counts shared out among the threads of a digit
+    const uint32_t v = threadIdx.x & (values - 1);
+    uint32_t some = 0, some_before = 0;
+    if (p.tiles > kFewTiles) {
+        if ((int)threadIdx.x < values) {
+            some = counts[p.tiles * values + v];
+            some_before = counts[(int64_t)blockIdx.x * values + v];
+        }
+    } else {
+        const int shares = kSortBlock >> p.bits, tiles = (int)p.tiles;
+        for (int b = threadIdx.x >> p.bits; b < tiles; b += shares * kTilesAhead) {
+            uint32_t k[kTilesAhead];
 #pragma unroll
-            for (int r = 0; r < 8; ++r) k[r] = c[(b + r) * values];
-#pragma unroll
-            for (int r = 0; r < 8; ++r) {
-                all += k[r];
-                before += b + r < (int64_t)blockIdx.x ? k[r] : 0;
+            for (int r = 0; r < kTilesAhead; ++r) {
+                const int tile = b + r * shares;
+                k[r] = counts[(tile < tiles ? tile : b) * values + v];
             }
-        }
-        for (; b < p.tiles; ++b) {
-            const uint32_t k = c[b * values];
-            all += k;
-            before += b < (int64_t)blockIdx.x ? k : 0;
-        }
-    }
-    uint32_t base = sum_before(all, sums) + before;
-    if ((int)threadIdx.x < values)
-        for (int w = 0; w < kSortWaves; ++w) {
-            const uint32_t k = place[w][threadIdx.x];
-            place[w][threadIdx.x] = base;
-            base += k;
-        }
-    __syncthreads();
-
-    for (int64_t k = begin; k < end; k += kBatch * kWave) {
-        uint32_t key[kBatch], from[kBatch];
 #pragma unroll
-        for (int r = 0; r < kBatch; ++r) {
-            const int64_t i = k + r * kWave + lane;
-            key[r] = i < end ? key_of(t, i) : 0;
-            from[r] = t.ids || i >= end ? (uint32_t)i : t.at[i];
-        }
-#pragma unroll
-        for (int r = 0; r < kBatch; ++r) {
-            if (k + r * kWave >= end) break;
-            const bool here = k + r * kWave + lane < end;
-            const uint32_t to = take_place(place[wave], (key[r] >> shift) & (values - 1), p.bits, here);
-            if (here) {
-                keys[to] = key[r];
-                at[to] = from[r];
+            for (int r = 0; r < kTilesAhead; ++r) {
+                const int tile = b + r * shares;
+                some += tile < tiles ? k[r] : 0;
+                some_before += tile < (int)blockIdx.x ? k[r] : 0;
             }
         }
     }
+    no_places(place, p.bits);
+    (&totals[0][0])[threadIdx.x] = 0;
+    __syncthreads();
+    atomicAdd(&totals[0][v], some);
+    atomicAdd(&totals[1][v], some_before);
+#pragma unroll
+    for (int r = 0; r < kRounds; ++r)
+        if (r < rounds)
+            rank[r] = take_place(place[wave], (key[r] >> shift) & (values - 1), p.bits, begin + r * kWave < p.n);
+    __syncthreads();
+    const bool one = (int)threadIdx.x < values;
+    const uint32_t base = sum_before(one ? totals[0][v] : 0, sums);
+    place_waves(place, values, base + (one ? totals[1][v] : 0));
+#pragma unroll
+    for (int r = 0; r < kRounds; ++r)
+        if (r < rounds && begin + r * kWave < p.n) {
+            const uint32_t to = place[wave][(key[r] >> shift) & (values - 1)] + rank[r];
+            keys[to] = key[r];
+            at[to] = from[r];
+        }
 }
 
 // ---- sums -------------------------------------------------------------------------
@@ -508,12 +550,20 @@ __global__ void __launch_bounds__(kRowBlock) join_kernel(SumArgs a, T* table)
     const int lane = lane_id(), wave = threadIdx.x / kWave;
     const int64_t c = blockIdx.x, begin = c * a.chunk, end = begin + a.chunk;
     if (end >= a.n) return;
-    const uint32_t key = a.keys[end - 1];
-    if (key >= a.vocab || a.keys[end] != key) return;                              // ends here
-    if (begin > 0 && a.keys[begin] == key && a.keys[begin - 1] == key) return;    // began before
-    // the chunks after this one whose first key is still `key`: a 64-way search
-    int64_t rows = 0, range = a.chunks - 1 - c;
-    while (range > 0) {
+    // all keys at once, the next 64 chunks' first ones among them: most workgroups end here
+    const uint32_t key = a.keys[end - 1], next = a.keys[end], head = a.keys[begin];
+    const uint32_t before = a.keys[begin > 0 ? begin - 1 : 0];
+    int64_t rows = a.chunks - 1 - c, range = 0;
+    const uint32_t heads = a.keys[end + (lane < rows ? lane : 0) * a.chunk];
+    if ((key >= a.vocab) | (next != key)) return;                                  // ends here
+    if ((begin > 0) & (head == key) & (before == key)) return;                     // began before
+    // the chunks after this one whose first key is still `key`
+    {
+        const int hits = __popcll(__ballot(lane < rows && heads == key));
+        if (hits == kWave) range = rows - kWave;
+        rows = hits;
+    }
+    while (range > 0) {                                                            // more: a 64-way search
         const int64_t step = (range + kWave - 1) / kWave, probe = lane * step;
         const bool still = probe < range && a.keys[end + (rows + probe) * a.chunk] == key;
         const int hits = __popcll(__ballot(still));
@@ -528,15 +578,15 @@ __global__ void __launch_bounds__(kRowBlock) join_kernel(SumArgs a, T* table)
     const float* part = a.part + (c + 1) * 2 * a.part_row + col;
     v4f sum = {0.0f, 0.0f, 0.0f, 0.0f};
     if (col < a.dim) {
-        int64_t k = from;
-        for (; k + 2 * kAhead <= upto; k += 2 * kAhead) {
+        for (int64_t k = from; k < upto; k += 2 * kAhead) {
             v4f x[2 * kAhead];
 #pragma unroll
-            for (int r = 0; r < 2 * kAhead; ++r) x[r] = load4(part + (k + r) * 2 * a.part_row);
+            for (int r = 0; r < 2 * kAhead; ++r)
+                x[r] = load4(part + (k + r < upto ? k + r : upto - 1) * 2 * a.part_row);
 #pragma unroll
-            for (int r = 0; r < 2 * kAhead; ++r) sum = sum + x[r];
+            for (int r = 0; r < 2 * kAhead; ++r)
+                if (k + r < upto) sum = sum + x[r];
         }
-        for (; k < upto; ++k) sum = sum + load4(part + k * 2 * a.part_row);
     }
     sums[wave][lane] = sum;
     __syncthreads();
@@ -561,19 +611,25 @@ int64_t align16(int64_t x)
 constexpr int64_t kEnoughWaves = 8192;   // 32 for each CU
 constexpr int64_t kLeastChunk = 8;
 
+// Positions of a chunk: 64, or fewer where that leaves CUs without waves (wide
+// rows), or where so few tokens make short chunks the quicker ones (narrow rows).
+int64_t chunk_of(int64_t tokens, int64_t dim)
+{
+    const int64_t waves = (dim + kJoinCols - 1) / kJoinCols;
+    int64_t chunk = kMostChunk;
+    while (chunk > kLeastChunk && (group_bits(dim) < 6 ? tokens < 512 * chunk : tokens / chunk * waves < kEnoughWaves))
+        chunk /= 2;
+    return chunk;
+}
+
 GradPlan grad_plan(const ea_embed_t& c)
 {
     GradPlan p{};
     if (c.tokens == 0) return p;
     p.sort = sort_plan(c);
-    const int gbits = group_bits(c.dim);
-    const int64_t quads = (c.dim + 3) / 4;
-    p.chunk = kMostChunk;
-    while (p.chunk > kLeastChunk &&
-           (c.tokens / p.chunk) * (gbits < 6 ? 1 : (quads + kWave - 1) / kWave) < kEnoughWaves)
-        p.chunk /= 2;
+    p.chunk = chunk_of(c.tokens, c.dim);
     p.chunks = (c.tokens + p.chunk - 1) / p.chunk;
-    p.part_row = quads * 4;
+    p.part_row = (c.dim + 3) / 4 * 4;
     int64_t off = 0;
     for (int k = 0; k < 2; ++k) {
         p.off_keys[k] = off;
@@ -582,14 +638,14 @@ GradPlan grad_plan(const ea_embed_t& c)
         off += align16(c.tokens * 4);
     }
     p.off_counts = off;
-    off += align16(p.sort.tiles * ((int64_t)4 << p.sort.bits));
+    off += align16((p.sort.tiles + 1) * ((int64_t)4 << p.sort.bits));
     p.off_part = off;
     off += p.chunks * 2 * p.part_row * 4;
     p.bytes = off;
     return p;
 }
 
-// Workgroups for `rows` rows, one group of lanes each; kernels loop over the rest.
+// Workgroups for `rows` rows, one group of lanes each; the kernel loops over the rest.
 unsigned row_groups(int64_t rows, int gbits)
 {
     const int64_t per = (int64_t)1 << (8 - gbits), blocks = (rows + per - 1) / per;
@@ -629,20 +685,20 @@ hipError_t start_grad(const ea_embed_t& c, const GradPlan& p, const void* ids, c
     uint32_t* counts = (uint32_t*)(ws + p.off_counts);
     const auto keys = [&](int k) { return (uint32_t*)(ws + p.off_keys[k & 1]); };
     const auto at = [&](int k) { return (uint32_t*)(ws + p.off_at[k & 1]); };
-    if (c.tokens <= kOneTile) {
+    if (c.tokens <= kMostTile) {
         hipLaunchKernelGGL(sort_one_kernel, dim3(1 + groups), dim3(kSortBlock), 0, s, t, p.sort, keys(0), at(0),
                            fill_part(f, units, 0, 1));
         t.keys = keys(0);
         t.at = at(0);
     } else {
         const unsigned tiles = (unsigned)p.sort.tiles;
-        const int of = 2 * p.sort.passes;
         for (int k = 0; k < p.sort.passes; ++k) {
             const int shift = k * p.sort.bits;
-            hipLaunchKernelGGL(digits_kernel, dim3(tiles + groups), dim3(kSortBlock), 0, s, t, p.sort, shift, counts,
-                               fill_part(f, units, 2 * k, of));
+            hipLaunchKernelGGL(digits_kernel, dim3(tiles), dim3(kSortBlock), 0, s, t, p.sort, shift, counts);
+            if (p.sort.tiles > kFewTiles)
+                hipLaunchKernelGGL(prefix_kernel, dim3(1u << p.sort.bits), dim3(kSortBlock), 0, s, p.sort, counts);
             hipLaunchKernelGGL(scatter_kernel, dim3(tiles + groups), dim3(kSortBlock), 0, s, t, p.sort, shift, counts,
-                               keys(k), at(k), fill_part(f, units, 2 * k + 1, of));
+                               keys(k), at(k), fill_part(f, units, k, p.sort.passes));
             t.ids = nullptr;
             t.keys = keys(k);
             t.at = at(k);
