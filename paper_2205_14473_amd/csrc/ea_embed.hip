@@ -168,7 +168,8 @@ __device__ __forceinline__ void wave_sync()
 
 // A lane's place among its wave's items of one digit: `count` holds the digits'
 // running counts, which move on by the 64 lanes' items.
-__device__ __forceinline__ uint32_t take_place(uint32_t* count, uint32_t digit, int bits, bool here)
+template <class C>
+__device__ __forceinline__ uint32_t take_place(C* count, uint32_t digit, int bits, bool here)
 {
     uint64_t same = __ballot(here);
     for (int b = 0; b < bits; ++b) {
@@ -178,7 +179,7 @@ __device__ __forceinline__ uint32_t take_place(uint32_t* count, uint32_t digit, 
     const uint64_t lower = same & ((1ull << lane_id()) - 1);
     const uint32_t first = here ? count[digit] : 0;
     wave_sync();
-    if (here && !lower) count[digit] = first + (uint32_t)__popcll(same);
+    if (here && !lower) count[digit] = (C)(first + (uint32_t)__popcll(same));
     wave_sync();
     return first + (uint32_t)__popcll(lower);
 }
@@ -201,7 +202,8 @@ __device__ __forceinline__ uint32_t sum_before(uint32_t x, uint32_t* sums)
 
 // Offsets of every wave's items of every digit, in place of its counts: `base`
 // is the first item of thread v's digit.
-__device__ __forceinline__ void place_waves(uint32_t (*place)[kMostValues], int values, uint32_t base)
+template <class C>
+__device__ __forceinline__ void place_waves(C (*place)[kMostValues], int values, uint32_t base)
 {
     if ((int)threadIdx.x < values) {
         uint32_t k[kSortWaves];
@@ -209,14 +211,15 @@ __device__ __forceinline__ void place_waves(uint32_t (*place)[kMostValues], int 
         for (int w = 0; w < kSortWaves; ++w) k[w] = place[w][threadIdx.x];
 #pragma unroll
         for (int w = 0; w < kSortWaves; ++w) {
-            place[w][threadIdx.x] = base;
+            place[w][threadIdx.x] = (C)base;
             base += k[w];
         }
     }
     __syncthreads();
 }
 
-__device__ __forceinline__ void no_places(uint32_t (*place)[kMostValues], int bits)
+template <class C>
+__device__ __forceinline__ void no_places(C (*place)[kMostValues], int bits)
 {
     for (int k = threadIdx.x; k < kSortWaves << bits; k += kSortBlock) place[k >> bits][k & ((1 << bits) - 1)] = 0;
 }
@@ -225,10 +228,9 @@ __device__ __forceinline__ void no_places(uint32_t (*place)[kMostValues], int bi
 // launch; the other workgroups zero the table.
 __global__ void __launch_bounds__(kSortBlock) sort_one_kernel(Items t, SortPlan p, uint32_t* keys, uint32_t* at, Fill f)
 {
-    __shared__ uint32_t place[kSortWaves][kMostValues];
-    __shared__ uint32_t skey[kMostTile];
+    __shared__ uint16_t place[kSortWaves][kMostValues];
+    __shared__ uint32_t skey[kMostTile];  // and sum_before's sums, while the registers hold the keys
     __shared__ uint16_t sat[kMostTile];
-    __shared__ uint32_t sums[kSortWaves];
     if (blockIdx.x > 0) {
         fill_zeros<kSortBlock>(f, blockIdx.x - 1, gridDim.x - 1);
         return;
@@ -256,7 +258,7 @@ __global__ void __launch_bounds__(kSortBlock) sort_one_kernel(Items t, SortPlan 
 #pragma unroll
             for (int w = 0; w < kSortWaves; ++w) all += place[w][threadIdx.x];
         }
-        place_waves(place, values, sum_before(all, sums));
+        place_waves(place, values, sum_before(all, skey));
 #pragma unroll
         for (int r = 0; r < kRounds; ++r)
             if (r < rounds && begin + r * kWave < n) {
@@ -503,16 +505,26 @@ __global__ void __launch_bounds__(kRowBlock) sum_narrow_kernel(SumArgs a, const 
     uint32_t key = a.keys[begin];
     bool open = begin > 0 && a.keys[begin - 1] == key;
     v4f sum = {0.0f, 0.0f, 0.0f, 0.0f};
+    uint32_t next_keys[kAhead], next_at[kAhead];
+    const auto fetch = [&](int64_t k) {
+#pragma unroll
+        for (int r = 0; r < kAhead; ++r) {
+            const int64_t i = k + r < end ? k + r : end - 1;
+            next_keys[r] = a.keys[i];
+            next_at[r] = a.at[i];
+        }
+    };
+    fetch(begin);
     for (int64_t k = begin; k < end; k += kAhead) {
         uint32_t keys[kAhead];
         typename Quad<X>::vec x[kAhead];
 #pragma unroll
         for (int r = 0; r < kAhead; ++r) {
-            const int64_t i = k + r < end ? k + r : end - 1;
-            keys[r] = a.keys[i];
-            const X* from = dx + (int64_t)a.at[i] * a.x_stride + col;
-            if (keys[r] < a.vocab) x[r] = n == 4 ? load4(from) : load_some(from, n);
+            keys[r] = next_keys[r];
+            const X* from = dx + (int64_t)next_at[r] * a.x_stride + col;
+            if (keys[r] < a.vocab) x[r] = n == 4 ? load4_once(from) : load_some(from, n);
         }
+        if (k + kAhead < end) fetch(k + kAhead);
 #pragma unroll
         for (int r = 0; r < kAhead; ++r) {
             if (k + r >= end) break;
@@ -608,7 +620,7 @@ int64_t align16(int64_t x)
     return (x + 15) / 16 * 16;
 }
 
-constexpr int64_t kEnoughWaves = 8192;   // 32 for each CU
+constexpr int64_t kEnoughWaves = 4096;   // 16 for each CU (8192: 16,384 tokens 49 us against 46)
 constexpr int64_t kLeastChunk = 8;
 
 // Positions of a chunk: 64, or fewer where that leaves CUs without waves (wide
@@ -617,7 +629,7 @@ int64_t chunk_of(int64_t tokens, int64_t dim)
 {
     const int64_t waves = (dim + kJoinCols - 1) / kJoinCols;
     int64_t chunk = kMostChunk;
-    while (chunk > kLeastChunk && (group_bits(dim) < 6 ? tokens < 512 * chunk : tokens / chunk * waves < kEnoughWaves))
+    while (chunk > kLeastChunk && (group_bits(dim) < 6 ? tokens < 4096 * chunk : tokens / chunk * waves < kEnoughWaves))
         chunk /= 2;
     return chunk;
 }
