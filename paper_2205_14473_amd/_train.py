@@ -114,6 +114,10 @@ class TensorList:
             self.array[i].weight_decay = weight_decay if isinstance(weight_decay, (int, float)) else weight_decay[i]
             self.array[i].lr_scale = lr_scale if isinstance(lr_scale, (int, float)) else lr_scale[i]
         self._held = (p, m, v, m_scale, v_scale, master)
+        if p is not None:
+            at = [e.p for e in self.array[:n] if e.n > 0]
+            if len(set(at)) != len(at):
+                raise ValueError("a parameter is in the list twice")
 
     def _set(self, name, ts, like, dtype, optional=False):
         kind, array, field = None, self.array, getattr(Tensor, name)
@@ -130,7 +134,7 @@ class TensorList:
                 raise ValueError("libea needs device tensors")
             e = like[i]
             if e is not t:
-                if t.device != e.device:
+                if t.get_device() != e.get_device():
                     raise ValueError(f"{name}[{i}] is on {t.device}, and others on {e.device}")
                 if t.shape != e.shape or (t.stride() != e.stride() and t.numel() > 1):
                     raise ValueError(f"{name}[{i}]: shape {tuple(t.shape)}, strides {t.stride()} are not the "
@@ -174,10 +178,23 @@ class TensorList:
                 raise ValueError(f"g[{i}]: {t.numel()} elements, and the parameter has {self.array[i].n}")
             self.array[i].n = t.numel()
         self.grad_type = kind
+        self.device = g[0].get_device() if g else None
+        for t in g:
+            if t.get_device() != self.device:
+                raise ValueError("the tensors are not all on one device")
         self._g = g
 
 
+def _here(device):
+    if device is not None and device != B._device():
+        raise ValueError(f"the tensors are on device {device}, and the current device is {B._device()}")
+
+
 def _check_list(cfg, tensors):
+    B._f32()                     # torch's lookups, made once
+    _here(tensors.device)
+    if tensors.param_type is None and tensors.count:
+        raise ValueError("a step needs p, m and v")
     if tensors.count and (tensors.param_type, tensors.grad_type, tensors.state_bits) != \
             (cfg.param_type, cfg.grad_type, cfg.state_bits):
         raise ValueError(f"the tensors' types (param {tensors.param_type}, grad {tensors.grad_type}, states "
@@ -203,6 +220,7 @@ def ea_grad_norm_workspace_bytes(tensors) -> int:
 
 def ea_grad_norm(tensors, scale, max_norm, norm, gscale, workspace, stream=None):
     f = B._f32()
+    _here(tensors.device)
     _room(workspace, lib.ea_grad_norm_workspace_bytes(tensors.count, tensors.array))
     return _check(lib.ea_grad_norm(EA_F32 if tensors.grad_type is None else tensors.grad_type, tensors.count,
                                    tensors.array, scale, max_norm, _ptr(norm, f), _ptr(gscale, f), _ptr(workspace),
@@ -210,6 +228,8 @@ def ea_grad_norm(tensors, scale, max_norm, norm, gscale, workspace, stream=None)
 
 
 def _room(workspace, need):
+    if need < 0:
+        raise B.EAError(need, B.ea_last_error())
     if need > 0 and hasattr(workspace, "numel") and workspace.numel() * workspace.element_size() < need:
         raise ValueError(f"the workspace holds {workspace.numel() * workspace.element_size()} bytes, {need} are needed")
 
@@ -218,6 +238,7 @@ def _rows(t, kind, rows, dim, stride, name):
     """Pointer of a [rows, dim] tensor (leading dimensions may be split) with `stride` elements between rows."""
     if t is None or isinstance(t, int):
         return t
+    _here(t.get_device() if t.is_cuda else None)
     if t.is_cuda and t.shape == (rows, dim) and t.stride() == (stride, 1) and t.dtype is _dtypes()[kind]:
         return t.data_ptr()
     if not t.is_cuda:
@@ -249,6 +270,7 @@ def _ids(t, cfg):
 
 
 def ea_embed_lookup(cfg, table, ids, x, stream=None):
+    B._f32()
     return _check(lib.ea_embed_lookup(C.byref(cfg),
                                       _rows(table, cfg.table_type, cfg.vocab, cfg.dim, cfg.table_stride, "table"),
                                       _ids(ids, cfg), _rows(x, cfg.x_type, cfg.tokens, cfg.dim, cfg.x_stride, "x"),
@@ -260,6 +282,7 @@ def ea_embed_workspace_bytes(cfg) -> int:
 
 
 def ea_embed_grad(cfg, ids, dx, dtable, accumulate, workspace, stream=None):
+    B._f32()
     _room(workspace, lib.ea_embed_workspace_bytes(C.byref(cfg)))
     return _check(lib.ea_embed_grad(C.byref(cfg), _ids(ids, cfg),
                                     _rows(dx, cfg.x_type, cfg.tokens, cfg.dim, cfg.x_stride, "dx"),

@@ -106,7 +106,7 @@ __device__ __forceinline__ void fill_zeros(const Fill& f, uint32_t group, uint32
 
 constexpr unsigned kFillGroups = 1024;   // of 1024 threads: 512 and 256 a little slower
 
-__global__ void __launch_bounds__(1024) fill_kernel16(Fill f)
+__global__ void __launch_bounds__(1024) fill_kernel(Fill f)
 {
     fill_zeros<1024>(f, blockIdx.x, gridDim.x);
 }
@@ -689,8 +689,8 @@ hipError_t start_grad(const ea_embed_t& c, const GradPlan& p, const void* ids, c
     const int64_t units = f.units * lines;
     const unsigned groups = units == 0 ? 0 : (unsigned)(units / kSortBlock < kFillGroups ? units / kSortBlock + 1 : kFillGroups);
     if (c.tokens == 0) {
-        if (groups)
-            hipLaunchKernelGGL(fill_kernel16, dim3(groups), dim3(kSortBlock), 0, s, fill_part(f, units, 0, 1));
+        if (groups == 0) return hipSuccess;
+        hipLaunchKernelGGL(fill_kernel, dim3(groups), dim3(kSortBlock), 0, s, fill_part(f, units, 0, 1));
         return hipGetLastError();
     }
     Items t{ids, nullptr, nullptr, c.index_bits, c.vocab, c.padding};

@@ -202,6 +202,8 @@ int ea_adamw_step_scheduled(const ea_adamw_t* c, const ea_schedule_t* s, uint32_
 {
     const int rc = check_schedule(s);
     if (rc) return rc;
+    if (s->kind == EA_SCHED_ASSUMPTION2 && !(1.0f - s->theta / (float)s->T < 1.0f))
+        return fail(EA_ERR_ARG, "schedule theta / T is too small: beta2 rounds to 1");
     if (!t_dev || ((uintptr_t)t_dev & 3u)) return fail(EA_ERR_ALIGN, "t_dev must be a 4-byte aligned device pointer");
     return adamw_impl("ea_adamw_step_scheduled", c, s, 1, t_dev, ntensors, tensors, gscale, stream);
 }

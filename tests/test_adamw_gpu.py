@@ -344,3 +344,57 @@ def test_no_tensors():
     E.ea_adamw_step(config(), 1, E.TensorList([], p=[], m=[], v=[]))
     e = torch.empty(0, device="cuda")
     E.ea_adamw_step(config(), 1, adamw_list([e], [e.clone()]))
+
+
+def test_lists_that_do_not_fit_are_refused():
+    f = lambda *shape, **kw: torch.zeros(*shape, device="cuda", **kw)  # noqa: E731
+    p = f(4, 8)
+    for bad, text in ((dict(p=[f(4, 9)]), "shape"), (dict(p=[f(8, 4).t()]), "strides"),
+                      (dict(p=[p], m=[f(32)]), "m and v"), (dict(p=[p], m=[f(31)], v=[f(32)]), r"m\[0\]"),
+                      (dict(p=[p], m=[f(32, dtype=torch.float64)], v=[f(32)]), r"m\[0\]"),
+                      (dict(p=[p.double()]), "float32, bfloat16 or float16"),
+                      (dict(p=[p], m=[f(32, dtype=torch.uint8)], v=[f(32, dtype=torch.uint8)]), "m_scale"),
+                      (dict(p=[p], master=[f(4, 8, dtype=torch.float16)]), "master")):
+        with pytest.raises(ValueError, match=text):
+            E.TensorList([f(4, 8)], **bad)
+    with pytest.raises(ValueError, match="gaps"):
+        E.TensorList([f(4, 10)[:, :8]])
+    with pytest.raises(ValueError, match="share one type"):
+        E.TensorList([f(3), f(3, dtype=torch.bfloat16)])
+    with pytest.raises(ValueError, match="twice"):
+        E.TensorList([f(32), f(32)], p=[p.view(-1), p.view(-1)], m=[f(32), f(32)], v=[f(32), f(32)])
+    tl = adamw_list([p], [f(4, 8)])
+    for cfg in (config(grad=torch.bfloat16), config(param=torch.bfloat16), config(bits=8)):
+        with pytest.raises(ValueError, match="not the configuration's"):
+            E.ea_adamw_step(cfg, 1, tl)
+    with pytest.raises(ValueError, match="needs p"):
+        E.ea_adamw_step(config(), 1, E.TensorList([f(3)]))
+    with pytest.raises(ValueError, match="the gradients' type changed"):
+        tl.set_grads([f(4, 8, dtype=torch.bfloat16)])
+    with pytest.raises(E.EAError, match="beta1"):
+        E.ea_adamw_step(config(beta1=1.0), 1, tl)
+    assert not p.any() and not any(s.any() for s in tl.states)
+
+
+def test_parts_of_very_large_tensors():
+    """A tensor of more than 2^30 elements is stepped in parts: its ends, the parts' borders and the
+    draws there against the same elements in a tensor of their own."""
+    n = (1 << 30) + 777
+    cfg = config(torch.bfloat16, torch.bfloat16, 8, rounding=E.EA_ROUND_STOCHASTIC, seed=3)
+    p, g = (torch.zeros(n, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    spots = [0, (1 << 30) - 1024, 1 << 30]
+    for k, a in enumerate(spots):
+        g[a:a + 777] = torch.randn(777, generator=torch.Generator().manual_seed(k)).to(torch.bfloat16)
+    tl = adamw_list([p], [g], state_bits=8)
+    E.ea_adamw_step(cfg, 5, tl)
+    for a in spots:
+        for kept, roots in ((tl.states[0], False), (tl.states[1], True)):
+            gk = g[a:a + 768].float().cpu().numpy()
+            m, r, _, want = R.adamw32(np.zeros(768, np.float32), gk, np.zeros(768, np.float32),
+                                      np.zeros(768, np.float32), 5, **HYPER)
+            word = R.philox_words(3, 5, 0, 768, a // 4)
+            codes, _ = R.encode32(r if roots else m, roots, word & 0xFFFF if roots else word >> 16)
+            assert np.array_equal(kept[a:a + 768].view(torch.uint8).cpu().numpy(), codes), a
+        R.within(p[a:a + 768], torch.from_numpy(want).double(), torch.full((768,), 1e-9).double(), f"p at {a}",
+                 extra=R.U16[torch.bfloat16])
+    assert not p[4096:4096 + 100].any()

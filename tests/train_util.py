@@ -103,10 +103,11 @@ def encode32(x, roots, u=None):
     return code.reshape(-1)[:n], scale
 
 
-def philox_words(seed, t, stream, n):
-    """The 32-bit word of each of n elements: word k & 3 of Philox4x32-10 at counter (k >> 2, t, stream)."""
+def philox_words(seed, t, stream, n, first=0):
+    """The 32-bit word of each of n elements from element 4 * first: word k & 3 of Philox4x32-10 at counter
+    (k >> 2, t, stream)."""
     m = np.uint64(0xFFFFFFFF)
-    quad = np.arange((n + 3) // 4, dtype=np.uint64)
+    quad = np.arange(first, first + (n + 3) // 4, dtype=np.uint64)
     x, y = quad & m, quad >> np.uint64(32)
     z, w = np.full_like(quad, t), np.full_like(quad, stream)
     k0, k1 = seed & 0xFFFFFFFF, seed >> 32
