@@ -94,8 +94,8 @@ typedef struct ea_adamw {
  *     applied to counter {lo(n>>2), hi(n>>2), t, i} with key {lo(seed),
  *     hi(seed)} (see ea.h): the high 16 bits for m, the low ones for r.
  *
- * tensors (host, ntensors) is read during the call.  ntensors >= 0; fewer
- * than 2^40 elements in all.  gscale (device, one float, or NULL). */
+ * tensors (host, ntensors) is read during the call.  0 <= ntensors <=
+ * 2^22, fewer than 2^40 elements in all.  gscale (device, one float, or NULL). */
 int ea_adamw_step(const ea_adamw_t *c, int64_t t, int32_t ntensors, const ea_tensor_t *tensors, const float *gscale,
                   void *stream);
 

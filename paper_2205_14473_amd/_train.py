@@ -185,18 +185,21 @@ class TensorList:
         self._g = g
 
 
-def _here(device):
-    if device is not None and device != B._device():
-        raise ValueError(f"the tensors are on device {device}, and the current device is {B._device()}")
+def _queue(stream, device):
+    """The raw stream of a call on tensors of `device`, which has to be the current one."""
+    if B._torch is None:
+        B._load_torch()
+    here = B._device()
+    if device != here and device is not None:
+        raise ValueError(f"the tensors are on device {device}, and the current device is {here}")
+    return B._raw_stream(here) if stream is None and B._raw_stream else _stream(stream)
 
 
 def _check_list(cfg, tensors):
-    B._f32()                     # torch's lookups, made once
-    _here(tensors.device)
-    if tensors.param_type is None and tensors.count:
-        raise ValueError("a step needs p, m and v")
-    if tensors.count and (tensors.param_type, tensors.grad_type, tensors.state_bits) != \
-            (cfg.param_type, cfg.grad_type, cfg.state_bits):
+    if tensors.count and (tensors.state_bits != cfg.state_bits or tensors.param_type != cfg.param_type or
+                          tensors.grad_type != cfg.grad_type):
+        if tensors.param_type is None or tensors.state_bits is None:
+            raise ValueError("a step needs p, m and v")
         raise ValueError(f"the tensors' types (param {tensors.param_type}, grad {tensors.grad_type}, states "
                          f"{tensors.state_bits} bits) are not the configuration's ({cfg.param_type}, "
                          f"{cfg.grad_type}, {cfg.state_bits} bits)")
@@ -204,14 +207,15 @@ def _check_list(cfg, tensors):
 
 def ea_adamw_step(cfg, t, tensors, gscale=None, stream=None):
     _check_list(cfg, tensors)
-    return _check(lib.ea_adamw_step(C.byref(cfg), t, tensors.count, tensors.array, _ptr(gscale, B._f32()),
-                                    _stream(stream)))
+    queue = _queue(stream, tensors.device)
+    return _check(lib.ea_adamw_step(C.byref(cfg), t, tensors.count, tensors.array, _ptr(gscale, B._F32), queue))
 
 
 def ea_adamw_step_scheduled(cfg, sched, t_dev, tensors, gscale=None, stream=None):
     _check_list(cfg, tensors)
+    queue = _queue(stream, tensors.device)
     return _check(lib.ea_adamw_step_scheduled(C.byref(cfg), C.byref(sched), _ptr_u32(t_dev), tensors.count,
-                                              tensors.array, _ptr(gscale, B._f32()), _stream(stream)))
+                                              tensors.array, _ptr(gscale, B._F32), queue))
 
 
 def ea_grad_norm_workspace_bytes(tensors) -> int:
@@ -219,12 +223,12 @@ def ea_grad_norm_workspace_bytes(tensors) -> int:
 
 
 def ea_grad_norm(tensors, scale, max_norm, norm, gscale, workspace, stream=None):
-    f = B._f32()
-    _here(tensors.device)
+    queue = _queue(stream, tensors.device)
+    f = B._F32
     _room(workspace, lib.ea_grad_norm_workspace_bytes(tensors.count, tensors.array))
     return _check(lib.ea_grad_norm(EA_F32 if tensors.grad_type is None else tensors.grad_type, tensors.count,
                                    tensors.array, scale, max_norm, _ptr(norm, f), _ptr(gscale, f), _ptr(workspace),
-                                   _stream(stream)))
+                                   queue))
 
 
 def _room(workspace, need):
@@ -238,7 +242,6 @@ def _rows(t, kind, rows, dim, stride, name):
     """Pointer of a [rows, dim] tensor (leading dimensions may be split) with `stride` elements between rows."""
     if t is None or isinstance(t, int):
         return t
-    _here(t.get_device() if t.is_cuda else None)
     if t.is_cuda and t.shape == (rows, dim) and t.stride() == (stride, 1) and t.dtype is _dtypes()[kind]:
         return t.data_ptr()
     if not t.is_cuda:
@@ -269,12 +272,18 @@ def _ids(t, cfg):
     return _ptr(t)
 
 
+def _device_of(*tensors):
+    """The one device of these tensors (raw pointers and None left out)."""
+    got = {t.get_device() for t in tensors if hasattr(t, "get_device") and t.is_cuda}
+    if len(got) > 1:
+        raise ValueError("the tensors are not all on one device")
+    return got.pop() if got else None
+
+
 def ea_embed_lookup(cfg, table, ids, x, stream=None):
-    B._f32()
-    return _check(lib.ea_embed_lookup(C.byref(cfg),
-                                      _rows(table, cfg.table_type, cfg.vocab, cfg.dim, cfg.table_stride, "table"),
-                                      _ids(ids, cfg), _rows(x, cfg.x_type, cfg.tokens, cfg.dim, cfg.x_stride, "x"),
-                                      _stream(stream)))
+    args = (_rows(table, cfg.table_type, cfg.vocab, cfg.dim, cfg.table_stride, "table"), _ids(ids, cfg),
+            _rows(x, cfg.x_type, cfg.tokens, cfg.dim, cfg.x_stride, "x"))
+    return _check(lib.ea_embed_lookup(C.byref(cfg), *args, _queue(stream, _device_of(table, ids, x))))
 
 
 def ea_embed_workspace_bytes(cfg) -> int:
@@ -282,9 +291,8 @@ def ea_embed_workspace_bytes(cfg) -> int:
 
 
 def ea_embed_grad(cfg, ids, dx, dtable, accumulate, workspace, stream=None):
-    B._f32()
     _room(workspace, lib.ea_embed_workspace_bytes(C.byref(cfg)))
-    return _check(lib.ea_embed_grad(C.byref(cfg), _ids(ids, cfg),
-                                    _rows(dx, cfg.x_type, cfg.tokens, cfg.dim, cfg.x_stride, "dx"),
-                                    _rows(dtable, cfg.table_type, cfg.vocab, cfg.dim, cfg.table_stride, "dtable"),
-                                    1 if accumulate else 0, _ptr(workspace), _stream(stream)))
+    args = (_ids(ids, cfg), _rows(dx, cfg.x_type, cfg.tokens, cfg.dim, cfg.x_stride, "dx"),
+            _rows(dtable, cfg.table_type, cfg.vocab, cfg.dim, cfg.table_stride, "dtable"), 1 if accumulate else 0,
+            _ptr(workspace))
+    return _check(lib.ea_embed_grad(C.byref(cfg), *args, _queue(stream, _device_of(ids, dx, dtable, workspace))))

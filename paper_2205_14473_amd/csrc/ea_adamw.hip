@@ -57,7 +57,8 @@ struct Factors {
     uint32_t t;
 };
 
-__device__ __forceinline__ Factors factors_of(const AdamwArgs& a, const TensorPart& e, float gs)
+template <class Args, class Part>
+__device__ __forceinline__ Factors factors_of(const Args& a, const Part& e, float gs)
 {
     Factors f;
     float lr = a.lr, beta2 = a.beta2;
@@ -100,7 +101,7 @@ constexpr int kAdamwBlock = 256;
 // the step of 355M parameters took 1689 and 1705 us against 1653; the caches
 // left out of loads and stores are the larger part (1834 with them, one quad).
 template <class P, class G>
-__device__ __forceinline__ void adamw32_quad(const Factors& f, const TensorPart& e, uint32_t i, int n)
+__device__ __forceinline__ void adamw32_quad(const Factors& f, const Part32& e, uint32_t i, int n)
 {
     const G* gp = (const G*)e.g + i;
     P* pp = (P*)e.p + i;
@@ -138,12 +139,12 @@ __device__ __forceinline__ void adamw32_quad(const Factors& f, const TensorPart&
 }
 
 template <class P, class G>
-__global__ void __launch_bounds__(kAdamwBlock) adamw32_kernel(AdamwArgs a)
+__global__ void __launch_bounds__(kAdamwBlock) adamw32_kernel(Adamw32Args a)
 {
     const float gs = a.gscale ? *a.gscale : 1.0f;
     if (!__builtin_isfinite(gs)) return;
-    const int at = __builtin_amdgcn_readfirstlane(part_of<kListParts>(a.first, a.count, blockIdx.x));
-    const TensorPart& e = a.part[at];
+    const int at = __builtin_amdgcn_readfirstlane(part_of<Adamw32Args::kMost>(a.first, a.count, blockIdx.x));
+    const Part32& e = a.part[at];
     const Factors f = factors_of(a, e, gs);
     const uint32_t i = ((blockIdx.x - a.first[at]) * kAdamwBlock + threadIdx.x) * 4;
     if (i < e.n) adamw32_quad<P, G>(f, e, i, e.n - i < 4 ? (int)(e.n - i) : 4);
@@ -288,14 +289,14 @@ constexpr float kLeastEps = 0x1p-100f;   // below, quotient's reciprocal could l
 
 // The codes of a quad of first moments and roots, in place of the old ones.
 template <bool DRAWS>
-__device__ __forceinline__ void store_states(const AdamwArgs& a, const Factors& f, const TensorPart& e, uint32_t at,
+__device__ __forceinline__ void store_states(const Adamw8Args& a, const Factors& f, const Part8& e, uint32_t at,
                                              uint8_t* mp, uint8_t* vp, v4f m, v4f r, float minv, float rinv, int n)
 {
     const float least = rinv > 0.0f ? 0x1p-9f : 0.0f;
     uint4 w = {0, 0, 0, 0};
     if (DRAWS) {
-        const uint64_t quad = ((uint64_t)e.piece * kPartElements + at) >> 2;
-        w = philox10(make_uint4((uint32_t)quad, (uint32_t)(quad >> 32), f.t, e.index), a.k0, a.k1);
+        const uint64_t quad = ((uint64_t)(e.place & ((1u << kPieceBits) - 1)) * kPartElements + at) >> 2;
+        w = philox10(make_uint4((uint32_t)quad, (uint32_t)(quad >> 32), f.t, e.place >> kPieceBits), a.k0, a.k1);
     }
     const uint32_t u[4] = {w.x, w.y, w.z, w.w};
     float ym[4], yr[4];
@@ -312,7 +313,7 @@ __device__ __forceinline__ void store_states(const AdamwArgs& a, const Factors& 
 // its quads j and j + 32.
 // The form for any values and any number of elements.
 template <class P, class G, bool DRAWS>
-__device__ __forceinline__ void adamw8_any(const AdamwArgs& a, const Factors& f, const TensorPart& e, uint32_t begin)
+__device__ __forceinline__ void adamw8_any(const Adamw8Args& a, const Factors& f, const Part8& e, uint32_t begin)
 {
     const int lane = lane_id(), row = lane / kRowLanes;
     const uint32_t block = begin / EA_STATE_BLOCK + row;
@@ -386,7 +387,7 @@ __device__ __forceinline__ uint32_t first_of_lane()
 }
 
 template <class P, class G, bool MASTER>
-__device__ __forceinline__ void fetch(const TensorPart& e, uint32_t begin, Held<P, G, MASTER>& h)
+__device__ __forceinline__ void fetch(const Part8& e, uint32_t begin, Held<P, G, MASTER>& h)
 {
     const int row = lane_id() / kRowLanes;
     h.ms = (e.m_scale + begin / EA_STATE_BLOCK)[row];
@@ -407,7 +408,7 @@ __device__ __forceinline__ void fetch(const TensorPart& e, uint32_t begin, Held<
 // The same for whole blocks, fetched before, and values that root_of and
 // quotient take, as nearly all are; false, with nothing written, where one is not.
 template <class P, class G, bool DRAWS, bool MASTER>
-__device__ __forceinline__ bool adamw8_whole(const AdamwArgs& a, const Factors& f, const TensorPart& e, uint32_t begin,
+__device__ __forceinline__ bool adamw8_whole(const Adamw8Args& a, const Factors& f, const Part8& e, uint32_t begin,
                                              const Held<P, G, MASTER>& h)
 {
     const uint32_t first = first_of_lane();
@@ -459,7 +460,7 @@ __device__ __forceinline__ bool adamw8_whole(const AdamwArgs& a, const Factors& 
 // A wave's run of its part: whole groups of blocks, each fetched before the
 // last one is worked on, then what is left of the part.
 template <class P, class G, bool DRAWS, bool MASTER>
-__device__ __forceinline__ void adamw8_run(const AdamwArgs& a, const Factors& f, const TensorPart& e, uint32_t begin,
+__device__ __forceinline__ void adamw8_run(const Adamw8Args& a, const Factors& f, const Part8& e, uint32_t begin,
                                            uint32_t end)
 {
     Held<P, G, MASTER> h, next;
@@ -479,12 +480,12 @@ __device__ __forceinline__ void adamw8_run(const AdamwArgs& a, const Factors& f,
 }
 
 template <class P, class G, bool DRAWS>
-__global__ void __launch_bounds__(kAdamwBlock) adamw8_kernel(AdamwArgs a)
+__global__ void __launch_bounds__(kAdamwBlock) adamw8_kernel(Adamw8Args a)
 {
     const float gs = a.gscale ? *a.gscale : 1.0f;
     if (!__builtin_isfinite(gs)) return;
-    const int at = __builtin_amdgcn_readfirstlane(part_of<kListParts>(a.first, a.count, blockIdx.x));
-    const TensorPart& e = a.part[at];
+    const int at = __builtin_amdgcn_readfirstlane(part_of<Adamw8Args::kMost>(a.first, a.count, blockIdx.x));
+    const Part8& e = a.part[at];
     const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), run = a.chunk / kWavesPerBlock;
     const uint32_t begin = ((blockIdx.x - a.first[at]) * kWavesPerBlock + wave) * run;
     if (begin >= e.n) return;
@@ -497,19 +498,23 @@ __global__ void __launch_bounds__(kAdamwBlock) adamw8_kernel(AdamwArgs a)
 }
 
 template <class P, class G>
-void start_adamw(const AdamwArgs& a, const ea_adamw_t& c, hipStream_t s)
+void start_adamw(const Adamw32Args& a, const ea_adamw_t&, hipStream_t s)
+{
+    hipLaunchKernelGGL((adamw32_kernel<P, G>), dim3(a.first[a.count]), dim3(kAdamwBlock), 0, s, a);
+}
+
+template <class P, class G>
+void start_adamw(const Adamw8Args& a, const ea_adamw_t& c, hipStream_t s)
 {
     const dim3 grid(a.first[a.count]), block(kAdamwBlock);
-    if (c.state_bits == 32)
-        hipLaunchKernelGGL((adamw32_kernel<P, G>), grid, block, 0, s, a);
-    else if (c.rounding == EA_ROUND_STOCHASTIC)
+    if (c.rounding == EA_ROUND_STOCHASTIC)
         hipLaunchKernelGGL((adamw8_kernel<P, G, true>), grid, block, 0, s, a);
     else
         hipLaunchKernelGGL((adamw8_kernel<P, G, false>), grid, block, 0, s, a);
 }
 
-template <class P>
-void start_adamw_g(const AdamwArgs& a, const ea_adamw_t& c, hipStream_t s)
+template <class P, class Args>
+void start_adamw_g(const Args& a, const ea_adamw_t& c, hipStream_t s)
 {
     if (c.grad_type == EA_F32)
         start_adamw<P, float>(a, c, s);
@@ -517,6 +522,19 @@ void start_adamw_g(const AdamwArgs& a, const ea_adamw_t& c, hipStream_t s)
         start_adamw<P, bf16>(a, c, s);
     else
         start_adamw<P, f16>(a, c, s);
+}
+
+template <class Args>
+hipError_t start_adamw_p(const Args& a, const ea_adamw_t& c, hipStream_t s)
+{
+    if (a.count < 1 || a.first[a.count] == 0) return hipSuccess;
+    if (c.param_type == EA_F32)
+        start_adamw_g<float>(a, c, s);
+    else if (c.param_type == EA_BF16)
+        start_adamw_g<bf16>(a, c, s);
+    else
+        start_adamw_g<f16>(a, c, s);
+    return hipGetLastError();
 }
 
 // ---- gradient norm -----------------------------------------------------------------
@@ -627,16 +645,14 @@ uint32_t adamw_chunk(const ea_adamw_t& c, int64_t total)
     return kWavesPerBlock * kWaveElements * (total < kShortRuns ? 1 : 4);
 }
 
-hipError_t launch_adamw(const AdamwArgs& a, const ea_adamw_t& c, hipStream_t s)
+hipError_t launch_adamw(const Adamw32Args& a, const ea_adamw_t& c, hipStream_t s)
 {
-    if (a.count < 1 || a.first[a.count] == 0) return hipSuccess;
-    if (c.param_type == EA_F32)
-        start_adamw_g<float>(a, c, s);
-    else if (c.param_type == EA_BF16)
-        start_adamw_g<bf16>(a, c, s);
-    else
-        start_adamw_g<f16>(a, c, s);
-    return hipGetLastError();
+    return start_adamw_p(a, c, s);
+}
+
+hipError_t launch_adamw(const Adamw8Args& a, const ea_adamw_t& c, hipStream_t s)
+{
+    return start_adamw_p(a, c, s);
 }
 
 int64_t norm_chunk(int64_t total)

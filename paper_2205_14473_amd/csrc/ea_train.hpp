@@ -83,29 +83,42 @@ __device__ __forceinline__ void store_some(T* p, typename Quad<T>::vec v, int n)
 // ---- AdamW ------------------------------------------------------------------
 
 // A tensor, or 2^30 consecutive elements of a larger one, as a launch sees it.
-struct TensorPart {
+struct Part32 {
     const void* g;
     void* p;
     void* m;
     void* v;
-    float* m_scale;
-    float* v_scale;
     float* master;
     uint32_t n;                            // at most 2^30
     // The factors of a step known to the host: 1 - lr_i wd and lr_i / (1 - beta1^t); of one read on the
     // device (t_dev): wd and the factor on the learning rate.
     float keep, step;
-    uint32_t index;                        // of the tensor in the call's list
-    uint32_t piece;                        // its first element is piece * 2^30
 };
+struct Part8 {
+    const void* g;
+    void* p;
+    void* m;
+    void* v;
+    float* master;
+    float* m_scale;
+    float* v_scale;
+    uint32_t n;
+    float keep, step;
+    uint32_t place;                        // tensor's index in the call's list * 2^10 + piece: the first
+                                           // element is piece * 2^30
+};
+static_assert(sizeof(Part32) == 56 && sizeof(Part8) == 72, "the tables below are sized for these");
 constexpr int64_t kPartElements = (int64_t)1 << 30;
+constexpr int kPieceBits = 10;
+constexpr int32_t kMostTensors = 1 << 22;
 
 // Parts of one launch: the table rides in the kernel's arguments, which hold
 // at most 4 KB, and a grid has fewer than 2^32 threads.
-constexpr int kListParts = 46;
 constexpr uint32_t kMostGroups = 1u << 23;
 
+template <class Part, int MOST>
 struct AdamwArgs {
+    static constexpr int kMost = MOST;
     // The step's values from the host, or (t_dev) from the device's step and the schedule.
     float lr, beta1, beta2, eps;
     float root;                            // 1 / sqrt(1 - beta2^t) (t_dev: unset)
@@ -116,10 +129,12 @@ struct AdamwArgs {
     const float* gscale;
     const uint32_t* t_dev;
     ea_schedule_t sched;
-    uint32_t first[kListParts + 1];        // first workgroup of each part
-    TensorPart part[kListParts];
+    uint32_t first[MOST + 1];              // first workgroup of each part
+    Part part[MOST];
 };
-static_assert(sizeof(AdamwArgs) <= 4096, "kernel arguments");
+using Adamw32Args = AdamwArgs<Part32, 64>;
+using Adamw8Args = AdamwArgs<Part8, 52>;
+static_assert(sizeof(Adamw32Args) <= 4096 && sizeof(Adamw8Args) <= 4096, "kernel arguments");
 
 // The step's factors, formed in binary64 and rounded once, on the host or on the device alike.
 __host__ __device__ inline double adamw_power(double b, uint32_t t)
@@ -146,7 +161,8 @@ __host__ __device__ inline float adamw_keep(double lri, float wd)
 
 // Elements per workgroup of a call of `total` elements: what `first` counts in.
 uint32_t adamw_chunk(const ea_adamw_t& c, int64_t total);
-hipError_t launch_adamw(const AdamwArgs& a, const ea_adamw_t& c, hipStream_t s);
+hipError_t launch_adamw(const Adamw32Args& a, const ea_adamw_t& c, hipStream_t s);
+hipError_t launch_adamw(const Adamw8Args& a, const ea_adamw_t& c, hipStream_t s);
 
 // ---- gradient norm ------------------------------------------------------------
 

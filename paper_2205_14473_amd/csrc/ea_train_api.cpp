@@ -32,6 +32,7 @@ constexpr int64_t kMostElements = (int64_t)1 << 40;
 int check_list(int32_t ntensors, const ea_tensor_t* tensors, int64_t* total)
 {
     if (ntensors < 0) return fail(EA_ERR_ARG, "ntensors must be >= 0 (got %d)", ntensors);
+    if (ntensors > ea::kMostTensors) return fail(EA_ERR_UNSUPPORTED, "more than 2^22 tensors in one call");
     if (ntensors > 0 && !tensors) return fail(EA_ERR_ARG, "tensors is NULL");
     *total = 0;
     for (int32_t i = 0; i < ntensors; ++i) {
@@ -97,61 +98,77 @@ T* past(T* ptr, int64_t elements, int64_t bytes)
     return ptr ? (T*)((uintptr_t)ptr + (uintptr_t)(elements * bytes)) : nullptr;
 }
 
-int adamw_impl(const char* name, const ea_adamw_t* c, const ea_schedule_t* s, int64_t t, uint32_t* t_dev,
-               int32_t ntensors, const ea_tensor_t* tensors, const float* gscale, void* stream)
+void set_scales(ea::Part32&, const ea_tensor_t&, int32_t, int64_t) {}
+
+void set_scales(ea::Part8& p, const ea_tensor_t& e, int32_t i, int64_t at)
 {
-    int64_t total = 0;
-    int rc = check_adamw(c, ntensors, tensors, gscale, &total);
-    if (rc) return rc;
-    ea::AdamwArgs a{};
-    a.lr = c->lr;
-    a.beta1 = c->beta1;
-    a.beta2 = c->beta2;
-    a.eps = c->eps;
+    p.m_scale = past(e.m_scale, at / EA_STATE_BLOCK, 4);
+    p.v_scale = past(e.v_scale, at / EA_STATE_BLOCK, 4);
+    p.place = ((uint32_t)i << ea::kPieceBits) | (uint32_t)(at / ea::kPartElements);
+}
+
+// The step over a checked list: launches of as many parts as a table holds.
+template <class Args>
+hipError_t adamw_launches(const ea_adamw_t& c, const ea_schedule_t* s, int64_t t, uint32_t* t_dev, int32_t ntensors,
+                          const ea_tensor_t* tensors, int64_t total, const float* gscale, hipStream_t st)
+{
+    Args a{};
+    a.lr = c.lr;
+    a.beta1 = c.beta1;
+    a.beta2 = c.beta2;
+    a.eps = c.eps;
     a.t = (uint32_t)t;
-    a.k0 = (uint32_t)c->seed;
-    a.k1 = (uint32_t)(c->seed >> 32);
+    a.k0 = (uint32_t)c.seed;
+    a.k1 = (uint32_t)(c.seed >> 32);
     a.gscale = gscale;
     a.t_dev = t_dev;
-    if (!t_dev) a.root = ea::adamw_root(c->beta2, a.t);
+    if (!t_dev) a.root = ea::adamw_root(c.beta2, a.t);
     if (s) a.sched = *s;
-    a.chunk = ea::adamw_chunk(*c, total);
-    const int64_t state = c->state_bits / 8;
-    const int64_t gb = (int64_t)type_bytes(c->grad_type), pb = (int64_t)type_bytes(c->param_type);
-    const hipStream_t st = (hipStream_t)stream;
+    a.chunk = ea::adamw_chunk(c, total);
+    const int64_t state = c.state_bits / 8;
+    const int64_t gb = (int64_t)type_bytes(c.grad_type), pb = (int64_t)type_bytes(c.param_type);
     hipError_t e = hipSuccess;
-    for (int32_t i = 0; i < ntensors && e == hipSuccess; ++i)
-        for (int64_t at = 0; at < tensors[i].n && e == hipSuccess; at += ea::kPartElements) {
+    for (int32_t i = 0; i < ntensors; ++i) {
+        float keep = tensors[i].weight_decay, step = tensors[i].lr_scale;
+        if (!t_dev) {
+            const double lri = (double)c.lr * (double)step;
+            keep = ea::adamw_keep(lri, tensors[i].weight_decay);
+            step = ea::adamw_step_size(lri, c.beta1, a.t);
+        }
+        for (int64_t at = 0; at < tensors[i].n; at += ea::kPartElements) {
             const int64_t left = tensors[i].n - at, n = left < ea::kPartElements ? left : ea::kPartElements;
             const uint32_t groups = (uint32_t)((n + a.chunk - 1) / a.chunk);
-            if (a.count == ea::kListParts || a.first[a.count] + groups > ea::kMostGroups) {
-                e = ea::launch_adamw(a, *c, st);
+            if (a.count == Args::kMost || a.first[a.count] + groups > ea::kMostGroups) {
+                if ((e = ea::launch_adamw(a, c, st)) != hipSuccess) return e;
                 a.count = 0;
-                if (e != hipSuccess) break;
             }
-            ea::TensorPart& p = a.part[a.count];
+            auto& p = a.part[a.count];
             p.g = past(tensors[i].g, at, gb);
             p.p = past(tensors[i].p, at, pb);
             p.m = past(tensors[i].m, at, state);
             p.v = past(tensors[i].v, at, state);
-            p.m_scale = state == 1 ? past(tensors[i].m_scale, at / EA_STATE_BLOCK, 4) : nullptr;
-            p.v_scale = state == 1 ? past(tensors[i].v_scale, at / EA_STATE_BLOCK, 4) : nullptr;
             p.master = past(tensors[i].master, at, 4);
             p.n = (uint32_t)n;
-            if (t_dev) {
-                p.keep = tensors[i].weight_decay;
-                p.step = tensors[i].lr_scale;
-            } else {
-                const double lri = (double)c->lr * (double)tensors[i].lr_scale;
-                p.keep = ea::adamw_keep(lri, tensors[i].weight_decay);
-                p.step = ea::adamw_step_size(lri, c->beta1, a.t);
-            }
-            p.index = (uint32_t)i;
-            p.piece = (uint32_t)(at / ea::kPartElements);
+            p.keep = keep;
+            p.step = step;
+            set_scales(p, tensors[i], i, at);
             a.first[a.count + 1] = a.first[a.count] + groups;
             ++a.count;
         }
-    if (e == hipSuccess) e = ea::launch_adamw(a, *c, st);
+    }
+    return ea::launch_adamw(a, c, st);
+}
+
+int adamw_impl(const char* name, const ea_adamw_t* c, const ea_schedule_t* s, int64_t t, uint32_t* t_dev,
+               int32_t ntensors, const ea_tensor_t* tensors, const float* gscale, void* stream)
+{
+    int64_t total = 0;
+    const int rc = check_adamw(c, ntensors, tensors, gscale, &total);
+    if (rc) return rc;
+    const hipStream_t st = (hipStream_t)stream;
+    hipError_t e = c->state_bits == 8
+                       ? adamw_launches<ea::Adamw8Args>(*c, s, t, t_dev, ntensors, tensors, total, gscale, st)
+                       : adamw_launches<ea::Adamw32Args>(*c, s, t, t_dev, ntensors, tensors, total, gscale, st);
     if (e == hipSuccess && t_dev) e = ea::launch_advance(t_dev, st);
     return hip_status(e, name);
 }
