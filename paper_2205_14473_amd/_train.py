@@ -6,6 +6,7 @@ tensors of the documented types, streams are torch streams, raw hipStream_t
 integers, or None for torch's current stream.
 """
 import ctypes as C
+from array import array
 
 from . import _binding as B
 from ._binding import _check, _ptr, _ptr_u32, _stream, lib
@@ -95,7 +96,8 @@ class TensorList:
         n = len(g)
         self.count = n
         self.array = (Tensor * max(n, 1))()
-        self.param_type = self.grad_type = self.state_bits = None
+        self._words = memoryview(self.array).cast("B").cast("Q")   # a field of all tensors: every 9th word
+        self.param_type = self.grad_type = self.state_bits = self._n = None
         self._p = p
         for name, ts in (("p", p), ("m", m), ("v", v), ("m_scale", m_scale), ("v_scale", v_scale),
                          ("master", master)):
@@ -103,26 +105,39 @@ class TensorList:
                 raise ValueError(f"{len(ts)} tensors in {name}, and {n} in g")
         self.set_grads(g)
         if p is not None:
-            self.param_type = self._set("p", p, g, dtype=None)
+            self.param_type, at = self._checked("p", p, g)
+            self._column("p", at)
             if master is not None:
-                self._set("master", master, p, dtype=_dtypes()[EA_F32], optional=True)
+                self._column("master", self._checked("master", master, p, _dtypes()[EA_F32], optional=True)[1])
         if (m is None) != (v is None):
             raise ValueError("m and v come together")
         if m is not None:
             self.state_bits = self._set_states(m, v, m_scale, v_scale)
-        for i in range(n):
-            self.array[i].weight_decay = weight_decay if isinstance(weight_decay, (int, float)) else weight_decay[i]
-            self.array[i].lr_scale = lr_scale if isinstance(lr_scale, (int, float)) else lr_scale[i]
+        for i, e in enumerate(self.array[:n]):
+            e.weight_decay = weight_decay if isinstance(weight_decay, (int, float)) else weight_decay[i]
+            e.lr_scale = lr_scale if isinstance(lr_scale, (int, float)) else lr_scale[i]
         self._held = (p, m, v, m_scale, v_scale, master)
         if p is not None:
-            at = [e.p for e in self.array[:n] if e.n > 0]
+            at = [t.data_ptr() for t in p if t.numel()]
             if len(set(at)) != len(at):
                 raise ValueError("a parameter is in the list twice")
 
-    def _set(self, name, ts, like, dtype, optional=False):
-        kind, array, field = None, self.array, getattr(Tensor, name)
+    def _column(self, name, values):
+        if values:
+            self._words[getattr(Tensor, name).offset // 8::C.sizeof(Tensor) // 8] = array("Q", values)
+
+    def _checked(self, name, ts, like, dtype=None, optional=False):
+        """`name`'s tensors checked against those of `like`: (their type, their addresses)."""
+        if ts and all(t is not None for t in ts) and len({t.dtype for t in ts}) == 1 and \
+                (dtype is None or ts[0].dtype is dtype) and {t.get_device() for t in ts} == {like[0].get_device()} and \
+                ts[0].is_cuda and all(t.is_contiguous() for t in ts) and \
+                (ts is like or all(t.shape == e.shape and e.is_contiguous() for t, e in zip(ts, like))):
+            return ea_type(ts[0].dtype), [t.data_ptr() for t in ts]
+        # other strides, a part of the entries, or something to refuse: one by one
+        kind, at = None, []
         for i, t in enumerate(ts):
             if t is None and optional:
+                at.append(0)
                 continue
             if dtype is not None and t.dtype is not dtype:
                 raise ValueError(f"{name}[{i}]: expected {dtype}, got {t.dtype}")
@@ -141,8 +156,8 @@ class TensorList:
                                      f"parameter's {tuple(e.shape)}, {e.stride()}")
             if not t.is_contiguous() and not _dense(t):
                 raise ValueError(f"{name}[{i}]: strides {t.stride()} leave gaps in shape {tuple(t.shape)}")
-            field.__set__(array[i], t.data_ptr())
-        return None if kind is None or dtype is not None else ea_type(kind)
+            at.append(t.data_ptr())
+        return None if kind is None else ea_type(kind), at
 
     def _set_states(self, m, v, m_scale, v_scale):
         import torch
@@ -154,34 +169,34 @@ class TensorList:
             if ts is None or (bits == 32 and name.endswith("scale")):
                 continue
             want = codes if bits == 8 and name in "mv" else (torch.float32,)
-            per, array, field = (1 if name in "mv" else EA_STATE_BLOCK), self.array, getattr(Tensor, name)
+            per = 1 if name in "mv" else EA_STATE_BLOCK
             for i, t in enumerate(ts):
-                most = (array[i].n + per - 1) // per
+                most = (self._n[i] + per - 1) // per
                 if not t.is_cuda:
                     raise ValueError("libea needs device tensors")
                 if t.dtype not in want or t.numel() != most or t.device != self._g[i].device or \
                         not (t.is_contiguous() or _dense(t)):
                     raise ValueError(f"{name}[{i}]: expected {most} dense elements of {want[0]} on the gradient's "
                                      f"device, got {t.numel()} of {t.dtype} on {t.device}")
-                field.__set__(array[i], t.data_ptr())
+            self._column(name, [t.data_ptr() for t in ts])
         return bits
 
     def set_grads(self, g):
         """Points the list at other gradients of the same shapes."""
         if len(g) != self.count:
             raise ValueError(f"{len(g)} gradients for {self.count} tensors")
-        kind = self._set("g", g, g if self._p is None else self._p, dtype=None)
+        kind, at = self._checked("g", g, g if self._p is None else self._p)
         if self.grad_type is not None and kind != self.grad_type:
             raise ValueError("the gradients' type changed")
-        for i, t in enumerate(g):
-            if self.array[i].p is not None and self.array[i].n != t.numel():
-                raise ValueError(f"g[{i}]: {t.numel()} elements, and the parameter has {self.array[i].n}")
-            self.array[i].n = t.numel()
-        self.grad_type = kind
-        self.device = g[0].get_device() if g else None
-        for t in g:
-            if t.get_device() != self.device:
-                raise ValueError("the tensors are not all on one device")
+        sizes, devices = [t.numel() for t in g], {t.get_device() for t in g}
+        if self._n is not None and sizes != self._n:
+            raise ValueError("the gradients' sizes changed")
+        if len(devices) > 1:
+            raise ValueError("the tensors are not all on one device")
+        self._n = sizes
+        self._column("n", sizes)
+        self._column("g", at)
+        self.grad_type, self.device = kind, devices.pop() if devices else None
         self._g = g
 
 
