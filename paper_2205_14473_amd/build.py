@@ -26,7 +26,7 @@ SOURCES = [os.path.join(CSRC, f) for f in ("ea_kernels.hip", "ea_half_c1.hip", "
                                             "ea_half_c8.hip", "ea_half_wide_c12.hip", "ea_half_wide_c48.hip",
                                             "ea_sym_c4.hip", "ea_sym_c8.hip", "ea_toy.hip", "ea_adamw.hip", "ea_embed.hip",
                                             "ea_api.cpp", "ea_train_api.cpp")]
-HEADERS = [os.path.join(CSRC, f) for f in ("ea_device.hpp", "ea_host.hpp", "ea_launch.hpp", "ea_round.hpp", "ea_train.hpp")] + \
+HEADERS = [os.path.join(CSRC, f) for f in ("ea_device.hpp", "ea_launch.hpp", "ea_round.hpp", "ea_train.hpp")] + \
     [os.path.join(ROOT, "include", f) for f in ("ea.h", "ea_train.h")]
 ARCH = "gfx950"
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")

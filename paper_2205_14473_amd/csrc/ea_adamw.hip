@@ -1,9 +1,12 @@
 // ea_adamw.hip -- AdamW over many tensors in one launch, with states in
 // binary32 or in blockwise-scaled E4M3, and the global gradient norm.
 //
-// Both walk a table of tensors (parts of very large ones) that rides in the kernel's arguments: workgroup
-// b belongs to the part whose range of workgroups holds b, found by one
-// vector compare of the ranges' starts.
+// Both walk a table of tensors (parts of very large ones) that rides in the
+// kernel's arguments: workgroup b belongs to the part whose range of workgroups
+// holds b, found by one vector compare of the ranges' starts.  No table is
+// uploaded and nothing is kept between calls; a list longer than the 4 KB of
+// arguments takes further launches (355M parameters in 292 tensors: five or
+// six, whose starts and ends are a twentieth of the time).
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -97,9 +100,16 @@ __device__ __forceinline__ void adamw_element(const Factors& f, float g, float& 
 
 constexpr int kAdamwBlock = 256;
 
-// One quad a thread.  With two or four a thread, loads ahead of the arithmetic,
-// the step of 355M parameters took 1689 and 1705 us against 1653; the caches
-// left out of loads and stores are the larger part (1834 with them, one quad).
+// m, v and p of one quad:
+//     m <- b1 m + (1 - b1) g;  v <- b2 v + (1 - b2) g g;  p <- keep p - step m / (root sqrt(v) + eps)
+// HBM bounds it: 28 bytes an element move once, and the arithmetic (45
+// instructions, with root and quotient rounded as IEEE 754 has them) takes half
+// of that time.  355M parameters (bfloat16 with binary32 masters) 1.65 ms, 6.0
+// TB/s; 110M (binary32, bfloat16 gradients) 473 us, 6.0; 11.7M in 62 tensors off
+// alignment 58 us, 5.6.  One quad a thread and many workgroups: with two or four
+// quads a thread, their loads ahead of the arithmetic, the first took 1.69 and
+// 1.71 ms.  Every byte is used once, so loads and stores pass the caches by
+// (1.83 ms through them).
 template <class P, class G>
 __device__ __forceinline__ void adamw32_quad(const Factors& f, const Part32& e, uint32_t i, int n)
 {
@@ -154,8 +164,8 @@ __global__ void __launch_bounds__(kAdamwBlock) adamw32_kernel(Adamw32Args a)
 
 constexpr int kRowLanes = 32;            // lanes that share a block of the 8-bit states
 
-// Largest bit pattern of a row of 16 lanes: of patterns without sign, an
-// infinity stands above every number and a NaN above that.
+// Largest bit pattern of a half wave: of patterns without sign, an infinity
+// stands above every number and a NaN above that.
 __device__ __forceinline__ uint32_t row_umax(uint32_t v)
 {
     v = max(v, dpp<kDppXor1>(v));
@@ -163,15 +173,8 @@ __device__ __forceinline__ uint32_t row_umax(uint32_t v)
     v = max(v, dpp<kDppHalfMirror>(v));
     v = max(v, dpp<kDppRowMirror>(v));
     uint32_t a, b;
-    if (kRowLanes >= 32) {
-        row_swap16(v, a, b);
-        v = max(a, b);
-    }
-    if (kRowLanes >= 64) {
-        row_swap32(v, a, b);
-        v = max(a, b);
-    }
-    return v;
+    row_swap16(v, a, b);
+    return max(a, b);
 }
 
 __device__ __forceinline__ uint32_t magnitude(float x)
@@ -196,7 +199,7 @@ __device__ __forceinline__ float block_scale(uint32_t top, float& inv)
 __device__ __forceinline__ float round_by(float y, uint32_t u)
 {
     const uint32_t up = (__float_as_uint(y) + ((u << 4) | 8u)) & ~0xFFFFFu;
-    const float low = floorf(y * 512.0f + ((float)u + 0.5f) * 0x1p-16f) * 0x1p-9f;
+    const float low = floorf(fmaf(y, 512.0f, fmaf((float)u, 0x1p-16f, 0x1p-17f))) * 0x1p-9f;   // products are exact
     return fminf(y < 0x1p-6f ? low : __uint_as_float(up), kCodeMax);
 }
 
@@ -284,7 +287,10 @@ __device__ __forceinline__ bool plain_square(float v)
     return !__builtin_amdgcn_classf(v, 0x003 | 0x004 | 0x010 | 0x080 | 0x200);
 }
 
-constexpr int64_t kShortRuns = 1 << 25;  // elements of a call below which a wave takes one group
+// Elements of a call below which a wave takes one group of blocks, above it
+// four with the next one's loads in flight (355M parameters: one 736 us, two 676,
+// four 661, eight 680; 11.7M: one 42, two 45, four 47).
+constexpr int64_t kShortRuns = 1 << 25;
 constexpr float kLeastEps = 0x1p-100f;   // below, quotient's reciprocal could leave the normal numbers
 
 // The codes of a quad of first moments and roots, in place of the old ones.
@@ -309,9 +315,22 @@ __device__ __forceinline__ void store_states(const Adamw8Args& a, const Factors&
     store_codes(vp, pack_codes(yr), n);
 }
 
-// One wave, two blocks of 256 elements: each row of 32 lanes has one, a lane
-// its quads j and j + 32.
-// The form for any values and any number of elements.
+// The step on blocks of 256 elements whose m and r = sqrt(v) are kept as E4M3
+// codes under a scale each:
+//     m = code scale, v = (code scale)^2;  the step as above;  r = sqrt(v)
+//     scale <- max|x| / 448, code <- round(x / scale)
+// A wave has two blocks, each on half of its lanes, a lane the block's quads j
+// and j + 32: the largest magnitude takes five steps without LDS, loads stay
+// side by side, and the scales' divisions serve eight elements a lane.  (With 16
+// lanes a block, and 16 elements a lane, registers halve the waves: 771 us
+// against 661 for 355M; with 64 the reduction and the divisions cost more, 739
+// against 689 before loads went ahead.)
+// 10 bytes an element (bfloat16 parameters and gradients) against 180
+// instructions for 256 elements: vector issue is busy two thirds of the time
+// beside HBM at 5.4 TB/s, 355M parameters 656 us.  With stochastic rounding the
+// draws double the instructions: 11.7M 44 us, 4.3 TB/s (16 bytes an element).
+//
+// This is the form for any values and any number of elements.
 template <class P, class G, bool DRAWS>
 __device__ __forceinline__ void adamw8_any(const Adamw8Args& a, const Factors& f, const Part8& e, uint32_t begin)
 {
@@ -555,6 +574,11 @@ __device__ __forceinline__ double block_sum(double v)
     return r;
 }
 
+// sum of g^2 in binary64: binary32 squares overflow above 1.8e19 and vanish under
+// 1e-23, and the wider sum is free beside HBM.  Chunks' sums are joined by a
+// second launch, in an order that the list alone fixes.  355M bfloat16 gradients
+// 112 us, 6.3 TB/s, with 8192 chunks (4096: 124; loads through the caches: 138).
+//
 // Squares of n elements summed over the workgroup's threads, in 16-byte loads,
 // up to eight in flight a thread.
 template <class G, int THREADS>

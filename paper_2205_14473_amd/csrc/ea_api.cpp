@@ -9,15 +9,7 @@
 #include <cstring>
 #include <mutex>
 
-#include "ea_host.hpp"
 #include "ea_launch.hpp"
-
-using ea::fail;
-using ea::ok;
-using ea::hip_status;
-using ea::check_schedule;
-using ea::check_t;
-using ea::PtrCheck;
 
 namespace {
 
@@ -36,10 +28,6 @@ void* g_scratch[kMaxDevices] = {nullptr};
 
 thread_local char g_err[512] = "";
 
-}  // namespace
-
-namespace ea {
-
 int fail(int code, const char* fmt, ...)
 {
     va_list ap;
@@ -54,48 +42,6 @@ int ok()
     g_err[0] = '\0';
     return EA_OK;
 }
-
-int check_t(int64_t t)
-{
-    if (t < 1 || t > (int64_t)0xFFFFFFFFLL) return fail(EA_ERR_ARG, "t must be in [1, 2^32-1] (got %lld)", (long long)t);
-    return EA_OK;
-}
-
-// Schedules (declared with their definition in ea.h).
-int check_schedule(const ea_schedule_t* s)
-{
-    if (!s) return fail(EA_ERR_ARG, "schedule is NULL");
-    switch (s->kind) {
-    case EA_SCHED_CONSTANT:
-        return EA_OK;
-    case EA_SCHED_ASSUMPTION2:
-        if (s->T < 1 || s->T >= ((int64_t)1 << 24))
-            return fail(EA_ERR_ARG, "schedule horizon T must be in [1, 2^24) (got %lld)", (long long)s->T);
-        if (!(s->theta > 0.0f) || !(s->theta <= (float)s->T))
-            return fail(EA_ERR_ARG, "schedule theta must be in (0, T] (got %g)", (double)s->theta);
-        break;
-    case EA_SCHED_STEP_DECAY:
-        if (s->period < 1) return fail(EA_ERR_ARG, "schedule period must be >= 1 (got %lld)", (long long)s->period);
-        if (!(s->factor > 0.0f) || !(s->factor <= 1.0f))
-            return fail(EA_ERR_ARG, "schedule factor must be in (0, 1] (got %g)", (double)s->factor);
-        break;
-    default:
-        return fail(EA_ERR_ARG, "unknown schedule kind %d", s->kind);
-    }
-    if (!std::isfinite(s->alpha) || s->alpha < 0.0f)
-        return fail(EA_ERR_ARG, "schedule alpha must be finite and >= 0 (got %g)", (double)s->alpha);
-    return EA_OK;
-}
-
-int hip_status(hipError_t e, const char* what)
-{
-    if (e != hipSuccess) return fail(EA_ERR_HIP, "%s: %s", what, hipGetErrorString(e));
-    return ok();
-}
-
-}  // namespace ea
-
-namespace {
 
 bool kind_has_scales(int32_t kind)
 {
@@ -271,6 +217,11 @@ int make_plan(const ea_config_t* c, Plan* p)
     return EA_OK;
 }
 
+bool aligned(const void* ptr, uintptr_t a)
+{
+    return ((uintptr_t)ptr % a) == 0;
+}
+
 // Fills the common part of the kernel argument block.
 ea::StepArgs base_args(const ea_config_t* c, const Plan& p, int64_t t)
 {
@@ -288,6 +239,38 @@ ea::StepArgs base_args(const ea_config_t* c, const Plan& p, int64_t t)
     a.qw = p.qw;
     a.qs = p.qs;
     return a;
+}
+
+int check_t(int64_t t)
+{
+    if (t < 1 || t > (int64_t)0xFFFFFFFFLL) return fail(EA_ERR_ARG, "t must be in [1, 2^32-1] (got %lld)", (long long)t);
+    return EA_OK;
+}
+
+// Schedules (declared with their definition in ea.h).
+int check_schedule(const ea_schedule_t* s)
+{
+    if (!s) return fail(EA_ERR_ARG, "schedule is NULL");
+    switch (s->kind) {
+    case EA_SCHED_CONSTANT:
+        return EA_OK;
+    case EA_SCHED_ASSUMPTION2:
+        if (s->T < 1 || s->T >= ((int64_t)1 << 24))
+            return fail(EA_ERR_ARG, "schedule horizon T must be in [1, 2^24) (got %lld)", (long long)s->T);
+        if (!(s->theta > 0.0f) || !(s->theta <= (float)s->T))
+            return fail(EA_ERR_ARG, "schedule theta must be in (0, T] (got %g)", (double)s->theta);
+        break;
+    case EA_SCHED_STEP_DECAY:
+        if (s->period < 1) return fail(EA_ERR_ARG, "schedule period must be >= 1 (got %lld)", (long long)s->period);
+        if (!(s->factor > 0.0f) || !(s->factor <= 1.0f))
+            return fail(EA_ERR_ARG, "schedule factor must be in (0, 1] (got %g)", (double)s->factor);
+        break;
+    default:
+        return fail(EA_ERR_ARG, "unknown schedule kind %d", s->kind);
+    }
+    if (!std::isfinite(s->alpha) || s->alpha < 0.0f)
+        return fail(EA_ERR_ARG, "schedule alpha must be finite and >= 0 (got %g)", (double)s->alpha);
+    return EA_OK;
 }
 
 // lr_t, beta2_t of a validated schedule at step t >= 1, in binary32.
@@ -309,6 +292,25 @@ void schedule_values(const ea_schedule_t* s, float lr0, float beta2_0, int64_t t
         *lr = s->alpha * r;
     }
 }
+
+int hip_status(hipError_t e, const char* what)
+{
+    if (e != hipSuccess) return fail(EA_ERR_HIP, "%s: %s", what, hipGetErrorString(e));
+    return ok();
+}
+
+struct PtrCheck {
+    int rc = EA_OK;
+    void need(const void* ptr, bool required, uintptr_t align, const char* name)
+    {
+        if (rc) return;
+        if (!ptr) {
+            if (required) rc = fail(EA_ERR_ARG, "%s is NULL", name);
+            return;
+        }
+        if (!aligned(ptr, align)) rc = fail(EA_ERR_ALIGN, "%s is not %u-byte aligned", name, (unsigned)align);
+    }
+};
 
 // One fused round.  With t_dev the step is read on the device, lr and beta2
 // come from the schedule at that step, and t_dev is advanced afterwards.

@@ -4,17 +4,52 @@
 #include "ea_train.h"
 
 #include <cmath>
+#include <cstdarg>
+#include <cstdio>
 
-#include "ea_host.hpp"
 #include "ea_train.hpp"
 
-using ea::PtrCheck;
-using ea::check_schedule;
-using ea::check_t;
-using ea::fail;
-using ea::hip_status;
-
 namespace {
+
+// Errors share the round's text: ea_last_error() gives the calling thread's
+// buffer (512 bytes, not const where it is defined), of which these calls write
+// the first half at most.
+constexpr size_t kErrorBytes = 256;
+
+__attribute__((format(printf, 2, 3))) int fail(int code, const char* fmt, ...)
+{
+    va_list ap;
+    va_start(ap, fmt);
+    vsnprintf(const_cast<char*>(ea_last_error()), kErrorBytes, fmt, ap);
+    va_end(ap);
+    return code;
+}
+
+int hip_status(hipError_t e, const char* what)
+{
+    if (e != hipSuccess) return fail(EA_ERR_HIP, "%s: %s", what, hipGetErrorString(e));
+    const_cast<char*>(ea_last_error())[0] = '\0';
+    return EA_OK;
+}
+
+int check_t(int64_t t)
+{
+    if (t < 1 || t > (int64_t)0xFFFFFFFFLL) return fail(EA_ERR_ARG, "t must be in [1, 2^32-1] (got %lld)", (long long)t);
+    return EA_OK;
+}
+
+struct PtrCheck {
+    int rc = EA_OK;
+    void need(const void* ptr, bool required, uintptr_t align, const char* name)
+    {
+        if (rc) return;
+        if (!ptr) {
+            if (required) rc = fail(EA_ERR_ARG, "%s is NULL", name);
+            return;
+        }
+        if ((uintptr_t)ptr % align) rc = fail(EA_ERR_ALIGN, "%s is not %u-byte aligned", name, (unsigned)align);
+    }
+};
 
 bool known_type(int32_t type)
 {
@@ -217,10 +252,12 @@ int ea_adamw_step(const ea_adamw_t* c, int64_t t, int32_t ntensors, const ea_ten
 int ea_adamw_step_scheduled(const ea_adamw_t* c, const ea_schedule_t* s, uint32_t* t_dev, int32_t ntensors,
                             const ea_tensor_t* tensors, const float* gscale, void* stream)
 {
-    const int rc = check_schedule(s);
+    // the schedule's own checks, and its beta2 (the same at every step)
+    ea_config_t at{};
+    float lr = 0.0f, beta2 = 0.0f;
+    const int rc = ea_schedule_at(&at, s, 1, &lr, &beta2);
     if (rc) return rc;
-    if (s->kind == EA_SCHED_ASSUMPTION2 && !(1.0f - s->theta / (float)s->T < 1.0f))
-        return fail(EA_ERR_ARG, "schedule theta / T is too small: beta2 rounds to 1");
+    if (!(beta2 < 1.0f)) return fail(EA_ERR_ARG, "schedule theta / T is too small: beta2 rounds to 1");
     if (!t_dev || ((uintptr_t)t_dev & 3u)) return fail(EA_ERR_ALIGN, "t_dev must be a 4-byte aligned device pointer");
     return adamw_impl("ea_adamw_step_scheduled", c, s, 1, t_dev, ntensors, tensors, gscale, stream);
 }

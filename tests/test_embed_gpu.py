@@ -244,3 +244,29 @@ def test_rows_past_32_bit_offsets():
     x = torch.empty((4, dim), dtype=torch.bfloat16, device="cuda")
     E.ea_embed_lookup(c, t, ids, x)
     assert torch.equal(x, t[ids])
+
+
+def test_batched_ids_and_rows_and_tensors_that_do_not_fit():
+    ids = torch.randint(0, 50, (4, 6), device="cuda")
+    table = torch.randn(50, 10, device="cuda")
+    x, flat = torch.empty((4, 6, 10), device="cuda"), torch.empty((24, 10), device="cuda")
+    c = config(24, 50, 10, torch.float32, torch.float32, 0.5)
+    E.ea_embed_lookup(c, table, ids, x)
+    E.ea_embed_lookup(c, table, ids.view(-1), flat)
+    assert torch.equal(x.view(24, 10), flat) and torch.equal(flat, table[ids.view(-1)] * 0.5)
+    ws = torch.empty(E.ea_embed_workspace_bytes(c), dtype=torch.uint8, device="cuda")
+    d = torch.zeros_like(table)
+    for bad, text in (((table.double(), ids, x), "float32, bfloat16 or float16"), ((table.half(), ids, x), "type"),
+                      ((table[:49], ids, x), "rows"), ((table, ids.int(), x), "64-bit"), ((table, ids[:3], x), "24"),
+                      ((table, ids.t(), x), "contiguous"), ((table, ids, x[:, :, :9]), "rows"),
+                      ((table.t().contiguous().t(), ids, x), "strides|next to"), ((table, ids, x.cpu()), "device"),
+                      ((table, ids, x.transpose(0, 1)), "strides")):
+        with pytest.raises(ValueError, match=text):
+            E.ea_embed_lookup(c, *bad)
+        with pytest.raises(ValueError, match=text):
+            E.ea_embed_grad(c, bad[1], bad[2], bad[0], False, ws)
+    with pytest.raises(ValueError, match="workspace"):
+        E.ea_embed_grad(c, ids, x, d, False, ws[:-1])
+    with pytest.raises(E.EAError, match="workspace"):
+        E.ea_embed_grad(c, ids, x, d, False, None)
+    assert not d.any()
