@@ -29,8 +29,9 @@ class Problem:
     """Tensors of the given sizes in one allocation per array, each `shift` elements off the last one's end."""
 
     def __init__(self, sizes, param=torch.float32, grad=torch.float32, bits=32, master=False, shift=0, seed=1,
-                 t=7, **list_args):
+                 t=7, between=77, **list_args):
         rng = np.random.default_rng(seed)
+        self.between = between                      # what stands between the tensors
         self.sizes, self.t, self.bits = sizes, t, bits
         self.p0, self.g0, self.m0, self.v0 = [], [], [], []
         for n in sizes:
@@ -57,7 +58,8 @@ class Problem:
 
     def _lay(self, ts, shift):
         total = sum(t.numel() + shift for t in ts) + shift
-        flat = torch.full((total,), 77, dtype=ts[0].dtype, device="cuda")
+        fill = self.between if ts[0].dtype is not torch.uint8 or self.between == self.between else 0x7F
+        flat = torch.full((total,), fill, dtype=ts[0].dtype, device="cuda")
         out, at = [], shift
         for t in ts:
             out.append(flat[at:at + t.numel()])
@@ -400,3 +402,15 @@ def test_parts_of_very_large_tensors():
         R.within(p[a:a + 768], torch.from_numpy(want).double(), torch.full((768,), 1e-9).double(), f"p at {a}",
                  extra=R.U16[torch.bfloat16])
     assert not p[4096:4096 + 100].any()
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_what_stands_beside_the_tensors_is_not_read(bits):
+    """NaN (and NaN codes) around every array change no bit of the results."""
+    outs = []
+    for between in (77, float("nan")):
+        P = Problem(SIZES, TYPES["bf16"], TYPES["f16"], bits=bits, master=True, shift=3, between=between)
+        E.ea_adamw_step(config(TYPES["bf16"], TYPES["f16"], bits), P.t, P.list)
+        outs.append([v.clone() for _, views in P.flats for v in views])
+    for x, y in zip(*outs):
+        assert torch.equal(x.view(torch.uint8), y.view(torch.uint8))

@@ -1,5 +1,7 @@
 """Embedding lookup and its gradient against 64 bits: types, odd widths, row gaps, ids outside the
 table, padding, one token for all, more tokens than rows and the reverse, accumulation, order of sums."""
+import sys
+
 import numpy as np
 import pytest
 
@@ -270,3 +272,24 @@ def test_batched_ids_and_rows_and_tensors_that_do_not_fit():
     with pytest.raises(E.EAError, match="workspace"):
         E.ea_embed_grad(c, ids, x, d, False, None)
     assert not d.any()
+
+
+def test_what_stands_beside_the_rows_is_not_read(monkeypatch):
+    """NaN between and around rows change no bit of a lookup or a gradient."""
+    n, vocab, dim = 300, 40, 67
+    ids = make_ids(n, vocab, "outside")
+    gen = torch.Generator().manual_seed(2)
+    dx, base = torch.randn((n, dim), generator=gen), torch.randn((vocab, dim), generator=gen)
+    outs = []
+    for beside in (55.0, float("nan")):
+        monkeypatch.setattr(sys.modules[__name__], "GAP", beside)
+        _, d = rows(n, dim, 5, torch.float32, dx, 3)
+        _, t = rows(vocab, dim, 2, torch.float32, base, 1)
+        _, x = rows(n, dim, 1, torch.float32, shift=1)
+        c = config(n, vocab, dim, torch.float32, torch.float32, 1.0, 7, tgap=2, xgap=1)
+        E.ea_embed_lookup(c, t, ids.cuda(), x)
+        c.x_stride = dim + 5
+        ws = torch.empty(E.ea_embed_workspace_bytes(c), dtype=torch.uint8, device="cuda").fill_(0xFF)
+        E.ea_embed_grad(c, ids.cuda(), d, t, True, ws)
+        outs.append((x.clone(), t.clone()))
+    assert torch.equal(outs[0][0], outs[1][0]) and torch.equal(outs[0][1], outs[1][1])

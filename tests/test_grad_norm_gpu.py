@@ -113,3 +113,16 @@ def test_norm_and_step_in_a_graph():
         torch.cuda.synchronize()
         assert torch.equal(p, q) and all(torch.equal(x, y) for x, y in zip(la.states, lb.states)), f"step {t}"
     assert torch.isfinite(p).all()
+
+
+def test_what_stands_beside_the_gradients_is_not_read():
+    for sizes in ([1, 5, 300], [70_001, 9]):
+        flat = torch.full((sum(sizes) + 8,), float("nan"), device="cuda")
+        grads, at = [], 3
+        for n in sizes:
+            grads.append(flat[at:at + n])
+            at += n + 1
+        for g in grads:
+            g.fill_(0.5)
+        norm, _ = norm_of(grads)
+        assert abs(norm - want(grads)) <= 2.0 ** -23 * norm
