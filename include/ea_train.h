@@ -83,6 +83,8 @@ typedef struct ea_adamw {
  * Both are widened, stepped and used for p in binary32, and rounded only to be
  * kept: scale = max|x| * (1/448) over the block, code = x * (1/scale) rounded to E4M3.
  *   - A block whose scale falls under 2^-126 is kept as zeros.
+ *   - Second moments are binary32 between reading and keeping them: roots
+ *     under 2^-63 square to subnormal numbers and lose digits, then vanish.
  *   - A positive root never gets the code 0 (it would leave m / eps): the
  *     smallest code, 2^-9 of the scale, takes its place.
  *   - An infinity or NaN in a block makes the block's scale NaN: it shows.
@@ -156,7 +158,9 @@ int64_t ea_embed_workspace_bytes(const ea_embed_t *c);
  * tokens with zeros; with it rows without tokens are not touched.
  *   ids (device, tokens), dx (device, tokens rows), dtable (device, vocab rows,
  *   write or read/write), workspace (device, ea_embed_workspace_bytes bytes,
- *   16-byte aligned; NULL when that is 0). */
+ *   16-byte aligned; NULL when that is 0; its contents do not matter).  The
+ *   arrays may not overlap, and calls that share a workspace are ordered by the
+ *   caller. */
 int ea_embed_grad(const ea_embed_t *c, const void *ids, const void *dx, void *dtable, int32_t accumulate,
                   void *workspace, void *stream);
 

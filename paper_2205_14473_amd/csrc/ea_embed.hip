@@ -4,9 +4,9 @@
 // The gradient sorts the ids stably (least significant digits first), cuts the
 // sorted order into chunks of equal length and sums each run of equal ids
 // inside a chunk; a run that crosses a chunk's end leaves one partial row per
-// chunk, joined in order by a second kernel.  The cut depends on the number
-// of tokens alone, so the order of every sum is fixed by the ids, and a
-// token that takes a tenth of the batch costs no more than the others.
+// chunk, joined in order by a second kernel.  The cut depends on the numbers of
+// tokens and columns alone, so the order of every sum is fixed by the ids, and
+// a token that takes a tenth of the batch costs no more than the others.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
