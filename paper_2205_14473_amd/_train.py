@@ -81,6 +81,11 @@ def _dense(t) -> bool:
     return True
 
 
+def _is_tensor(name, i, t):
+    if not hasattr(t, "data_ptr"):
+        raise ValueError(f"{name}[{i}]: expected a tensor, got {type(t).__name__}")
+
+
 class TensorList:
     """The tensors of an AdamW step or a gradient norm: an ea_tensor_t array and references to what it points
     to.  A program makes it once and passes it every step; ``set_grads`` replaces the gradients.
@@ -128,7 +133,7 @@ class TensorList:
 
     def _checked(self, name, ts, like, dtype=None, optional=False):
         """`name`'s tensors checked against those of `like`: (their type, their addresses)."""
-        if ts and all(t is not None for t in ts) and len({t.dtype for t in ts}) == 1 and \
+        if ts and all(hasattr(t, "data_ptr") for t in ts) and len({t.dtype for t in ts}) == 1 and \
                 (dtype is None or ts[0].dtype is dtype) and {t.get_device() for t in ts} == {like[0].get_device()} and \
                 ts[0].is_cuda and all(t.is_contiguous() for t in ts) and \
                 (ts is like or all(t.shape == e.shape and e.is_contiguous() for t, e in zip(ts, like))):
@@ -139,6 +144,7 @@ class TensorList:
             if t is None and optional:
                 at.append(0)
                 continue
+            _is_tensor(name, i, t)
             if dtype is not None and t.dtype is not dtype:
                 raise ValueError(f"{name}[{i}]: expected {dtype}, got {t.dtype}")
             if kind is None:
@@ -162,7 +168,7 @@ class TensorList:
     def _set_states(self, m, v, m_scale, v_scale):
         import torch
         codes = (torch.float8_e4m3fn, torch.uint8)
-        bits = 8 if self.count and m[0].dtype in codes else 32
+        bits = 8 if self.count and getattr(m[0], "dtype", None) in codes else 32
         if bits == 8 and (m_scale is None or v_scale is None):
             raise ValueError("8-bit states come with m_scale and v_scale")
         for name, ts in (("m", m), ("v", v), ("m_scale", m_scale), ("v_scale", v_scale)):
@@ -172,6 +178,7 @@ class TensorList:
             per = 1 if name in "mv" else EA_STATE_BLOCK
             for i, t in enumerate(ts):
                 most = (self._n[i] + per - 1) // per
+                _is_tensor(name, i, t)
                 if not t.is_cuda:
                     raise ValueError("libea needs device tensors")
                 if t.dtype not in want or t.numel() != most or t.device != self._g[i].device or \

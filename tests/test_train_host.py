@@ -204,5 +204,10 @@ def test_host_tensors_are_refused(E):
         E.TensorList([t])
     with pytest.raises(ValueError, match="device tensors"):
         E.ea_embed_lookup(embed(E), torch.zeros(7, 6), torch.zeros(10, dtype=torch.int64), torch.zeros(10, 6), 0)
+    for bad in (None, 3):
+        with pytest.raises(ValueError, match=r"g\[1\]: expected a tensor|device tensors"):
+            E.TensorList([t, bad])
+        with pytest.raises(ValueError, match=r"g\[0\]: expected a tensor"):
+            E.TensorList([bad, t])
     with pytest.raises(ValueError, match="2 tensors in p, and 1 in g"):
         E.TensorList([t], p=[t, t])
