@@ -51,13 +51,20 @@ for _name, _res, _args in (
     getattr(lib, _name).restype, getattr(lib, _name).argtypes = _res, _args
 
 
-_types = None        # torch's dtypes by EA_F32, EA_BF16, EA_F16; looked up on first use
+# torch's dtypes by EA_F32, EA_BF16, EA_F16, its integer dtypes by bits, and the current device's number;
+# looked up on first use.  A small call takes the GPU 2 to 3 us and a launch the host 3.5, so what a call checks
+# is kept short (from Python, AdamW on four tensors 6.2 -> 5.9 us a call, a lookup 7.0 -> 6.0).
+_types = _ids_types = _current = None
 
 
 def _dtypes():
-    global _types
+    global _types, _ids_types, _current
     if _types is None:
         import torch
+        if B._torch is None:
+            B._load_torch()
+        _ids_types = {32: torch.int32, 64: torch.int64}
+        _current = getattr(torch._C, "_cuda_getDevice", None) or B._device
         _types = (torch.float32, torch.bfloat16, torch.float16)
     return _types
 
@@ -101,6 +108,7 @@ class TensorList:
         n = len(g)
         self.count = n
         self.array = (Tensor * max(n, 1))()
+        self.address = C.addressof(self.array)
         self._words = memoryview(self.array).cast("B").cast("Q")   # a field of all tensors: every 9th word
         self.param_type = self.grad_type = self.state_bits = self._n = None
         self._p = p
@@ -121,6 +129,8 @@ class TensorList:
         for i, e in enumerate(self.array[:n]):
             e.weight_decay = weight_decay if isinstance(weight_decay, (int, float)) else weight_decay[i]
             e.lr_scale = lr_scale if isinstance(lr_scale, (int, float)) else lr_scale[i]
+        self.kinds = (self.param_type, self.grad_type, self.state_bits)
+        self.norm_bytes = _check(lib.ea_grad_norm_workspace_bytes(n, self.address))
         self._held = (p, m, v, m_scale, v_scale, master)
         if p is not None:
             at = [t.data_ptr() for t in p if t.numel()]
@@ -209,48 +219,48 @@ class TensorList:
 
 def _queue(stream, device):
     """The raw stream of a call on tensors of `device`, which has to be the current one."""
-    if B._torch is None:
-        B._load_torch()
-    here = B._device()
+    if _types is None:
+        _dtypes()
+    here = _current() if device is not None else B._device()
     if device != here and device is not None:
         raise ValueError(f"the tensors are on device {device}, and the current device is {here}")
     return B._raw_stream(here) if stream is None and B._raw_stream else _stream(stream)
 
 
 def _check_list(cfg, tensors):
-    if tensors.count and (tensors.state_bits != cfg.state_bits or tensors.param_type != cfg.param_type or
-                          tensors.grad_type != cfg.grad_type):
-        if tensors.param_type is None or tensors.state_bits is None:
-            raise ValueError("a step needs p, m and v")
-        raise ValueError(f"the tensors' types (param {tensors.param_type}, grad {tensors.grad_type}, states "
-                         f"{tensors.state_bits} bits) are not the configuration's ({cfg.param_type}, "
-                         f"{cfg.grad_type}, {cfg.state_bits} bits)")
+    if tensors.param_type is None or tensors.state_bits is None:
+        raise ValueError("a step needs p, m and v")
+    raise ValueError(f"the tensors' types (param {tensors.param_type}, grad {tensors.grad_type}, states "
+                     f"{tensors.state_bits} bits) are not the configuration's ({cfg.param_type}, "
+                     f"{cfg.grad_type}, {cfg.state_bits} bits)")
 
 
 def ea_adamw_step(cfg, t, tensors, gscale=None, stream=None):
-    _check_list(cfg, tensors)
+    if tensors.kinds != (cfg.param_type, cfg.grad_type, cfg.state_bits) and tensors.count:
+        _check_list(cfg, tensors)
     queue = _queue(stream, tensors.device)
-    return _check(lib.ea_adamw_step(C.byref(cfg), t, tensors.count, tensors.array, _ptr(gscale, B._F32), queue))
+    return _check(lib.ea_adamw_step(C.byref(cfg), t, tensors.count, tensors.address,
+                                    None if gscale is None else _ptr(gscale, B._F32), queue))
 
 
 def ea_adamw_step_scheduled(cfg, sched, t_dev, tensors, gscale=None, stream=None):
-    _check_list(cfg, tensors)
+    if tensors.kinds != (cfg.param_type, cfg.grad_type, cfg.state_bits) and tensors.count:
+        _check_list(cfg, tensors)
     queue = _queue(stream, tensors.device)
     return _check(lib.ea_adamw_step_scheduled(C.byref(cfg), C.byref(sched), _ptr_u32(t_dev), tensors.count,
-                                              tensors.array, _ptr(gscale, B._F32), queue))
+                                              tensors.address, _ptr(gscale, B._F32), queue))
 
 
 def ea_grad_norm_workspace_bytes(tensors) -> int:
-    return _check(lib.ea_grad_norm_workspace_bytes(tensors.count, tensors.array))
+    return _check(lib.ea_grad_norm_workspace_bytes(tensors.count, tensors.address))
 
 
 def ea_grad_norm(tensors, scale, max_norm, norm, gscale, workspace, stream=None):
     queue = _queue(stream, tensors.device)
     f = B._F32
-    _room(workspace, lib.ea_grad_norm_workspace_bytes(tensors.count, tensors.array))
-    return _check(lib.ea_grad_norm(EA_F32 if tensors.grad_type is None else tensors.grad_type, tensors.count,
-                                   tensors.array, scale, max_norm, _ptr(norm, f), _ptr(gscale, f), _ptr(workspace),
-                                   queue))
+    _room(workspace, tensors.norm_bytes)
+    return _check(lib.ea_grad_norm(tensors.grad_type or EA_F32, tensors.count, tensors.address, scale, max_norm,
+                                   _ptr(norm, f), _ptr(gscale, f), _ptr(workspace), queue))
 
 
 def _room(workspace, need):
@@ -264,8 +274,6 @@ def _rows(t, kind, rows, dim, stride, name):
     """Pointer of a [rows, dim] tensor (leading dimensions may be split) with `stride` elements between rows."""
     if t is None or isinstance(t, int):
         return t
-    if t.is_cuda and t.shape == (rows, dim) and t.stride() == (stride, 1) and t.dtype is _dtypes()[kind]:
-        return t.data_ptr()
     if not t.is_cuda:
         raise ValueError("libea needs device tensors")
     if ea_type(t.dtype) != kind:
@@ -302,7 +310,23 @@ def _device_of(*tensors):
     return got.pop() if got else None
 
 
+def _fits(cfg, table, ids, x):
+    """Whether three tensors are what the configuration says, the plain way; anything else is looked at in turn."""
+    try:
+        dim, device, types = cfg.dim, table.get_device(), _types or _dtypes()
+        return device >= 0 and x.get_device() == device and ids.get_device() == device and \
+            table.dtype is types[cfg.table_type] and x.dtype is types[cfg.x_type] and \
+            ids.dtype is _ids_types[cfg.index_bits] and ids.is_contiguous() and ids.numel() == cfg.tokens and \
+            table.shape == (cfg.vocab, dim) and table.stride() == (cfg.table_stride, 1) and \
+            x.shape == (cfg.tokens, dim) and x.stride() == (cfg.x_stride, 1)
+    except (AttributeError, IndexError, KeyError):
+        return False
+
+
 def ea_embed_lookup(cfg, table, ids, x, stream=None):
+    if _fits(cfg, table, ids, x):
+        return _check(lib.ea_embed_lookup(C.byref(cfg), table.data_ptr(), ids.data_ptr(), x.data_ptr(),
+                                          _queue(stream, table.get_device())))
     args = (_rows(table, cfg.table_type, cfg.vocab, cfg.dim, cfg.table_stride, "table"), _ids(ids, cfg),
             _rows(x, cfg.x_type, cfg.tokens, cfg.dim, cfg.x_stride, "x"))
     return _check(lib.ea_embed_lookup(C.byref(cfg), *args, _queue(stream, _device_of(table, ids, x))))
@@ -314,6 +338,9 @@ def ea_embed_workspace_bytes(cfg) -> int:
 
 def ea_embed_grad(cfg, ids, dx, dtable, accumulate, workspace, stream=None):
     _room(workspace, lib.ea_embed_workspace_bytes(C.byref(cfg)))
+    if _fits(cfg, dtable, ids, dx) and (workspace is None or workspace.get_device() == dx.get_device()):
+        return _check(lib.ea_embed_grad(C.byref(cfg), ids.data_ptr(), dx.data_ptr(), dtable.data_ptr(),
+                                        1 if accumulate else 0, _ptr(workspace), _queue(stream, dx.get_device())))
     args = (_ids(ids, cfg), _rows(dx, cfg.x_type, cfg.tokens, cfg.dim, cfg.x_stride, "dx"),
             _rows(dtable, cfg.table_type, cfg.vocab, cfg.dim, cfg.table_stride, "dtable"), 1 if accumulate else 0,
             _ptr(workspace))
