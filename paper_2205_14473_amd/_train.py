@@ -95,7 +95,8 @@ def _is_tensor(name, i, t):
 
 class TensorList:
     """The tensors of an AdamW step or a gradient norm: an ea_tensor_t array and references to what it points
-    to.  A program makes it once and passes it every step; ``set_grads`` replaces the gradients.
+    to.  A program makes it once and passes it every step; ``set_grads`` replaces the gradients.  It stands for
+    the memory that the tensors had when it was made: one whose storage is replaced (``t.data = ...``) needs a new list.
 
     g, p, m, v, m_scale, v_scale, master: lists of device tensors, one per parameter (all but g may be None;
     entries of master too).  g, p and master of a parameter share its shape and strides and are dense; m and v
@@ -111,7 +112,7 @@ class TensorList:
         self.address = C.addressof(self.array)
         self._words = memoryview(self.array).cast("B").cast("Q")   # a field of all tensors: every 9th word
         self.param_type = self.grad_type = self.state_bits = self._n = None
-        self._p = p
+        self._p = None if p is None else tuple(p)
         for name, ts in (("p", p), ("m", m), ("v", v), ("m_scale", m_scale), ("v_scale", v_scale),
                          ("master", master)):
             if ts is not None and len(ts) != n:
@@ -131,7 +132,9 @@ class TensorList:
             e.lr_scale = lr_scale if isinstance(lr_scale, (int, float)) else lr_scale[i]
         self.kinds = (self.param_type, self.grad_type, self.state_bits)
         self.norm_bytes = _check(lib.ea_grad_norm_workspace_bytes(n, self.address))
-        self._held = (p, m, v, m_scale, v_scale, master)
+        # the memory stays, whatever becomes of the caller's lists and tensors
+        self._held = [t.untyped_storage() for ts in (p, m, v, m_scale, v_scale, master) if ts is not None
+                      for t in ts if t is not None]
         if p is not None:
             at = [t.data_ptr() for t in p if t.numel()]
             if len(set(at)) != len(at):
@@ -214,7 +217,7 @@ class TensorList:
         self._column("n", sizes)
         self._column("g", at)
         self.grad_type, self.device = kind, devices.pop() if devices else None
-        self._g = g
+        self._g = tuple(g)
 
 
 def _queue(stream, device):

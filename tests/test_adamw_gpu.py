@@ -414,3 +414,18 @@ def test_what_stands_beside_the_tensors_is_not_read(bits):
         outs.append([v.clone() for _, views in P.flats for v in views])
     for x, y in zip(*outs):
         assert torch.equal(x.view(torch.uint8), y.view(torch.uint8))
+
+
+def test_the_list_outlives_what_it_was_made_from():
+    """The caller's lists and tensors may go: the memory stays, and no other tensor takes its place."""
+    ps, gs = [torch.ones(5000, device="cuda") for _ in range(3)], [torch.ones(5000, device="cuda") for _ in range(3)]
+    ms, vs = ([torch.zeros(5000, device="cuda") for _ in range(3)] for _ in range(2))
+    tl = E.TensorList(gs, p=ps, m=ms, v=vs)
+    keep = ps[0]
+    ps[1].data = torch.zeros(7, device="cuda")
+    for x in (ps, gs, ms, vs):
+        x.clear()
+    others = [torch.full((5000,), 9.0, device="cuda") for _ in range(40)]
+    E.ea_adamw_step(config(), 1, tl)
+    assert all(bool((x == 9.0).all()) for x in others)
+    assert bool((keep < 1).all())
