@@ -292,6 +292,40 @@ __global__ void __launch_bounds__(kSortBlock) sort_one_kernel(Items t, SortPlan 
     }
 }
 
+constexpr int kFewTokens = 512;          // that one workgroup ranks by comparing all with all
+
+// So few that comparing each with all is the shortest: 2^bits threads a token,
+// a share of the others each.  256 ids 3 us (in digits 6), 512 4.5; the work grows
+// with the square (1,024 took 45).
+__global__ void __launch_bounds__(kSortBlock) rank_kernel(Items t, int n, int bits, uint32_t* keys, uint32_t* at, Fill f)
+{
+    __shared__ uint4 all[kFewTokens / 4];
+    if (blockIdx.x > 0) {
+        fill_zeros<kSortBlock>(f, blockIdx.x - 1, gridDim.x - 1);
+        return;
+    }
+    const int i = threadIdx.x >> bits, shares = 1 << bits, share = threadIdx.x & (shares - 1), own = i / 4;
+    const uint32_t key = i < n ? key_of(t, i) : 0xFFFFFFFFu;
+    if (share == 0 && i < kFewTokens) ((uint32_t*)all)[i] = key;
+    __syncthreads();
+    int rank = 0;
+#pragma unroll 4
+    for (int q = share; q < (n + 3) / 4; q += shares) {
+        const uint4 x = all[q];
+        const uint32_t above = q < own ? key + 1 : key;    // equal ids before this one come first
+        rank += (x.x < above) + (x.y < above) + (x.z < above) + (x.w < above);
+    }
+    if (share == 0 && i < n) {                             // and those of the same four
+        const uint4 x = all[own];
+        rank += (i % 4 > 0 && x.x == key) + (i % 4 > 1 && x.y == key) + (i % 4 > 2 && x.z == key);
+    }
+    for (int d = 1; d < shares; d *= 2) rank += __shfl_xor(rank, d);
+    if (share == 0 && i < n) {
+        keys[rank] = key;
+        at[rank] = (uint32_t)i;
+    }
+}
+
 // Larger batches: the digits of each tile counted, then the tile's items put in place.
 __global__ void __launch_bounds__(kSortBlock) digits_kernel(Items t, SortPlan p, int shift, uint32_t* counts)
 {
@@ -502,6 +536,42 @@ __global__ void __launch_bounds__(kRowBlock) sum_kernel(SumArgs a, const X* dx, 
         finish_row(a, table, end_key, col, n, sum);
 }
 
+// Few tokens: a workgroup a position of the sorted order, of which those where a
+// run begins sum the run; no row is split and nothing is left to join.
+template <class T, class X>
+__global__ void __launch_bounds__(kRowBlock) sum_runs_kernel(SumArgs a, const X* dx, T* table)
+{
+    const int lane = lane_id(), i = blockIdx.x, count = (int)a.n;
+    const int64_t col = ((int64_t)blockIdx.y * blockDim.x + threadIdx.x) * 4;
+    const int n = a.dim - col >= 4 ? 4 : a.dim > col ? (int)(a.dim - col) : 0;
+    const uint32_t key = a.keys[i], before = a.keys[i > 0 ? i - 1 : 0];
+    int from = i, mine = from + lane < count ? from + lane : count - 1;
+    uint32_t others = a.keys[mine], at = a.at[mine];
+    if ((key >= a.vocab) | ((i > 0) & (before == key))) return;
+    v4f sum = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (;;) {
+        const int run = __popcll(__ballot(from + lane < count && others == key));
+        for (int k = 0; k < run; k += kAhead) {
+            typename Quad<X>::vec x[kAhead];
+#pragma unroll
+            for (int r = 0; r < kAhead; ++r) {
+                const int p = k + r < run ? k + r : run - 1;
+                const X* row = dx + (int64_t)(uint32_t)__builtin_amdgcn_readlane((int)at, p) * a.x_stride + col;
+                x[r] = n == 4 ? load4_once(row) : load_some(row, n);
+            }
+#pragma unroll
+            for (int r = 0; r < kAhead; ++r)
+                if (k + r < run) sum = sum + widen(x[r]);
+        }
+        from += kWave;
+        if (run < kWave || from >= count) break;
+        mine = from + lane < count ? from + lane : count - 1;
+        others = a.keys[mine];
+        at = a.at[mine];
+    }
+    if (n > 0) finish_row(a, table, key, col, n, sum);
+}
+
 // The same for narrow rows, several groups a wave, each lane for itself.
 template <class T, class X>
 __global__ void __launch_bounds__(kRowBlock) sum_narrow_kernel(SumArgs a, const X* dx, T* table)
@@ -708,7 +778,14 @@ hipError_t start_grad(const ea_embed_t& c, const GradPlan& p, const void* ids, c
     uint32_t* counts = (uint32_t*)(ws + p.off_counts);
     const auto keys = [&](int k) { return (uint32_t*)(ws + p.off_keys[k & 1]); };
     const auto at = [&](int k) { return (uint32_t*)(ws + p.off_at[k & 1]); };
-    if (c.tokens <= kMostTile) {
+    if (c.tokens <= kFewTokens) {
+        int bits = 0;
+        while (bits < 3 && c.tokens << (bits + 1) <= kSortBlock) ++bits;
+        hipLaunchKernelGGL(rank_kernel, dim3(1 + groups), dim3(kSortBlock), 0, s, t, (int)c.tokens, bits, keys(0), at(0),
+                           fill_part(f, units, 0, 1));
+        t.keys = keys(0);
+        t.at = at(0);
+    } else if (c.tokens <= kMostTile) {
         hipLaunchKernelGGL(sort_one_kernel, dim3(1 + groups), dim3(kSortBlock), 0, s, t, p.sort, keys(0), at(0),
                            fill_part(f, units, 0, 1));
         t.keys = keys(0);
@@ -742,6 +819,12 @@ hipError_t start_grad(const ea_embed_t& c, const GradPlan& p, const void* ids, c
     a.scale = c.scale;
     a.gbits = group_bits(c.dim);
     a.accumulate = accumulate ? 1 : 0;
+    if (c.tokens <= kFewTokens) {
+        const int64_t waves = c.dim > 3 * kJoinCols ? 4 : (c.dim + kJoinCols - 1) / kJoinCols, cols = waves * kJoinCols;
+        hipLaunchKernelGGL((sum_runs_kernel<T, X>), dim3((unsigned)c.tokens, (unsigned)((c.dim + cols - 1) / cols)),
+                           dim3((unsigned)(waves * kWave)), 0, s, a, dx, table);
+        return hipGetLastError();
+    }
     const int64_t per = (int64_t)1 << (8 - a.gbits);
     const dim3 grid((unsigned)((p.chunks + per - 1) / per),
                     (unsigned)((c.dim + ((int64_t)4 << a.gbits) - 1) >> (2 + a.gbits)));
@@ -756,7 +839,7 @@ hipError_t start_grad(const ea_embed_t& c, const GradPlan& p, const void* ids, c
 }
 
 // Tokens below which a group takes one (R = 1): 16 tokens are 7 us either way, the call.
-constexpr int64_t kFewTokens = 8192;
+constexpr int64_t kOneByOne = 8192;
 
 // f(table element, row element) with the types that c names.
 template <class F, class T>
@@ -784,7 +867,7 @@ hipError_t launch_embed_lookup(const ea_embed_t& c, const void* table, const voi
     return with_types(c, [&](auto t, auto e) {
         using T = decltype(t);
         using X = decltype(e);
-        if (c.tokens < kFewTokens)
+        if (c.tokens < kOneByOne)
             hipLaunchKernelGGL((lookup_kernel<T, X, 1>), dim3(row_groups(c.tokens, gbits)), dim3(kRowBlock), 0, s, c,
                                (const T*)table, ids, (X*)x, gbits);
         else

@@ -102,7 +102,7 @@ KINDS = ["any", "same", "zipf", "ordered", "outside", "nothing"]
 
 @pytest.mark.parametrize("kind", KINDS)
 @pytest.mark.parametrize("n,vocab,dim", [(1, 1, 1), (1, 1000, 16), (2, 3, 5), (31, 10, 64), (32, 4, 64), (33, 100, 66),
-                                         (64, 7, 130), (1000, 50, 96), (2049, 3000, 32), (5000, 700, 40),
+                                         (64, 7, 130), (129, 40, 7), (257, 9, 300), (512, 30, 20), (513, 30, 20), (500, 2000, 1100), (1000, 50, 96), (2049, 3000, 32), (5000, 700, 40),
                                          (20_000, 70_000, 8), (9000, 300_000, 4), (4096, 600, 12), (8191, 600, 12), (8193, 600, 12),
                                          (140_000, 90, 5), (262_145, 50, 4), (530_000, 1_100_000, 4), (30_000, 600_000, 3)])
 def test_gradient(n, vocab, dim, kind):
