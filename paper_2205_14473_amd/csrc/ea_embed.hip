@@ -472,9 +472,11 @@ __device__ __forceinline__ void finish_row(const SumArgs& a, T* table, uint32_t 
 // A group of lanes sums one chunk of the sorted order over its slice of the
 // columns.  A row is finished here where its run lies within the chunk; a run
 // that came from the chunk before goes to partial row 0, one that goes on in
-// the chunk after to partial row 1.  Groups are whole waves here: a lane holds
-// one position's key and row, from which the wave takes the next rows' addresses
-// and the ends of the runs without a branch of its own.  HBM bounds it: 131,072
+// the chunk after to partial row 1.  Groups are whole waves: a lane holds one
+// position's key and row, from which the wave takes the next rows' addresses and
+// the ends of the runs without a branch of its own.  (Rows of up to 128 columns
+// leave lanes idle; with several groups a wave, each lane for itself, 131,072
+// rows of 128 binary32 columns took 105 us in all, against 57.)  HBM bounds it: 131,072
 // rows of 1024 bfloat16 columns 72 us, 5.3 TB/s with the rows and partial rows
 // written (95 us with dx through the caches, which the sums' rows then leave).
 template <class T, class X>
@@ -572,63 +574,6 @@ __global__ void __launch_bounds__(kRowBlock) sum_runs_kernel(SumArgs a, const X*
     if (n > 0) finish_row(a, table, key, col, n, sum);
 }
 
-// The same for narrow rows, several groups a wave, each lane for itself.
-template <class T, class X>
-__global__ void __launch_bounds__(kRowBlock) sum_narrow_kernel(SumArgs a, const X* dx, T* table)
-{
-    const int64_t c = ((int64_t)blockIdx.x << (8 - a.gbits)) + (threadIdx.x >> a.gbits);
-    const int64_t col = (threadIdx.x & ((1 << a.gbits) - 1)) * 4;
-    if (c >= a.chunks || col >= a.dim) return;
-    const int n = a.dim - col < 4 ? (int)(a.dim - col) : 4;
-    const int64_t begin = c * a.chunk, end = begin + a.chunk < a.n ? begin + a.chunk : a.n;
-    float* part = a.part + c * 2 * a.part_row + col;
-    uint32_t key = a.keys[begin];
-    bool open = begin > 0 && a.keys[begin - 1] == key;
-    v4f sum = {0.0f, 0.0f, 0.0f, 0.0f};
-    uint32_t next_keys[kAhead], next_at[kAhead];
-    const auto fetch = [&](int64_t k) {
-#pragma unroll
-        for (int r = 0; r < kAhead; ++r) {
-            const int64_t i = k + r < end ? k + r : end - 1;
-            next_keys[r] = a.keys[i];
-            next_at[r] = a.at[i];
-        }
-    };
-    fetch(begin);
-    for (int64_t k = begin; k < end; k += kAhead) {
-        uint32_t keys[kAhead];
-        typename Quad<X>::vec x[kAhead];
-#pragma unroll
-        for (int r = 0; r < kAhead; ++r) {
-            keys[r] = next_keys[r];
-            const X* from = dx + (int64_t)next_at[r] * a.x_stride + col;
-            if (keys[r] < a.vocab) x[r] = n == 4 ? load4_once(from) : load_some(from, n);
-        }
-        if (k + kAhead < end) fetch(k + kAhead);
-#pragma unroll
-        for (int r = 0; r < kAhead; ++r) {
-            if (k + r >= end) break;
-            if (keys[r] != key) {
-                if (open)
-                    store4(part, sum);
-                else
-                    finish_row(a, table, key, col, n, sum);
-                open = false;
-                key = keys[r];
-                sum = v4f{0.0f, 0.0f, 0.0f, 0.0f};
-            }
-            if (key >= a.vocab) return;
-            sum = sum + widen(x[r]);
-        }
-    }
-    if (open)
-        store4(part, sum);
-    else if (end < a.n && a.keys[end] == key)
-        store4(part + a.part_row, sum);
-    else
-        finish_row(a, table, key, col, n, sum);
-}
-
 constexpr int kJoinWaves = kRowBlock / kWave;
 constexpr int kJoinCols = kWave * 4;
 
@@ -704,14 +649,12 @@ int64_t align16(int64_t x)
 constexpr int64_t kEnoughWaves = 4096;   // 16 for each CU (8192: 16,384 tokens 49 us against 46)
 constexpr int64_t kLeastChunk = 8;
 
-// Positions of a chunk: 64, or fewer where that leaves CUs without waves (wide
-// rows), or where so few tokens make short chunks the quicker ones (narrow rows).
+// Positions of a chunk: 64, or fewer where that leaves CUs without waves.
 int64_t chunk_of(int64_t tokens, int64_t dim)
 {
     const int64_t waves = (dim + kJoinCols - 1) / kJoinCols;
     int64_t chunk = kMostChunk;
-    while (chunk > kLeastChunk && (group_bits(dim) < 6 ? tokens < 4096 * chunk : tokens / chunk * waves < kEnoughWaves))
-        chunk /= 2;
+    while (chunk > kLeastChunk && tokens / chunk * waves < kEnoughWaves) chunk /= 2;
     return chunk;
 }
 
@@ -817,7 +760,7 @@ hipError_t start_grad(const ea_embed_t& c, const GradPlan& p, const void* ids, c
     a.part = (float*)(ws + p.off_part);
     a.part_row = p.part_row;
     a.scale = c.scale;
-    a.gbits = group_bits(c.dim);
+    a.gbits = c.dim <= kJoinCols ? 6 : group_bits(c.dim);   // whole waves, also of narrow rows
     a.accumulate = accumulate ? 1 : 0;
     if (c.tokens <= kFewTokens) {
         const int64_t waves = c.dim > 3 * kJoinCols ? 4 : (c.dim + kJoinCols - 1) / kJoinCols, cols = waves * kJoinCols;
@@ -828,10 +771,7 @@ hipError_t start_grad(const ea_embed_t& c, const GradPlan& p, const void* ids, c
     const int64_t per = (int64_t)1 << (8 - a.gbits);
     const dim3 grid((unsigned)((p.chunks + per - 1) / per),
                     (unsigned)((c.dim + ((int64_t)4 << a.gbits) - 1) >> (2 + a.gbits)));
-    if (a.gbits < 6)
-        hipLaunchKernelGGL((sum_narrow_kernel<T, X>), grid, dim3(kRowBlock), 0, s, a, dx, table);
-    else
-        hipLaunchKernelGGL((sum_kernel<T, X>), grid, dim3(kRowBlock), 0, s, a, dx, table);
+    hipLaunchKernelGGL((sum_kernel<T, X>), grid, dim3(kRowBlock), 0, s, a, dx, table);
     if (p.chunks > 1)
         hipLaunchKernelGGL(join_kernel<T>, dim3((unsigned)(p.chunks - 1), (unsigned)((c.dim + kJoinCols - 1) / kJoinCols)),
                            dim3(kRowBlock), 0, s, a, table);
