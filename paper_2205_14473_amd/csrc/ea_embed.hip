@@ -371,7 +371,7 @@ __global__ void __launch_bounds__(kSortBlock) prefix_kernel(SortPlan p, uint32_t
 
 // Each wave owns a run of its tile's items and ranks them among its own, 64 at
 // a time, in order; waves, tiles and digits before then add their counts.
-// Latency bounds it, a dozen dependent trips: 7.5 us for 8,192 to 131,072 ids, 18
+// Latency bounds it, a dozen dependent trips: 7.5 us for 8,192 to 131,072 ids, 16
 // with 103 MB of zeros written beside it (13 by themselves).
 __global__ void __launch_bounds__(kSortBlock) scatter_kernel(Items t, SortPlan p, int shift, const uint32_t* counts,
                                                              uint32_t* keys, uint32_t* at, Fill f)
@@ -477,7 +477,7 @@ __device__ __forceinline__ void finish_row(const SumArgs& a, T* table, uint32_t 
 // the ends of the runs without a branch of its own.  (Rows of up to 128 columns
 // leave lanes idle; with several groups a wave, each lane for itself, 131,072
 // rows of 128 binary32 columns took 105 us in all, against 57.)  HBM bounds it: 131,072
-// rows of 1024 bfloat16 columns 72 us, 5.3 TB/s with the rows and partial rows
+// rows of 1024 bfloat16 columns 71 us, 5.3 TB/s with the rows and partial rows
 // written (95 us with dx through the caches, which the sums' rows then leave).
 template <class T, class X>
 __global__ void __launch_bounds__(kRowBlock) sum_kernel(SumArgs a, const X* dx, T* table)
@@ -579,7 +579,7 @@ constexpr int kJoinCols = kWave * 4;
 
 // The runs that cross chunks: the workgroup of the chunk in which one begins
 // adds up its partial rows, a quarter of them to each wave, in an order that
-// their number fixes.  Latency: 4 us for 256 chunks, 13 for 2,048 and a token
+// their number fixes.  Latency: 4 us for 256 chunks, 12 for 2,048 and a token
 // with a tenth of them.
 template <class T>
 __global__ void __launch_bounds__(kRowBlock) join_kernel(SumArgs a, T* table)
