@@ -293,7 +293,8 @@ __device__ __forceinline__ bool plain_square(float v)
 // four with the next one's loads in flight (355M parameters: one 736 us, two 676,
 // four 661, eight 680; 11.7M: one 42, two 45, four 47).
 constexpr int64_t kShortRuns = 1 << 25;
-constexpr float kLeastEps = 0x1p-100f;   // below, quotient's reciprocal could leave the normal numbers
+constexpr float kLeastEps = 0x1p-100f;   // outside these two, quotient's reciprocal could leave the
+constexpr float kMostEps = 0x1p100f;     // normal numbers
 
 // The codes of a quad of first moments and roots, in place of the old ones.
 template <bool DRAWS>
@@ -327,8 +328,8 @@ __device__ __forceinline__ void store_states(const Adamw8Args& a, const Factors&
 // lanes a block, and 16 elements a lane, registers halve the waves: 771 us
 // against 661 for 355M; with 64 the reduction and the divisions cost more, 739
 // against 689 before loads went ahead.)
-// 10 bytes an element (bfloat16 parameters and gradients) against 180
-// instructions for 256 elements: vector issue is busy two thirds of the time
+// 10 bytes an element (bfloat16 parameters and gradients) against 200
+// instructions for 256 elements: vector issue is busy three quarters of the time
 // beside HBM at 5.4 TB/s, 355M parameters 656 us.  With stochastic rounding the
 // draws double the instructions: 11.7M 44 us, 4.3 TB/s (16 bytes an element).
 //
@@ -485,7 +486,7 @@ __device__ __forceinline__ void adamw8_run(const Adamw8Args& a, const Factors& f
                                            uint32_t end)
 {
     Held<P, G, MASTER> h, next;
-    if (f.eps >= kLeastEps && end - begin >= kWaveElements) {
+    if (f.eps >= kLeastEps && f.eps <= kMostEps && end - begin >= kWaveElements) {
         fetch<P, G, MASTER>(e, begin, h);
         for (;;) {
             const uint32_t then = begin + kWaveElements;

@@ -380,6 +380,28 @@ def test_lists_that_do_not_fit_are_refused():
     assert not p.any() and not any(s.any() for s in tl.states)
 
 
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("eps,lr", [(1e-38, 1e-3), (2.0 ** -100, 1e-3), (7e-31, 1e-3), (1e30, 1e28), (2.0 ** 101, 1e28),
+                                    (2e38, 1e36)])
+def test_eps_at_the_ends_of_binary32(eps, lr, bits):
+    """Quotients by an eps whose reciprocal is subnormal or next to overflow, whole blocks and a ragged end."""
+    P = Problem([2048, 777], bits=bits, seed=4)
+    hyper = {**HYPER, "eps": eps, "lr": lr}
+    E.ea_adamw_step(config(bits=bits, eps=eps, lr=lr), P.t, P.list)
+    for i in range(2):
+        if bits == 32:
+            m, v = P.m0[i], P.v0[i]
+        else:
+            m = R.decode(*P.cm0[i]).float().numpy()
+            v = R.decode(*P.cv0[i]).float().numpy() ** 2
+        *_, want = R.adamw32(P.p0[i].numpy(), P.g0[i].numpy(), m, v, P.t, **hyper)
+        # at most two units in the last place of the quotient, or two quanta of a subnormal one, then the
+        # product's and the difference's roundings
+        step, moved = R.f32(lr) / (1 - 0.9 ** P.t), np.abs(want.astype(np.float64) - P.p0[i].numpy())
+        bound = 8 * R.U32 * (np.abs(P.p0[i].numpy()) + moved) + step * 2 * 2.0 ** -149
+        R.within(P.p[i], torch.from_numpy(want).double(), torch.from_numpy(bound), f"p {i}")
+
+
 def test_parts_of_very_large_tensors():
     """A tensor of more than 2^30 elements is stepped in parts: its ends, the parts' borders and the
     draws there against the same elements in a tensor of their own."""
