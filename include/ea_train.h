@@ -115,7 +115,7 @@ int64_t ea_grad_norm_workspace_bytes(int32_t ntensors, const ea_tensor_t *tensor
  * are not looked at) of type grad_type, summed in binary64:
  *     norm   <- scale * sqrt(sum of squares)
  *     gscale <- scale * (max_norm < norm ? max_norm / norm : 1)
- * `scale` (finite) undoes a loss scale or averages accumulated gradients;
+ * `scale` (finite, > 0) undoes a loss scale or averages accumulated gradients;
  * max_norm > 0, infinity for no clipping.  Where the norm is not finite,
  * gscale is NaN, and ea_adamw_step with it changes nothing.
  *   norm, gscale (device, one float each, write; gscale may be NULL),

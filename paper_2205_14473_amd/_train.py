@@ -238,20 +238,33 @@ def _check_list(cfg, tensors):
                      f"{cfg.grad_type}, {cfg.state_bits} bits)")
 
 
+def _one(t, device, name):
+    """Pointer of a scalar (float32, but for t_dev) on the list's device."""
+    if t is None or isinstance(t, int):
+        return t
+    at = _ptr_u32(t) if name == "t_dev" else _ptr(t, B._F32)
+    if t.numel() < 1:
+        raise ValueError(f"{name}: expected one element, got none")
+    if device is not None and t.get_device() != device:
+        raise ValueError(f"{name} is on {t.device}, and the list's tensors on device {device}")
+    return at
+
+
 def ea_adamw_step(cfg, t, tensors, gscale=None, stream=None):
     if tensors.kinds != (cfg.param_type, cfg.grad_type, cfg.state_bits) and tensors.count:
         _check_list(cfg, tensors)
     queue = _queue(stream, tensors.device)
     return _check(lib.ea_adamw_step(C.byref(cfg), t, tensors.count, tensors.address,
-                                    None if gscale is None else _ptr(gscale, B._F32), queue))
+                                    None if gscale is None else _one(gscale, tensors.device, "gscale"), queue))
 
 
 def ea_adamw_step_scheduled(cfg, sched, t_dev, tensors, gscale=None, stream=None):
     if tensors.kinds != (cfg.param_type, cfg.grad_type, cfg.state_bits) and tensors.count:
         _check_list(cfg, tensors)
     queue = _queue(stream, tensors.device)
-    return _check(lib.ea_adamw_step_scheduled(C.byref(cfg), C.byref(sched), _ptr_u32(t_dev), tensors.count,
-                                              tensors.address, _ptr(gscale, B._F32), queue))
+    return _check(lib.ea_adamw_step_scheduled(C.byref(cfg), C.byref(sched), _one(t_dev, tensors.device, "t_dev"),
+                                              tensors.count, tensors.address, _one(gscale, tensors.device, "gscale"),
+                                              queue))
 
 
 def ea_grad_norm_workspace_bytes(tensors) -> int:
@@ -260,10 +273,12 @@ def ea_grad_norm_workspace_bytes(tensors) -> int:
 
 def ea_grad_norm(tensors, scale, max_norm, norm, gscale, workspace, stream=None):
     queue = _queue(stream, tensors.device)
-    f = B._F32
+    d = tensors.device
     _room(workspace, tensors.norm_bytes)
+    if d is not None and hasattr(workspace, "get_device") and workspace.is_cuda and workspace.get_device() != d:
+        raise ValueError(f"the workspace is on {workspace.device}, and the list's tensors on device {d}")
     return _check(lib.ea_grad_norm(tensors.grad_type or EA_F32, tensors.count, tensors.address, scale, max_norm,
-                                   _ptr(norm, f), _ptr(gscale, f), _ptr(workspace), queue))
+                                   _one(norm, d, "norm"), _one(gscale, d, "gscale"), _ptr(workspace), queue))
 
 
 def _room(workspace, need):

@@ -402,6 +402,23 @@ def test_eps_at_the_ends_of_binary32(eps, lr, bits):
         R.within(P.p[i], torch.from_numpy(want).double(), torch.from_numpy(bound), f"p {i}")
 
 
+def test_scalars_that_do_not_fit_are_refused():
+    f = lambda *shape, **kw: torch.zeros(*shape, device="cuda", **kw)  # noqa: E731
+    p = f(4)
+    tl = adamw_list([p], [f(4) + 1])
+    t_dev = torch.ones(1, dtype=torch.int32, device="cuda")
+    for bad, text in ((f(0), "gscale"), (torch.ones(1), "device"), (f(1, dtype=torch.float64), "float32")):
+        with pytest.raises(ValueError, match=text):
+            E.ea_adamw_step(config(), 1, tl, gscale=bad)
+        with pytest.raises(ValueError, match=text):
+            E.ea_adamw_step_scheduled(config(), SCHEDULES[0], t_dev, tl, gscale=bad)
+        with pytest.raises(ValueError, match=text.replace("gscale", "norm")):
+            E.ea_grad_norm(tl, 1.0, 1.0, bad, None, f(1024))
+    with pytest.raises(ValueError, match="t_dev"):
+        E.ea_adamw_step_scheduled(config(), SCHEDULES[0], t_dev[:0], tl)
+    assert not p.any() and t_dev.item() == 1
+
+
 def test_parts_of_very_large_tensors():
     """A tensor of more than 2^30 elements is stepped in parts: its ends, the parts' borders and the
     draws there against the same elements in a tensor of their own."""
