@@ -132,7 +132,7 @@ class TensorList:
             e.lr_scale = lr_scale if isinstance(lr_scale, (int, float)) else lr_scale[i]
         self.kinds = (self.param_type, self.grad_type, self.state_bits)
         self.norm_bytes = _check(lib.ea_grad_norm_workspace_bytes(n, self.address))
-        # the memory stays, whatever becomes of the caller's lists and tensors
+        # the memory stays, whatever becomes of the caller's lists and tensors (the gradients': set_grads)
         self._held = [t.untyped_storage() for ts in (p, m, v, m_scale, v_scale, master) if ts is not None
                       for t in ts if t is not None]
         if p is not None:
@@ -217,7 +217,7 @@ class TensorList:
         self._column("n", sizes)
         self._column("g", at)
         self.grad_type, self.device = kind, devices.pop() if devices else None
-        self._g = tuple(g)
+        self._g, self._g_held = tuple(g), [t.untyped_storage() for t in g]
 
 
 def _queue(stream, device):
