@@ -356,7 +356,8 @@ def ea_embed_workspace_bytes(cfg) -> int:
 
 def ea_embed_grad(cfg, ids, dx, dtable, accumulate, workspace, stream=None):
     _room(workspace, lib.ea_embed_workspace_bytes(C.byref(cfg)))
-    if _fits(cfg, dtable, ids, dx) and (workspace is None or workspace.get_device() == dx.get_device()):
+    if _fits(cfg, dtable, ids, dx) and (not hasattr(workspace, "get_device") or
+                                        workspace.get_device() == dx.get_device()):
         return _check(lib.ea_embed_grad(C.byref(cfg), ids.data_ptr(), dx.data_ptr(), dtable.data_ptr(),
                                         1 if accumulate else 0, _ptr(workspace), _queue(stream, dx.get_device())))
     args = (_ids(ids, cfg), _rows(dx, cfg.x_type, cfg.tokens, cfg.dim, cfg.x_stride, "dx"),

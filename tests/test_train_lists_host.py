@@ -51,3 +51,31 @@ def test_a_list_holds_its_gradients_memory(E):
     assert all(m() is not None for m in memory)
     tl.set_grads(other)
     assert memory[1]() is None and memory[2]() is None
+
+
+@pytest.fixture
+def current_device(E, monkeypatch):
+    """Device 0 is the current one, whether there is a GPU or not."""
+    from paper_2205_14473_amd import _train
+    _train._dtypes()
+    monkeypatch.setattr(_train, "_current", lambda: 0)
+
+
+def embedding(E):
+    c = E.Embed(tokens=4, vocab=7, dim=6, table_stride=6, x_stride=6, padding=-1, scale=1.0, index_bits=64)
+    return c, on_device(torch.zeros(4, dtype=torch.int64)), on_device(torch.zeros(4, 6)), on_device(torch.zeros(7, 6))
+
+
+@pytest.mark.parametrize("plain", [True, False])
+def test_a_workspace_may_be_a_raw_pointer(E, current_device, plain):
+    """Beside tensors of the plain form and of others alike: the call gets as far as the library, which
+    refuses the address (8 is not 16-byte aligned)."""
+    c, ids, dx, dtable = embedding(E)
+    if not plain:
+        ids = on_device(torch.zeros(2, 2, dtype=torch.int64))
+        dx = on_device(torch.zeros(2, 2, 6))
+    with pytest.raises(E.EAError, match="workspace is not 16-byte aligned"):
+        E.ea_embed_grad(c, ids, dx, dtable, False, 8, 0)
+    tl = E.TensorList([on_device(torch.zeros(5))])
+    with pytest.raises(E.EAError, match="workspace is not 8-byte aligned"):
+        E.ea_grad_norm(tl, 1.0, 1.0, 16, 16, 4, 0)
