@@ -88,6 +88,11 @@ def _dense(t) -> bool:
     return True
 
 
+def _same_order(t, e) -> bool:
+    """Whether two tensors of one shape go through their elements in the same order of memory."""
+    return t.stride() == e.stride() or all(a == b for a, b, n in zip(t.stride(), e.stride(), t.shape) if n != 1)
+
+
 def _is_tensor(name, i, t):
     if not hasattr(t, "data_ptr"):
         raise ValueError(f"{name}[{i}]: expected a tensor, got {type(t).__name__}")
@@ -170,7 +175,7 @@ class TensorList:
             if e is not t:
                 if t.get_device() != e.get_device():
                     raise ValueError(f"{name}[{i}] is on {t.device}, and others on {e.device}")
-                if t.shape != e.shape or (t.stride() != e.stride() and t.numel() > 1):
+                if t.shape != e.shape or (t.numel() > 1 and not _same_order(t, e)):
                     raise ValueError(f"{name}[{i}]: shape {tuple(t.shape)}, strides {t.stride()} are not the "
                                      f"parameter's {tuple(e.shape)}, {e.stride()}")
             if not t.is_contiguous() and not _dense(t):

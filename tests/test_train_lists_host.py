@@ -79,3 +79,21 @@ def test_a_workspace_may_be_a_raw_pointer(E, current_device, plain):
     tl = E.TensorList([on_device(torch.zeros(5))])
     with pytest.raises(E.EAError, match="workspace is not 8-byte aligned"):
         E.ea_grad_norm(tl, 1.0, 1.0, 16, 16, 4, 0)
+
+
+def test_strides_of_one_element_do_not_matter(E):
+    """A dimension of one element has no order: a convolution of 1 x 1 is laid out alike under either of
+    torch's memory formats, also beside one of 3 x 3 whose format differs from the default."""
+    def like(shape, strides):
+        return on_device(torch.zeros(shape).as_strided(shape, strides))
+
+    wide, narrow = ((8, 4, 3, 3), (36, 1, 12, 4)), (8, 4, 1, 1)
+    for a, b in (((4, 1, 1, 1), (4, 1, 4, 4)), ((4, 1, 4, 4), (4, 1, 1, 1))):
+        p, g = [like(*wide), like(narrow, a)], [like(*wide), like(narrow, b)]
+        tl = E.TensorList(g, p=p)
+        assert [e.p for e in tl.array] == [t.data_ptr() for t in p]
+        assert [e.g for e in tl.array] == [t.data_ptr() for t in g]
+        tl.set_grads([like(*wide), like(narrow, a)])
+    # the order of dimensions that have one does
+    with pytest.raises(ValueError, match="strides"):
+        E.TensorList([like(*wide), like((8, 4, 1, 1), (1, 8, 1, 1))], p=[like(*wide), like(narrow, (4, 1, 1, 1))])
