@@ -318,7 +318,7 @@ def _rows(t, kind, rows, dim, stride, name):
 def _ids(t, cfg):
     if t is None or isinstance(t, int):
         return t
-    if t.is_floating_point() or t.element_size() * 8 != cfg.index_bits:
+    if t.is_floating_point() or t.is_complex() or t.element_size() * 8 != cfg.index_bits:
         raise ValueError(f"ids: expected {cfg.index_bits}-bit integers, got {t.dtype}")
     if t.numel() != cfg.tokens:
         raise ValueError(f"ids: expected {cfg.tokens}, got {t.numel()}")

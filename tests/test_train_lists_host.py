@@ -97,3 +97,17 @@ def test_strides_of_one_element_do_not_matter(E):
     # the order of dimensions that have one does
     with pytest.raises(ValueError, match="strides"):
         E.TensorList([like(*wide), like((8, 4, 1, 1), (1, 8, 1, 1))], p=[like(*wide), like(narrow, (4, 1, 1, 1))])
+
+
+@pytest.mark.parametrize("bits,kind", [(64, torch.complex64), (32, torch.complex32), (32, torch.float32),
+                                       (64, torch.float64), (64, torch.int32), (32, torch.int64)])
+def test_ids_are_integers(E, current_device, bits, kind):
+    """Types of an id's size that hold no integers are refused (the library would refuse the rest: a scale
+    of NaN, a workspace at 8)."""
+    c, _, x, table = embedding(E)
+    c.index_bits, ids = bits, on_device(torch.zeros(4, dtype=kind))
+    with pytest.raises(ValueError, match=f"expected {bits}-bit integers"):
+        E.ea_embed_grad(c, ids, x, table, False, 8, 0)
+    c.scale = float("nan")
+    with pytest.raises(ValueError, match=f"expected {bits}-bit integers"):
+        E.ea_embed_lookup(c, table, ids, x, 0)
