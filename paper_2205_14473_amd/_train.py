@@ -98,6 +98,15 @@ def _is_tensor(name, i, t):
         raise ValueError(f"{name}[{i}]: expected a tensor, got {type(t).__name__}")
 
 
+def _each(name, x, n):
+    """n numbers from one for all, or from a sequence of n."""
+    if isinstance(x, (int, float)) or getattr(x, "ndim", 1) == 0:
+        return [x] * n
+    if len(x) != n:
+        raise ValueError(f"{len(x)} values of {name}, and {n} tensors")
+    return x
+
+
 class TensorList:
     """The tensors of an AdamW step or a gradient norm: an ea_tensor_t array and references to what it points
     to.  A program makes it once and passes it every step; ``set_grads`` replaces the gradients.  It stands for
@@ -132,9 +141,8 @@ class TensorList:
             raise ValueError("m and v come together")
         if m is not None:
             self.state_bits = self._set_states(m, v, m_scale, v_scale)
-        for i, e in enumerate(self.array[:n]):
-            e.weight_decay = weight_decay if isinstance(weight_decay, (int, float)) else weight_decay[i]
-            e.lr_scale = lr_scale if isinstance(lr_scale, (int, float)) else lr_scale[i]
+        for e, wd, ls in zip(self.array, _each("weight_decay", weight_decay, n), _each("lr_scale", lr_scale, n)):
+            e.weight_decay, e.lr_scale = wd, ls
         self.kinds = (self.param_type, self.grad_type, self.state_bits)
         self.norm_bytes = _check(lib.ea_grad_norm_workspace_bytes(n, self.address))
         # the memory stays, whatever becomes of the caller's lists and tensors (the gradients': set_grads)

@@ -111,3 +111,15 @@ def test_ids_are_integers(E, current_device, bits, kind):
     c.scale = float("nan")
     with pytest.raises(ValueError, match=f"expected {bits}-bit integers"):
         E.ea_embed_lookup(c, table, ids, x, 0)
+
+
+@pytest.mark.parametrize("name", ["weight_decay", "lr_scale"])
+def test_factors_come_one_for_all_or_one_for_each(E, name):
+    g = [on_device(torch.zeros(3)) for _ in range(2)]
+    for bad in ([0.1], [0.1, 0.2, 0.3], []):
+        with pytest.raises(ValueError, match=f"{len(bad)} values of {name}, and 2 tensors"):
+            E.TensorList(g, **{name: bad})
+    for one in (0.5, 1, np.float32(0.5), torch.tensor(0.5)):
+        assert [getattr(e, name) for e in E.TensorList(g, **{name: one}).array] == [float(one)] * 2
+    for each in ([0.25, 0.5], (0.25, 0.5), np.array([0.25, 0.5]), torch.tensor([0.25, 0.5])):
+        assert [getattr(e, name) for e in E.TensorList(g, **{name: each}).array] == [0.25, 0.5]
