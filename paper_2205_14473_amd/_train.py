@@ -131,6 +131,8 @@ class TensorList:
                          ("master", master)):
             if ts is not None and len(ts) != n:
                 raise ValueError(f"{len(ts)} tensors in {name}, and {n} in g")
+        for i, t in enumerate(p or ()):
+            _is_tensor("p", i, t)
         self.set_grads(g)
         if p is not None:
             self.param_type, at = self._checked("p", p, g)

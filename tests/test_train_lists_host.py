@@ -123,3 +123,13 @@ def test_factors_come_one_for_all_or_one_for_each(E, name):
         assert [getattr(e, name) for e in E.TensorList(g, **{name: one}).array] == [float(one)] * 2
     for each in ([0.25, 0.5], (0.25, 0.5), np.array([0.25, 0.5]), torch.tensor([0.25, 0.5])):
         assert [getattr(e, name) for e in E.TensorList(g, **{name: each}).array] == [0.25, 0.5]
+
+
+def test_entries_of_p_that_are_no_tensors_are_named(E):
+    g = [on_device(torch.zeros(3)) for _ in range(2)]
+    for bad in (None, 3):
+        for at in (0, 1):
+            p = [on_device(torch.zeros(3)) for _ in range(2)]
+            p[at] = bad
+            with pytest.raises(ValueError, match=rf"p\[{at}\]: expected a tensor, got {type(bad).__name__}"):
+                E.TensorList(g, p=p)
