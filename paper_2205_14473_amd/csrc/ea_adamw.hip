@@ -295,6 +295,8 @@ __device__ __forceinline__ bool plain_square(float v)
 constexpr int64_t kShortRuns = 1 << 25;
 constexpr float kLeastEps = 0x1p-100f;   // outside these two, quotient's reciprocal could leave the
 constexpr float kMostEps = 0x1p100f;     // normal numbers
+constexpr float kMostOverEps = 0x1p120f; // first moments over eps from which it could overflow (and end as
+                                         // inf - inf where the division gives an infinity)
 
 // The codes of a quad of first moments and roots, in place of the old ones.
 template <bool DRAWS>
@@ -457,6 +459,7 @@ __device__ __forceinline__ bool adamw8_whole(const Adamw8Args& a, const Factors&
             rtop = fmaxf(rtop, rk);
         }
     }
+    fine &= mtop < f.eps * kMostOverEps;
     if (__ballot(!fine)) return false;
 #pragma unroll
     for (int q = 0; q < kRowQuads; ++q) {

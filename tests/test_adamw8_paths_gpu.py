@@ -1,0 +1,68 @@
+"""AdamW with 8-bit states: whole blocks of ordinary values take a shorter form than ragged ends and
+unusual values.  What the two leave has to be the same, up to the bound that the header states for p."""
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+if not torch.cuda.is_available():  # pragma: no cover - CPU-only host
+    pytest.skip("needs a GPU", allow_module_level=True)
+
+import paper_2205_14473_amd as E  # noqa: E402
+import train_util as R  # noqa: E402
+
+HYPER = dict(lr=3e-3, beta1=0.9, beta2=0.95)
+
+
+class Block8:
+    """One tensor with 8-bit states in float32 and as codes, on the host."""
+
+    def __init__(self, n, seed=1):
+        rng = np.random.default_rng(seed)
+        self.n, blocks = n, -(-n // 256)
+        self.p = (rng.standard_normal(n) * 0.1).astype(np.float32)
+        self.g = (rng.standard_normal(n) * 1e-2).astype(np.float32)
+        self.cm, self.ms = R.encode32((rng.standard_normal(n) * 3e-3).astype(np.float32), False)
+        self.cv, self.vs = R.encode32(np.abs(rng.standard_normal(n) * 1e-2).astype(np.float32), True)
+        assert self.ms.shape == (blocks,)
+
+    def values(self, codes, scales):
+        return R.VALUES[codes].astype(np.float32) * np.repeat(scales, 256)[:self.n]
+
+    def wanted(self, t, eps):
+        """m, root, p of the step, each operation in binary32."""
+        with np.errstate(over="ignore", invalid="ignore"):
+            r = self.values(self.cv, self.vs)
+            m, r, _, p = R.adamw32(self.p, self.g, self.values(self.cm, self.ms), r * r, t, eps=eps, **HYPER)
+        return m, r, p
+
+    def step(self, t, eps, **kw):
+        """(p, codes and scales of m, codes and scales of the root) after the step on the GPU."""
+        up = lambda x: torch.from_numpy(x.copy()).cuda()  # noqa: E731
+        p, g, m, v, ms, vs = (up(x) for x in (self.p, self.g, self.cm, self.cv, self.ms, self.vs))
+        cfg = E.AdamW(eps=eps, state_bits=8, **HYPER, **kw)
+        E.ea_adamw_step(cfg, t, E.TensorList([g], p=[p], m=[m], v=[v], m_scale=[ms], v_scale=[vs]))
+        return [x.cpu().numpy() for x in (p, m, ms, v, vs)]
+
+
+@pytest.mark.parametrize("sign", [1, -1])
+@pytest.mark.parametrize("n", [512, 2048, 2048 + 300])
+def test_an_overflowing_quotient_is_an_infinity(n, sign):
+    """A first moment far above its root and eps: m / (root + eps) leaves binary32, and p becomes an infinity
+    of the other sign, as by the division, in whole blocks and in others."""
+    eps, at = 1e-10, [5, n - 200, n - 1]
+    b = Block8(n)
+    for k in {i // 256 for i in at}:
+        b.cm[256 * k:256 * (k + 1)], b.ms[k] = 0, np.float32(2.0 ** 100)
+    for i in at:
+        b.cm[i] = 0x7E if sign > 0 else 0xFE       # 448 of the scale
+        b.cv[i], b.g[i] = 0, 0
+    m, r, want = b.wanted(7, eps)
+    assert np.isinf(want[at]).all() and np.isfinite(np.delete(want, at)).all()
+    p, cm, ms, cv, vs = b.step(7, eps)
+    assert p[at].tolist() == [-sign * np.inf] * len(at)
+    assert np.isfinite(np.delete(p, at)).all()
+    for codes, scales, x, roots in ((cm, ms, m, False), (cv, vs, r, True)):
+        c, s = R.encode32(x, roots)
+        assert np.array_equal(codes, c) and np.array_equal(scales, s)
