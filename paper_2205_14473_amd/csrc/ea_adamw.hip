@@ -438,7 +438,7 @@ __device__ __forceinline__ bool adamw8_whole(const Adamw8Args& a, const Factors&
     const uint32_t first = first_of_lane();
     v4f p[kRowQuads], m[kRowQuads], r[kRowQuads];
     float mtop = 0.0f, rtop = 0.0f;
-    bool fine = h.ms == h.ms;
+    bool fine = true;
 #pragma unroll
     for (int q = 0; q < kRowQuads; ++q) {
         m[q] = values_of(h.cm[q], h.ms);
@@ -455,11 +455,11 @@ __device__ __forceinline__ bool adamw8_whole(const Adamw8Args& a, const Factors&
             p[q][k] = p[q][k] * f.keep - quotient(mk, rk * f.root + f.eps) * f.step;
             m[q][k] = mk;
             r[q][k] = rk;
-            mtop = fmaxf(mtop, fabsf(mk));
+            mtop = __builtin_elementwise_maximum(mtop, fabsf(mk));  // a NaN stays
             rtop = fmaxf(rtop, rk);
         }
     }
-    fine &= mtop < f.eps * kMostOverEps;
+    fine &= mtop < f.eps * kMostOverEps;                   // nor NaN
     if (__ballot(!fine)) return false;
 #pragma unroll
     for (int q = 0; q < kRowQuads; ++q) {

@@ -66,3 +66,27 @@ def test_an_overflowing_quotient_is_an_infinity(n, sign):
     for codes, scales, x, roots in ((cm, ms, m, False), (cv, vs, r, True)):
         c, s = R.encode32(x, roots)
         assert np.array_equal(codes, c) and np.array_equal(scales, s)
+
+
+@pytest.mark.parametrize("state", ["m", "v"])
+def test_a_nan_code_makes_its_block_s_scale_nan(state):
+    """A NaN among the codes that a caller brings (0x7F, 0xFF) under a finite scale: p is NaN in that element,
+    the scale of that state's block becomes NaN, and nothing else differs, in whole blocks and in others."""
+    for code in (0x7F, 0xFF):
+        for at in (100, 300, 511, 700, 999):            # of 1000 elements the first 512 are two whole blocks
+            b = Block8(1000)
+            m, r, want = b.wanted(3, 1e-8)
+            p0, cm0, ms0, cv0, vs0 = b.step(3, 1e-8)
+            (b.cm if state == "m" else b.cv)[at] = code
+            p, cm, ms, cv, vs = b.step(3, 1e-8)
+            assert np.flatnonzero(np.isnan(p)).tolist() == [at]
+            # one form's root and quotient are a unit in the last place off at most, 2^-22 of what p moves by; then
+            # p's roundings
+            bound = 2.0 ** -22 * np.abs(p0 - b.p) + 2.0 ** -22 * np.maximum(np.abs(p0), np.abs(b.p))
+            assert (np.delete(np.abs(p - p0) - bound, at) <= 0).all()
+            odd, other = (ms, vs) if state == "m" else (vs, ms)
+            assert np.flatnonzero(np.isnan(odd)).tolist() == [at // 256], (code, at)
+            assert np.array_equal(other, vs0 if state == "m" else ms0)
+            rest = np.arange(1000) // 256 != at // 256
+            assert np.array_equal(cm[rest], cm0[rest]) and np.array_equal(cv[rest], cv0[rest])
+            assert np.array_equal(odd[~np.isnan(odd)], (ms0 if state == "m" else vs0)[~np.isnan(odd)])
