@@ -66,11 +66,11 @@ typedef struct ea_adamw {
 /* One AdamW step (Loshchilov and Hutter: decoupled weight decay, bias
  * correction) over ntensors tensors, t >= 1 the step.  With s = *gscale (1
  * when gscale is NULL), lr_i = lr * lr_scale, every operation rounded to
- * binary32 by itself:
+ * binary32 by itself (with 8-bit states but for the root and the quotient, see below):
  *     g <- g * s
  *     m <- beta1 m + (1 - beta1) g
  *     v <- beta2 v + (1 - beta2) (g g)
- *     p <- p (1 - lr_i wd) - (lr_i / (1 - beta1^t)) (m / (sqrt(v) / sqrt(1 - beta2^t) + eps))
+ *     p <- p (1 - lr_i wd) - (lr_i / (1 - beta1^t)) (m / (sqrt(v) (1 / sqrt(1 - beta2^t)) + eps))
  * where the factors in parentheses that hold no element are formed in
  * binary64 and rounded once.  With a master the update is the master's and p
  * its rounding (p is not read).  If *gscale is not finite the call changes
@@ -82,12 +82,17 @@ typedef struct ea_adamw {
  * those of the root r of the second moment; element k is code * scale[k/256].
  * Both are widened, stepped and used for p in binary32, and rounded only to be
  * kept: scale = max|x| * (1/448) over the block, code = x * (1/scale) rounded to E4M3.
+ *   - The square root of v and the quotient in p may each be one unit in the
+ *     last place off the rounded result (in practice one in a million is).
+ *     They are the rounded ones for blocks past the last multiple of 512
+ *     elements, and near values that are subnormal, infinite or NaN.
  *   - A block whose scale falls under 2^-126 is kept as zeros.
  *   - Second moments are binary32 between reading and keeping them: roots
  *     under 2^-63 square to subnormal numbers and lose digits, then vanish.
  *   - A positive root never gets the code 0 (it would leave m / eps): the
  *     smallest code, 2^-9 of the scale, takes its place.
- *   - An infinity or NaN in a block makes the block's scale NaN: it shows.
+ *   - An infinity or NaN in a block, or a NaN among its codes, makes the
+ *     block's scale NaN: it shows.
  *   - EA_ROUND_STOCHASTIC: codes between two neighbours go up with the
  *     probability of the fraction, from 16 bits.  To nearest, a relative change
  *     of a state by less than half a code step (3 to 6%) is lost every time,

@@ -263,9 +263,11 @@ __device__ __forceinline__ void store_codes(uint8_t* p, uint32_t c, int n)
 constexpr int kRowQuads = EA_STATE_BLOCK / 4 / kRowLanes;
 constexpr uint32_t kWaveElements = (kWave / kRowLanes) * EA_STATE_BLOCK;
 
-// Root and quotient by one correction step on the hardware's approximations:
-// rounded as sqrtf and the division do but for about one value in a million,
-// which is one unit in the last place off.  Those two check for operands that
+// Root and quotient by one correction step on the hardware's approximations
+// (each within one unit in the last place): what is left before the last
+// rounding is of second order, some 2^-21 of a unit for the quotient's and the
+// root's alike, so the result is one of the value's two neighbours, and for all
+// but about one value in a million the nearer, as sqrtf and the division give.  Those two check for operands that
 // the approximations do not take (29 instructions an element together, of 45;
 // here 12), which is left to plain_square below.
 __device__ __forceinline__ float root_of(float v)

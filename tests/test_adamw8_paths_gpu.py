@@ -90,3 +90,36 @@ def test_a_nan_code_makes_its_block_s_scale_nan(state):
             rest = np.arange(1000) // 256 != at // 256
             assert np.array_equal(cm[rest], cm0[rest]) and np.array_equal(cv[rest], cv0[rest])
             assert np.array_equal(odd[~np.isnan(odd)], (ms0 if state == "m" else vs0)[~np.isnan(odd)])
+
+
+@pytest.mark.parametrize("t", [1, 7, 1000])
+def test_parameters_and_roots_of_whole_blocks(t):
+    """p and the roots behind the kept scales against each operation in binary32: the same bits where a block
+    is ragged, and in whole blocks within one unit in the last place of the root and one of the quotient."""
+    n, eps = (1 << 20) + 300, 1e-8
+    b = Block8(n, seed=t)
+    m, r, want = b.wanted(t, eps)
+    p, cm, ms, cv, vs = b.step(t, eps)
+    assert np.array_equal(p[1 << 20:], want[1 << 20:])
+    # the root's unit, and a product and a sum that may round the other way: 2^-21 of the denominator; the
+    # quotient's own; then a product and a difference: 2^-20 of the move and 2^-22 of p
+    bound = 2.0 ** -20 * np.abs(want.astype(np.float64) - b.p) + 2.0 ** -22 * np.maximum(np.abs(want), np.abs(b.p))
+    off = np.abs(p.astype(np.float64) - want)
+    assert (off <= bound).all(), float((off / bound).max())
+    assert (p != want).sum() <= 100                 # of a million; one in a million is what the kernel's comment says
+    codes, scales = R.encode32(m, False)
+    assert np.array_equal(cm, codes) and np.array_equal(ms, scales)
+    codes, scales = R.encode32(r, True)
+    assert (np.abs(vs.astype(np.float64) - scales) <= 2.0 ** -22 * scales).all()
+    assert (cv != codes).sum() <= 20                # a root next to the border between two codes
+
+
+@pytest.mark.parametrize("t", [1, 7, 1000])
+def test_32_bit_states_have_each_operation_s_bits(t):
+    b = Block8(5003, seed=t)
+    m0, v0 = b.values(b.cm, b.ms), b.values(b.cv, b.vs) ** 2
+    m, r, _, want = R.adamw32(b.p, b.g, m0, v0, t, eps=1e-8, wd=0.1, **HYPER)
+    p, g, mg, vg = (torch.from_numpy(x.copy()).cuda() for x in (b.p, b.g, m0, v0))
+    E.ea_adamw_step(E.AdamW(eps=1e-8, state_bits=32, **HYPER), t, E.TensorList([g], p=[p], m=[mg], v=[vg], weight_decay=0.1))
+    assert np.array_equal(mg.cpu().numpy(), m) and np.array_equal(np.sqrt(vg.cpu().numpy()), r)
+    assert np.array_equal(p.cpu().numpy(), want)
