@@ -123,3 +123,65 @@ def test_32_bit_states_have_each_operation_s_bits(t):
     E.ea_adamw_step(E.AdamW(eps=1e-8, state_bits=32, **HYPER), t, E.TensorList([g], p=[p], m=[mg], v=[vg], weight_decay=0.1))
     assert np.array_equal(mg.cpu().numpy(), m) and np.array_equal(np.sqrt(vg.cpu().numpy()), r)
     assert np.array_equal(p.cpu().numpy(), want)
+
+
+@pytest.mark.parametrize("kind,master", [("bf16", True), ("bf16", False), ("f32", False)])
+def test_long_calls_step_as_short_ones(kind, master):
+    """From 2^25 elements on a wave takes four groups of blocks, each fetched while the last is worked on.  The
+    same elements in calls of fewer, one group a wave, leave the same bits: values that send a group in the
+    middle of a run to the general form (NaN, subnormal second moments, a NaN code) among them."""
+    param = {"bf16": torch.bfloat16, "f32": torch.float32}[kind]
+    n, cut = (1 << 25) + 5 * 512 + 77, (1 << 24)
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    rand = lambda scale: torch.randn(n, device="cuda", generator=gen) * scale  # noqa: E731
+    w, g = rand(0.1), rand(1e-2)
+    m, v = (torch.randint(0, 127, (n,), device="cuda", generator=gen, dtype=torch.uint8) for _ in range(2))
+    m |= torch.randint(0, 2, (n,), device="cuda", generator=gen, dtype=torch.uint8) << 7
+    ms, vs = (torch.rand(-(-n // 256), device="cuda", generator=gen) * 1e-5 + 1e-6 for _ in range(2))
+    # one group of the four of a run for each fault, first to last, in different runs
+    for run, (group, fault) in enumerate([(0, "nan"), (1, "small"), (2, "code"), (3, "nan"), (1, "nan"), (2, "small")]):
+        at = (1 << 20) + run * 2048 + group * 512 + 100 + run
+        if fault == "nan":
+            g[at] = float("nan")
+        elif fault == "small":
+            g[at], v[at], vs[at // 256] = 0, 1, 2.0 ** -55      # its root squares to 2^-128, a subnormal
+        else:
+            m[at] = 0x7F
+    p = w.to(param)
+    g = g.to(param)
+    outs = []
+    for cuts in ([(0, n)], [(0, cut), (cut, n)]):
+        got = [x.clone() for x in (p, m, v, ms, vs)] + ([w.clone()] if master else [])
+        for a, b in cuts:
+            part = [x[a:b] if x.numel() == n else x[a // 256:-(-b // 256)] for x in got]
+            tl = E.TensorList([g[a:b]], p=[part[0]], m=[part[1]], v=[part[2]], m_scale=[part[3]], v_scale=[part[4]],
+                              master=[part[5]] if master else None, weight_decay=0.01)
+            E.ea_adamw_step(E.AdamW(eps=1e-8, state_bits=8, param_type=E.ea_type(param), grad_type=E.ea_type(param),
+                                    **HYPER), 5, tl)
+        outs.append(got)
+    for x, y in zip(*outs):
+        assert torch.equal(x.view(torch.uint8), y.view(torch.uint8))
+    # the faults reached the blocks they stand in, and no other
+    odd = torch.isnan(outs[0][3]).nonzero().view(-1).tolist()
+    first = (1 << 20) // 256
+    assert odd == [first + 0, first + 8 + 8 + 4 + 0, first + 24 + 6, first + 32 + 2], odd
+    # each block against the formula, around the faults and at the ends
+    m32 = lambda c, s, a, b: R.VALUES[c[a:b].cpu().numpy()].astype(np.float32) * \
+        np.repeat(s[a // 256:-(-b // 256)].cpu().numpy(), 256)[:b - a]  # noqa: E731
+    for a, b in ((0, 2048), ((1 << 20) - 2048, (1 << 20) + 8 * 2048), ((1 << 25) - 2048, n)):
+        with np.errstate(invalid="ignore"):
+            r0 = m32(v, vs, a, b)
+            start = (w if master else p)[a:b].float().cpu().numpy()
+            mk, rk, _, pk = R.adamw32(start, g[a:b].float().cpu().numpy(), m32(m, ms, a, b), r0 * r0, 5, eps=1e-8, wd=0.01,
+                                      **HYPER)
+        fine = ~np.repeat(np.isnan(R.pad(mk)).any(1) | np.isnan(R.pad(rk)).any(1), 256)[:b - a]
+        for codes, scales, x, roots in ((1, 3, mk, False), (2, 4, rk, True)):
+            want, s = R.encode32(np.where(fine, x, 0), roots)
+            got = outs[0][codes][a:b].cpu().numpy()
+            assert (got[fine] != want[fine]).sum() <= (2 if roots else 0)      # a root next to the border of two codes
+        got = outs[0][5 if master else 0][a:b].float().cpu().numpy()
+        bound = 2.0 ** -20 * np.abs(pk - start) + 2.0 ** -22 * np.maximum(np.abs(pk), np.abs(start))
+        if not master and kind == "bf16":
+            bound = bound + 2.0 ** -8 * np.abs(pk)
+        odd = np.isnan(pk)
+        assert np.array_equal(np.isnan(got), odd) and (np.abs(got - pk)[~odd] <= bound[~odd]).all()
