@@ -180,9 +180,12 @@ struct NormArgs {
 };
 static_assert(sizeof(NormArgs) + 32 <= 4096, "kernel arguments");
 
-// Gradients that one workgroup sums by itself.  On the GPU that takes 2.5 us (8,192 elements) to 5.1
-// (65,536 in four tensors) against 4.4 in two launches; issued from the host, 6.4 against 9.6.
-constexpr int kSmallParts = 4;
+// Gradients that one workgroup sums by itself, in one launch instead of two.  Issued from the host that
+// takes 5.9 us against 8.5 to 9.3 while the GPU keeps up, which it does for up to 8 tensors (12: up to 11 us)
+// and 131,072 elements in all (262,144: 9 to 14).  On the GPU alone (a graph) it takes 2 to 4 us against 3.4
+// to 4.4 for up to 4 tensors and 65,536 elements, and up to 1.6 us more than two launches between 5 and 8
+// tensors, 0.7 to 3.6 more at 131,072 elements: the limits keep what the host gains above what a graph loses.
+constexpr int kSmallParts = 8;
 constexpr int64_t kSmallTotal = 1 << 16;
 
 int64_t norm_chunk(int64_t total);

@@ -79,3 +79,20 @@ def test_norm_of_large_lists(sizes):
     ws = torch.empty(E.ea_grad_norm_workspace_bytes(tl), dtype=torch.uint8, device="cuda")
     E.ea_grad_norm(tl, 1.0, math.inf, norm, factor, ws)
     assert norm.item() == torch.tensor(math.sqrt(terms), dtype=torch.float32).item()   # integers: exact until the root
+
+
+@pytest.mark.parametrize("kind", [torch.float32, torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("count", [1, 4, 5, 8, 9, 12])
+@pytest.mark.parametrize("total", [60, 4_097, 65_536, 65_537])
+def test_norm_of_few_and_many_small_gradients(count, total, kind):
+    """On both sides of the limits for one launch; integers, so the sum of squares is exact."""
+    sizes = [total // count] * (count - 1)
+    sizes.append(total - sum(sizes))
+    gen = torch.Generator().manual_seed(total + count)
+    grads = [torch.randint(-4, 5, (n,), generator=gen).to(kind).cuda() for n in sizes] + [torch.empty(0, dtype=kind, device="cuda")]
+    want = math.sqrt(sum(int((g.double() ** 2).sum().item()) for g in grads))
+    tl = E.TensorList(grads)
+    norm, factor = torch.zeros(1, device="cuda"), torch.zeros(1, device="cuda")
+    ws = torch.empty(E.ea_grad_norm_workspace_bytes(tl), dtype=torch.uint8, device="cuda")
+    E.ea_grad_norm(tl, 1.0, math.inf, norm, factor, ws)
+    assert norm.item() == torch.tensor(want, dtype=torch.float32).item() and factor.item() == 1.0
