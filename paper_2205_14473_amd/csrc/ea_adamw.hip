@@ -291,10 +291,16 @@ __device__ __forceinline__ bool plain_square(float v)
     return !__builtin_amdgcn_classf(v, 0x003 | 0x004 | 0x010 | 0x080 | 0x200);
 }
 
-// Elements of a call below which a wave takes one group of blocks, above it
-// four with the next one's loads in flight (355M parameters: one 736 us, two 676,
-// four 661, eight 680; 11.7M: one 42, two 45, four 47).
-constexpr int64_t kShortRuns = 1 << 25;
+// A wave takes one group of blocks; where parameters and gradients have 16 bits
+// and no masters stand behind them, four from this many elements on (twice as
+// many with draws), with the next one's loads in flight: with few bytes in
+// flight a lane, waves that start and end leave HBM idle (both 16 bits, us for
+// one and four a wave: 2^23 elements 29.6 and 32.4, 2^25 76.8 and 73.3, 2^27 278
+// and 256; with draws 2^25 89.8 and 93.0, 2^26 170.6 and 167.3).  Others
+// have enough in flight and lose by the longer runs and their registers: 2^27 of
+// binary32 340 and 383, binary32 with bfloat16 gradients 303 and 333, bfloat16
+// with masters 352 and 384, with binary32 gradients 269 and 288.
+constexpr int64_t kLongRuns = 1 << 25;
 constexpr float kLeastEps = 0x1p-100f;   // outside these two, quotient's reciprocal could leave the
 constexpr float kMostEps = 0x1p100f;     // normal numbers
 constexpr float kMostOverEps = 0x1p120f; // first moments over eps from which it could overflow (and end as
@@ -335,7 +341,7 @@ __device__ __forceinline__ void store_states(const Adamw8Args& a, const Factors&
 // 10 bytes an element (bfloat16 parameters and gradients) against 200
 // instructions for 256 elements: vector issue is busy three quarters of the time
 // beside HBM at 5.4 TB/s, 355M parameters 656 us.  With stochastic rounding the
-// draws double the instructions: 11.7M 44 us, 4.3 TB/s (16 bytes an element).
+// draws double the instructions: 11.7M 41 us, 4.6 TB/s (16 bytes an element).
 //
 // This is the form for any values and any number of elements.
 template <class P, class G, bool DRAWS>
@@ -490,12 +496,13 @@ template <class P, class G, bool DRAWS, bool MASTER>
 __device__ __forceinline__ void adamw8_run(const Adamw8Args& a, const Factors& f, const Part8& e, uint32_t begin,
                                            uint32_t end)
 {
+    constexpr bool kSeveral = sizeof(P) == 2 && sizeof(G) == 2 && !MASTER;   // adamw_chunk's runs of four
     Held<P, G, MASTER> h, next;
     if (f.eps >= kLeastEps && f.eps <= kMostEps && end - begin >= kWaveElements) {
         fetch<P, G, MASTER>(e, begin, h);
         for (;;) {
             const uint32_t then = begin + kWaveElements;
-            const bool more = end - then >= kWaveElements;
+            const bool more = kSeveral && end - then >= kWaveElements;
             if (more) fetch<P, G, MASTER>(e, then, next);
             if (!adamw8_whole<P, G, DRAWS, MASTER>(a, f, e, begin, h)) adamw8_any<P, G, DRAWS>(a, f, e, begin);
             begin = then;
@@ -669,10 +676,12 @@ __global__ void __launch_bounds__(kFinishBlock) norm_small_kernel(NormArgs a, fl
 
 }  // namespace
 
-uint32_t adamw_chunk(const ea_adamw_t& c, int64_t total)
+uint32_t adamw_chunk(const ea_adamw_t& c, int64_t total, bool masters)
 {
     if (c.state_bits == 32) return kAdamwBlock * 4;
-    return kWavesPerBlock * kWaveElements * (total < kShortRuns ? 1 : 4);
+    const bool light = c.param_type != EA_F32 && c.grad_type != EA_F32 && !masters;
+    const bool many = total >= (c.rounding == EA_ROUND_STOCHASTIC ? 2 * kLongRuns : kLongRuns);
+    return kWavesPerBlock * kWaveElements * (light && many ? 4 : 1);
 }
 
 hipError_t launch_adamw(const Adamw32Args& a, const ea_adamw_t& c, hipStream_t s)

@@ -159,8 +159,8 @@ __host__ __device__ inline float adamw_keep(double lri, float wd)
     return (float)(1.0 - lri * (double)wd);
 }
 
-// Elements per workgroup of a call of `total` elements: what `first` counts in.
-uint32_t adamw_chunk(const ea_adamw_t& c, int64_t total);
+// Elements per workgroup of a call of `total` elements, some with masters or none: what `first` counts in.
+uint32_t adamw_chunk(const ea_adamw_t& c, int64_t total, bool masters);
 hipError_t launch_adamw(const Adamw32Args& a, const ea_adamw_t& c, hipStream_t s);
 hipError_t launch_adamw(const Adamw8Args& a, const ea_adamw_t& c, hipStream_t s);
 

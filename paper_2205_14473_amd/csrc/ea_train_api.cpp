@@ -159,7 +159,9 @@ hipError_t adamw_launches(const ea_adamw_t& c, const ea_schedule_t* s, int64_t t
     a.t_dev = t_dev;
     if (!t_dev) a.root = ea::adamw_root(c.beta2, a.t);
     if (s) a.sched = *s;
-    a.chunk = ea::adamw_chunk(c, total);
+    bool masters = false;
+    for (int32_t i = 0; i < ntensors; ++i) masters |= tensors[i].master != nullptr;
+    a.chunk = ea::adamw_chunk(c, total, masters);
     const int64_t state = c.state_bits / 8;
     const int64_t gb = (int64_t)type_bytes(c.grad_type), pb = (int64_t)type_bytes(c.param_type);
     hipError_t e = hipSuccess;
