@@ -778,8 +778,12 @@ hipError_t start_grad(const ea_embed_t& c, const GradPlan& p, const void* ids, c
     return hipGetLastError();
 }
 
-// Tokens below which a group takes one (R = 1): 16 tokens are 7 us either way, the call.
-constexpr int64_t kOneByOne = 8192;
+// A group of lanes takes four tokens where they fill the GPU: from 3M elements and 4,096 tokens on; otherwise
+// one.  Binary32, us on the GPU for one and four: 8,192 tokens of 64 columns 2.2 and 3.1, 32,768 3.6 and 4.0,
+// 4,096 of 256 2.7 and 3.3, of 768 4.9 and 4.5, 8,192 of 1,024 11.5 and 10.5, 65,536 97 and 76; few and wide,
+// 1,024 of 4,096 5.4 and 6.8, 4,096 of them 21.1 and 21.2.  The 16-bit types cross between 2.1M and 4.2M alike.
+constexpr int64_t kFourElements = 3 << 20;
+constexpr int64_t kFourTokens = 4096;
 
 // f(table element, row element) with the types that c names.
 template <class F, class T>
@@ -807,7 +811,7 @@ hipError_t launch_embed_lookup(const ea_embed_t& c, const void* table, const voi
     return with_types(c, [&](auto t, auto e) {
         using T = decltype(t);
         using X = decltype(e);
-        if (c.tokens < kOneByOne)
+        if (c.tokens < kFourTokens || c.tokens * c.dim < kFourElements)
             hipLaunchKernelGGL((lookup_kernel<T, X, 1>), dim3(row_groups(c.tokens, gbits)), dim3(kRowBlock), 0, s, c,
                                (const T*)table, ids, (X*)x, gbits);
         else
