@@ -82,7 +82,9 @@ __global__ void __launch_bounds__(kRowBlock) lookup_kernel(ea_embed_t c, const T
 
 // The table's rows as lines of bytes (one line where no elements lie between
 // rows), zeroed in units of 16 by workgroups that ride along with the sort's:
-// the sort is latency, and the zeros are bandwidth.
+// the sort is latency, and the zeros are bandwidth.  (Lines by a division each:
+// 50,257 rows of 1,024 binary32 columns in one line 26.3 us, with 32 elements
+// between them 26.8, with 5 and so off the 16-byte grid 28.2.)
 struct Fill {
     char* base;
     int64_t line, pitch;                 // bytes of a line, and to the next
@@ -489,7 +491,7 @@ __global__ void __launch_bounds__(kRowBlock) sum_kernel(SumArgs a, const X* dx, 
     if (c >= a.chunks) return;
     const int64_t begin = c * a.chunk;
     const int count = (int)(a.n - begin < a.chunk ? a.n - begin : a.chunk);
-    // lane l: position l; lane `count`'s key ends the last run
+    // lane l: position l; the keys beside the chunk say whether its first and last runs go on there
     const uint32_t none = 0xFFFFFFFFu;
     const int64_t mine = begin + (lane < count ? lane : count - 1);
     const uint32_t key = a.keys[mine], at = a.at[mine];
