@@ -4,7 +4,9 @@ The work runs in ``libea.so`` (hand-written HIP kernels for gfx950 behind the
 C ABI of ``include/ea.h``); this package only binds it.  ``state`` allocates
 the device buffers one round needs (PyTorch provides memory and streams).
 Beside the round, ``include/ea_train.h`` holds AdamW over many tensors, the
-global gradient norm, and the embedding lookup with its gradient.
+global gradient norm, and the embedding lookup with its gradient, and
+``include/ea_layer.h`` layer norm, dropout, the gated linear recurrence and the
+token loss with theirs.
 
 The binding is loaded on first use of any of its names, so that the ``build``
 submodule can be imported (and the library compiled) before the library
@@ -28,7 +30,15 @@ _TRAIN_EXPORTS = (
     "ea_adamw_step", "ea_adamw_step_scheduled", "ea_grad_norm", "ea_grad_norm_workspace_bytes",
     "ea_embed_lookup", "ea_embed_grad", "ea_embed_workspace_bytes",
 )
-__all__ = list(_EXPORTS + _TRAIN_EXPORTS)
+# The layers' operators (include/ea_layer.h).
+_LAYER_EXPORTS = (
+    "EA_GATE_PLAIN", "EA_GATE_SIGMOID", "EA_RECURRENCE_BLOCK", "EA_REDUCE_MEAN", "EA_REDUCE_SUM",
+    "LayerNorm", "Dropout", "Recurrence", "TokenLoss",
+    "ea_layer_norm", "ea_layer_norm_grad", "ea_layer_norm_workspace_bytes", "ea_dropout", "ea_dropout_grad",
+    "ea_recurrence", "ea_recurrence_grad", "ea_recurrence_states_bytes", "ea_recurrence_workspace_bytes",
+    "ea_token_loss", "ea_token_loss_workspace_bytes",
+)
+__all__ = list(_EXPORTS + _TRAIN_EXPORTS + _LAYER_EXPORTS)
 
 
 def __getattr__(name):
@@ -38,8 +48,11 @@ def __getattr__(name):
     if name in _TRAIN_EXPORTS:
         from . import _train
         return getattr(_train, name)
+    if name in _LAYER_EXPORTS:
+        from . import _layer
+        return getattr(_layer, name)
     raise AttributeError(f"module {__name__!r} has no attribute {name!r}")
 
 
 def __dir__():
-    return sorted(list(globals()) + list(_EXPORTS + _TRAIN_EXPORTS))
+    return sorted(list(globals()) + list(_EXPORTS + _TRAIN_EXPORTS + _LAYER_EXPORTS))

@@ -1,0 +1,182 @@
+// ea_layer.hpp -- vectors of elements, reductions and launchers of the layers'
+// operators (ea_layer.h).
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "ea_device.hpp"
+#include "ea_layer.h"
+#include "ea_train.hpp"
+
+namespace ea {
+
+// ---- vectors of N elements --------------------------------------------------
+
+// N consecutive elements of type T at an address aligned to one element.
+template <class T, int N>
+struct VecOf {
+    typedef T vec __attribute__((ext_vector_type(N)));
+    typedef vec unaligned __attribute__((aligned(sizeof(T))));
+};
+template <class T>
+struct VecOf<T, 1> {
+    typedef T vec;
+    typedef T unaligned;
+};
+template <class T, int N>
+using Vec = typename VecOf<T, N>::vec;
+
+template <int N, class T>
+__device__ __forceinline__ Vec<T, N> load_vec(const T* p)
+{
+    return *(const typename VecOf<T, N>::unaligned*)p;
+}
+
+template <int N, class T>
+__device__ __forceinline__ void store_vec(T* p, Vec<T, N> v)
+{
+    *(typename VecOf<T, N>::unaligned*)p = v;
+}
+
+// The same for data that a pass reads or writes once: it leaves the caches to others.
+template <int N, class T>
+__device__ __forceinline__ Vec<T, N> load_vec_once(const T* p)
+{
+    return __builtin_nontemporal_load((const typename VecOf<T, N>::unaligned*)p);
+}
+
+template <int N, class T>
+__device__ __forceinline__ void store_vec_once(T* p, Vec<T, N> v)
+{
+    __builtin_nontemporal_store(v, (typename VecOf<T, N>::unaligned*)p);
+}
+
+// Element k of a vector, also of one of a single element.
+template <int N, class T>
+__device__ __forceinline__ T element(const Vec<T, N>& v, int k)
+{
+    if constexpr (N == 1)
+        return v;
+    else
+        return v[k];
+}
+
+template <int N, class T>
+__device__ __forceinline__ void set_element(Vec<T, N>& v, int k, T x)
+{
+    if constexpr (N == 1)
+        v = x;
+    else
+        v[k] = x;
+}
+
+// The first `n` (0 to N) elements; the rest read as `rest`, and are not written.
+template <int N, class T>
+__device__ __forceinline__ Vec<T, N> load_part(const T* p, int n, float rest = 0.0f)
+{
+    Vec<T, N> v;
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+        T x = (T)rest;
+        if (k < n) x = p[k];
+        set_element<N, T>(v, k, x);
+    }
+    return v;
+}
+
+template <int N, class T>
+__device__ __forceinline__ void store_part(T* p, Vec<T, N> v, int n)
+{
+#pragma unroll
+    for (int k = 0; k < N; ++k)
+        if (k < n) p[k] = element<N, T>(v, k);
+}
+
+template <int N, class T>
+__device__ __forceinline__ void widen_to(float* x, const Vec<T, N>& v)
+{
+#pragma unroll
+    for (int k = 0; k < N; ++k) x[k] = (float)element<N, T>(v, k);
+}
+
+template <int N, class T>
+__device__ __forceinline__ Vec<T, N> narrow_from(const float* x)
+{
+    Vec<T, N> v;
+#pragma unroll
+    for (int k = 0; k < N; ++k) set_element<N, T>(v, k, (T)x[k]);
+    return v;
+}
+
+// One element of a tensor whose type is known when it runs only, for what is read once per column.
+__device__ __forceinline__ float element_at(const void* p, int32_t type, int64_t i)
+{
+    if (type == EA_F32) return ((const float*)p)[i];
+    if (type == EA_BF16) return (float)((const bf16*)p)[i];
+    return (float)((const f16*)p)[i];
+}
+
+__device__ __forceinline__ void set_element_at(void* p, int32_t type, int64_t i, float x)
+{
+    if (type == EA_F32)
+        ((float*)p)[i] = x;
+    else if (type == EA_BF16)
+        ((bf16*)p)[i] = (bf16)x;
+    else
+        ((f16*)p)[i] = (f16)x;
+}
+
+// ---- reductions ---------------------------------------------------------------
+
+// All 64 lanes end with the same bits.
+__device__ __forceinline__ float wave_sum(float v)
+{
+    v = v + __uint_as_float(dpp<kDppXor1>(__float_as_uint(v)));
+    v = v + __uint_as_float(dpp<kDppXor2>(__float_as_uint(v)));
+    v = v + __uint_as_float(dpp<kDppHalfMirror>(__float_as_uint(v)));
+    v = v + __uint_as_float(dpp<kDppRowMirror>(__float_as_uint(v)));
+    uint32_t a, b;
+    row_swap16(__float_as_uint(v), a, b);
+    v = __uint_as_float(a) + __uint_as_float(b);
+    row_swap32(__float_as_uint(v), a, b);
+    return __uint_as_float(a) + __uint_as_float(b);
+}
+
+// ---- types at run time ----------------------------------------------------------
+
+// f with a value of the element type: f(float{}), f(bf16{}) or f(f16{}).
+template <class F>
+hipError_t with_type(int32_t type, F&& f)
+{
+    if (type == EA_F32) return f(float{});
+    if (type == EA_BF16) return f(bf16{});
+    return f(f16{});
+}
+
+// ---- launchers ------------------------------------------------------------------
+
+hipError_t launch_layer_norm(const ea_layer_norm_t& c, const void* x, const void* weight, const void* bias, void* y,
+                             float* mean, float* rstd, hipStream_t s);
+int64_t layer_norm_workspace_bytes(const ea_layer_norm_t& c);
+hipError_t launch_layer_norm_grad(const ea_layer_norm_t& c, const void* x, const void* dy, const void* weight,
+                                  const float* mean, const float* rstd, const void* add, void* dx, void* dweight,
+                                  void* dbias, bool accumulate, void* workspace, hipStream_t s);
+
+// residual is NULL for the gradient, whose dy takes x's place (in_type the type of what is read).
+hipError_t launch_dropout(const ea_dropout_t& c, bool backward, uint32_t t, const uint32_t* t_dev, const void* in,
+                          const void* residual, void* out, hipStream_t s);
+
+int64_t recurrence_workspace_bytes(const ea_recurrence_t& c);
+hipError_t launch_recurrence(const ea_recurrence_t& c, const void* g, const void* x, const float* h0,
+                             const int32_t* lengths, void* y, float* states, float* h_last, void* workspace,
+                             hipStream_t s);
+hipError_t launch_recurrence_grad(const ea_recurrence_t& c, const void* g, const void* x, const float* states,
+                                  const int32_t* lengths, const void* dy, const float* dh_last, void* dg, void* dx,
+                                  float* dh0, void* workspace, hipStream_t s);
+
+int64_t token_loss_workspace_bytes(const ea_token_loss_t& c);
+hipError_t launch_token_loss(const ea_token_loss_t& c, const void* logits, const void* targets, float* loss,
+                             float* total, int32_t* count, void* dlogits, void* workspace, hipStream_t s);
+
+}  // namespace ea

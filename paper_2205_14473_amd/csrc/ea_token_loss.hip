@@ -1,0 +1,345 @@
+// ea_token_loss.hip -- cross-entropy of tokens and its gradient in one pass over
+// the logits.
+//
+// A row is held in registers, as it is stored, by 1, 4 or 16 waves: its largest
+// logit and the sum of exponentials are reductions, and the gradient leaves the
+// same registers.  Longer rows are read twice.  The mean's gradient needs the
+// number of tokens that count first: a workgroup counts few targets itself, many
+// are counted by a launch of their own.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include <type_traits>
+
+#include "ea_layer.hpp"
+
+namespace ea {
+
+namespace {
+
+constexpr float kLog2e = 0x1.715476p+0f;
+constexpr int kCountBlock = 1024;
+constexpr int64_t kMostCounts = 256;                   // workgroups that count
+constexpr int64_t kOwnCount = 4096;                    // targets that every workgroup counts by itself
+constexpr int64_t kMostGroups = 2048;                  // workgroups of the main pass, each with a sum of its own
+constexpr int kEndBlock = 256;
+
+// Workspace: the counting groups' counts, then each main group's sum and count.
+struct Sums {
+    double loss;
+    int64_t count;
+};
+static_assert(sizeof(Sums) == 16, "the workspace's layout");
+
+struct Loss {
+    ea_token_loss_t c;
+    const void* targets;
+    float* loss;
+    int64_t* counts;                                   // of `parts` groups, or NULL: the targets are few
+    Sums* sums;
+    int32_t parts;
+};
+
+__device__ __forceinline__ int64_t target_at(const Loss& a, int64_t row)
+{
+    const int64_t t = a.c.index_bits == 64 ? ((const int64_t*)a.targets)[row] : (int64_t)((const int32_t*)a.targets)[row];
+    return t >= 0 && t < a.c.vocab ? t : -1;
+}
+
+// The workgroup's sum of integers; every thread gets it.
+template <int THREADS>
+__device__ __forceinline__ int64_t group_count(int64_t v)
+{
+    __shared__ int64_t lds[THREADS / kWave];
+    for (int k = kWave / 2; k > 0; k /= 2) v += __shfl_xor(v, k);
+    if (lane_id() == 0) lds[threadIdx.x / kWave] = v;
+    __syncthreads();
+    v = 0;
+    for (int k = 0; k < THREADS / kWave; ++k) v += lds[k];
+    __syncthreads();
+    return v;
+}
+
+__global__ void __launch_bounds__(kCountBlock) count_kernel(Loss a)
+{
+    int64_t n = 0;
+    for (int64_t i = (int64_t)blockIdx.x * kCountBlock + threadIdx.x; i < a.c.rows; i += (int64_t)gridDim.x * kCountBlock)
+        n += target_at(a, i) >= 0;
+    n = group_count<kCountBlock>(n);
+    if (threadIdx.x == 0) a.counts[blockIdx.x] = n;
+}
+
+// What the gradient of a row that counts is multiplied by.
+template <int THREADS>
+__device__ __forceinline__ float row_factor(const Loss& a)
+{
+    if (a.c.reduction == EA_REDUCE_SUM) return a.c.scale;
+    int64_t n = 0;
+    if (a.counts) {
+        for (int i = threadIdx.x; i < a.parts; i += THREADS) n += a.counts[i];
+    } else {
+        for (int64_t i = threadIdx.x; i < a.c.rows; i += THREADS) n += target_at(a, i) >= 0;
+    }
+    n = group_count<THREADS>(n);
+    return n > 0 ? (float)((double)a.c.scale / (double)n) : 0.0f;
+}
+
+template <int WAVES>
+__device__ __forceinline__ float group_max(float v, float* lds)
+{
+    v = wave_max(v);
+    if (WAVES == 1) return v;
+    if (lane_id() == 0) lds[threadIdx.x / kWave] = v;
+    __syncthreads();
+    v = lds[0];
+#pragma unroll
+    for (int k = 1; k < WAVES; ++k) v = fmaxf(v, lds[k]);
+    return v;
+}
+
+template <int WAVES>
+__device__ __forceinline__ float group_sum(float v, float* lds)
+{
+    v = wave_sum(v);
+    if (WAVES == 1) return v;
+    if (lane_id() == 0) lds[threadIdx.x / kWave] = v;
+    __syncthreads();
+    v = 0.0f;
+#pragma unroll
+    for (int k = 0; k < WAVES; ++k) v = v + lds[k];
+    return v;
+}
+
+// e^(z - top): the difference is rounded before it is scaled, so that a logit near the largest loses nothing.
+__device__ __forceinline__ float exp_under(float z, float top)
+{
+    return __builtin_amdgcn_exp2f((z - top) * kLog2e);
+}
+
+template <int V, class T>
+__device__ __forceinline__ void zero_row(T* to, int64_t vocab, int lane, int lanes)
+{
+    const float none[V] = {};
+    for (int64_t at = (int64_t)lane * V; at < vocab; at += (int64_t)lanes * V) {
+        if (vocab - at >= V)
+            store_vec<V>(to + at, narrow_from<V, T>(none));
+        else
+            store_part<V>(to + at, narrow_from<V, T>(none), (int)(vocab - at));
+    }
+}
+
+// WAVES of a row (1: four rows a workgroup), K vectors of 16 bytes a lane; K = 0: a row that is read again.
+template <class T, int WAVES, int K, bool GRAD>
+__global__ void __launch_bounds__(WAVES == 1 ? 256 : WAVES * kWave)
+    loss_kernel(Loss a, const T* logits, T* dlogits)
+{
+    constexpr int V = 16 / sizeof(T), kRows = WAVES == 1 ? 4 : 1, kLanes = WAVES * kWave;
+    constexpr int kThreads = WAVES == 1 ? 256 : kLanes;
+    __shared__ float lds[2][WAVES], hit_of[kRows];
+    const int lane = WAVES == 1 ? lane_id() : (int)threadIdx.x;
+    const int64_t vocab = a.c.vocab;
+    const float factor = GRAD ? row_factor<kThreads>(a) : 0.0f;
+    double total = 0.0;
+    int64_t used = 0;
+    for (int64_t row = (int64_t)blockIdx.x * kRows + (WAVES == 1 ? threadIdx.x / kWave : 0); row < a.c.rows;
+         row += (int64_t)gridDim.x * kRows) {
+        const int64_t target = target_at(a, row);
+        const T* from = logits + row * a.c.logits_stride;
+        T* to = dlogits + row * a.c.dlogits_stride;
+        if (target < 0) {
+            if (lane == 0 && a.loss) a.loss[row] = 0.0f;
+            if (GRAD) zero_row<V>(to, vocab, lane, kLanes);
+            continue;
+        }
+        float top = -__builtin_inff(), sum = 0.0f;
+        Vec<T, V> z[K ? K : 1];
+        if constexpr (K > 0) {
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
+                const int64_t at = ((int64_t)k * kLanes + lane) * V, left = vocab - at;
+                z[k] = left >= V ? load_vec<V>(from + at) : load_part<V>(from + at, left > 0 ? (int)left : 0, -__builtin_inff());
+            }
+#pragma unroll
+            for (int k = 0; k < K; ++k)
+#pragma unroll
+                for (int i = 0; i < V; ++i) top = fmaxf(top, (float)z[k][i]);
+        } else {
+            for (int64_t at = (int64_t)lane * V; at < vocab; at += kLanes * V) {
+                const int64_t left = vocab - at;
+                z[0] = left >= V ? load_vec<V>(from + at) : load_part<V>(from + at, (int)left, -__builtin_inff());
+#pragma unroll
+                for (int i = 0; i < V; ++i) top = fmaxf(top, (float)z[0][i]);
+            }
+        }
+        // The target's logit, from one lane before the last reduction: when rows are written where they were read,
+        // no lane may still want it after that.
+        if (lane == 0) hit_of[WAVES == 1 ? threadIdx.x / kWave : 0] = (float)from[target];
+        top = group_max<WAVES>(top, lds[0]);
+        if constexpr (K > 0) {
+#pragma unroll
+            for (int k = 0; k < K; ++k)
+#pragma unroll
+                for (int i = 0; i < V; ++i) sum = sum + exp_under((float)z[k][i], top);
+        } else {
+            for (int64_t at = (int64_t)lane * V; at < vocab; at += kLanes * V) {
+                const int64_t left = vocab - at;
+                z[0] = left >= V ? load_vec<V>(from + at) : load_part<V>(from + at, (int)left, -__builtin_inff());
+#pragma unroll
+                for (int i = 0; i < V; ++i) sum = sum + exp_under((float)z[0][i], top);
+            }
+        }
+        sum = group_sum<WAVES>(sum, lds[1]);
+        const float loss = logf(sum) - (hit_of[WAVES == 1 ? threadIdx.x / kWave : 0] - top);
+        total = total + (double)loss;
+        ++used;
+        if (lane == 0 && a.loss) a.loss[row] = loss;
+        if constexpr (GRAD) {
+            const float share = factor / sum;
+            auto out = [&](Vec<T, V> v, int64_t at) {
+                float d[V];
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+                    d[i] = exp_under((float)v[i], top) * share;
+                    if (at + i == target) d[i] = d[i] - factor;
+                }
+                if (vocab - at >= V)
+                    store_vec<V>(to + at, narrow_from<V, T>(d));
+                else
+                    store_part<V>(to + at, narrow_from<V, T>(d), vocab > at ? (int)(vocab - at) : 0);
+            };
+            if constexpr (K > 0) {
+#pragma unroll
+                for (int k = 0; k < K; ++k) out(z[k], ((int64_t)k * kLanes + lane) * V);
+            } else {
+                for (int64_t at = (int64_t)lane * V; at < vocab; at += kLanes * V) {
+                    const int64_t left = vocab - at;
+                    out(left >= V ? load_vec<V>(from + at) : load_part<V>(from + at, (int)left), at);
+                }
+            }
+        }
+        if (WAVES > 1) __syncthreads();                // the next row's reductions write where this one's were read
+    }
+    // one sum for each row's group of waves
+    if (lane == 0) a.sums[(int64_t)blockIdx.x * kRows + (WAVES == 1 ? threadIdx.x / kWave : 0)] = Sums{total, used};
+}
+
+// The groups' sums, in their order.
+__global__ void __launch_bounds__(kEndBlock) loss_end_kernel(Loss a, int64_t groups, float* total, int32_t* count)
+{
+    __shared__ double sums[kEndBlock];
+    double sum = 0.0;
+    int64_t used = 0;
+    for (int64_t i = threadIdx.x; i < groups; i += kEndBlock) {
+        sum = sum + a.sums[i].loss;
+        used += a.sums[i].count;
+    }
+    used = group_count<kEndBlock>(used);
+    sums[threadIdx.x] = sum;
+    __syncthreads();
+    for (int half = kEndBlock / 2; half > 0; half /= 2) {
+        if ((int)threadIdx.x < half) sums[threadIdx.x] = sums[threadIdx.x] + sums[threadIdx.x + half];
+        __syncthreads();
+    }
+    if (threadIdx.x > 0) return;
+    sum = sums[0];
+    if (a.c.reduction == EA_REDUCE_MEAN && used > 0) sum = sum / (double)used;
+    *total = (float)sum;
+    if (count) *count = (int32_t)used;
+}
+
+int64_t at_most(int64_t n, int64_t most)
+{
+    return n < most ? n : most;
+}
+
+// Waves of a row and vectors a lane: the smallest that hold it, or 16 and 0 where none does.
+struct Shape {
+    int waves, k;
+};
+
+Shape shape_of(const ea_token_loss_t& c)
+{
+    const int64_t v = c.type == EA_F32 ? 4 : 8;
+    const Shape all[] = {{1, 2}, {1, 4}, {4, 2}, {4, 4}, {16, 2}, {16, 4}, {16, 6}, {16, 8}, {16, 12}, {16, 16}};
+    for (const Shape& s : all)
+        if (c.vocab <= v * kWave * s.waves * s.k) return s;
+    return {16, 0};
+}
+
+// Workgroups of the main pass, and the sums they leave.
+int64_t groups_of(const ea_token_loss_t& c, Shape s)
+{
+    return s.waves == 1 ? at_most((c.rows + 3) / 4, kMostGroups) : at_most(c.rows, kMostGroups);
+}
+
+int64_t sums_of(const ea_token_loss_t& c, Shape s)
+{
+    return groups_of(c, s) * (s.waves == 1 ? 4 : 1);
+}
+
+int64_t counting_groups(const ea_token_loss_t& c)
+{
+    return c.rows > kOwnCount ? at_most((c.rows + kCountBlock * 4 - 1) / (kCountBlock * 4), kMostCounts) : 0;
+}
+
+template <class T, bool GRAD>
+hipError_t start_loss(const Loss& a, Shape s, unsigned groups, const void* logits, void* dlogits, hipStream_t st)
+{
+#define EA_SHAPE(W, K)                                                                                            \
+    if (s.waves == W && s.k == K) {                                                                               \
+        hipLaunchKernelGGL((loss_kernel<T, W, K, GRAD>), dim3(groups), dim3(W == 1 ? 256 : W * kWave), 0, st, a,  \
+                           (const T*)logits, (T*)dlogits);                                                        \
+        return hipGetLastError();                                                                                 \
+    }
+    EA_SHAPE(1, 2)
+    EA_SHAPE(1, 4)
+    EA_SHAPE(4, 2)
+    EA_SHAPE(4, 4)
+    EA_SHAPE(16, 2)
+    EA_SHAPE(16, 4)
+    EA_SHAPE(16, 6)
+    EA_SHAPE(16, 8)
+    EA_SHAPE(16, 12)
+    EA_SHAPE(16, 16)
+    EA_SHAPE(16, 0)
+#undef EA_SHAPE
+    return hipErrorInvalidValue;
+}
+
+}  // namespace
+
+int64_t token_loss_workspace_bytes(const ea_token_loss_t& c)
+{
+    return counting_groups(c) * 16 + sums_of(c, shape_of(c)) * 16;
+}
+
+hipError_t launch_token_loss(const ea_token_loss_t& c, const void* logits, const void* targets, float* loss,
+                             float* total, int32_t* count, void* dlogits, void* workspace, hipStream_t s)
+{
+    const Shape shape = shape_of(c);
+    const int64_t parts = counting_groups(c);
+    Loss a{};
+    a.c = c;
+    a.targets = targets;
+    a.loss = loss;
+    a.sums = (Sums*)((char*)workspace + parts * 16);
+    hipError_t e = hipSuccess;
+    if (dlogits && c.reduction == EA_REDUCE_MEAN && parts > 0) {
+        a.counts = (int64_t*)workspace;
+        a.parts = (int32_t)parts;
+        hipLaunchKernelGGL(count_kernel, dim3((unsigned)parts), dim3(kCountBlock), 0, s, a);
+        e = hipGetLastError();
+    }
+    if (e == hipSuccess && c.rows > 0)
+        e = with_type(c.type, [&](auto t) {
+            using T = decltype(t);
+            const unsigned groups = (unsigned)groups_of(c, shape);
+            return dlogits ? start_loss<T, true>(a, shape, groups, logits, dlogits, s)
+                           : start_loss<T, false>(a, shape, groups, logits, dlogits, s);
+        });
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(loss_end_kernel, dim3(1), dim3(kEndBlock), 0, s, a, sums_of(c, shape), total, count);
+    return hipGetLastError();
+}
+
+}  // namespace ea
