@@ -86,7 +86,8 @@ __device__ __forceinline__ int steps_at(int64_t t, int64_t n)
     return left >= kSteps ? kSteps : left > 0 ? (int)left : 0;
 }
 
-// a and w of a gate.  1 / (1 + e) and e / (1 + e) with e = exp(-|g|) keep both to their last places.
+// a and w of a gate: 1 / (1 + e) and e / (1 + e) with e = exp(-|g|).  The reciprocal gets a correction step: gates near
+// 1 are multiplied over hundreds of steps, where a unit each would add up.
 template <bool SIGMOID>
 __device__ __forceinline__ void gate_of(float g, float& a, float& w)
 {
@@ -96,7 +97,8 @@ __device__ __forceinline__ void gate_of(float g, float& a, float& w)
         return;
     }
     const float e = __builtin_amdgcn_exp2f(-fabsf(g) * 0x1.715476p+0f);
-    const float r = __builtin_amdgcn_rcpf(1.0f + e), s = e * r;
+    const float d = 1.0f + e, q = __builtin_amdgcn_rcpf(d);
+    const float r = __builtin_fmaf(__builtin_fmaf(-d, q, 1.0f), q, q), s = e * r;
     a = g < 0.0f ? s : r;
     w = g < 0.0f ? r : s;
 }

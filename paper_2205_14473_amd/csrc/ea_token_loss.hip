@@ -110,22 +110,56 @@ __device__ __forceinline__ float group_sum(float v, float* lds)
     return v;
 }
 
-// e^(z - top): the difference is rounded before it is scaled, so that a logit near the largest loses nothing.
+// e^(z - top): the difference is rounded before it is scaled, so that logits near the largest, and large ones, lose
+// nothing.
 __device__ __forceinline__ float exp_under(float z, float top)
 {
     return __builtin_amdgcn_exp2f((z - top) * kLog2e);
 }
 
-template <int V, class T>
-__device__ __forceinline__ void zero_row(T* to, int64_t vocab, int lane, int lanes)
+// Four words of a row made opaque: what a pass made of them (as floats, and their exponentials) is made anew by the
+// next one.  Kept, it would take two to four times the registers of the row itself.
+typedef uint32_t Words __attribute__((ext_vector_type(4)));
+typedef Words WordsAt __attribute__((aligned(2)));
+
+__device__ __forceinline__ void renew(Words& w)
 {
+    asm volatile("" : "+v"(w));
+}
+
+template <class T>
+__device__ __forceinline__ void as_floats(float* x, Words w)
+{
+    constexpr int V = 16 / sizeof(T);
+    widen_to<V, T>(x, __builtin_bit_cast(Vec<T, V>, w));
+}
+
+template <class T>
+__device__ __forceinline__ Words load_words(const T* row, int at, int vocab)
+{
+    constexpr int V = 16 / sizeof(T);
+    const int left = vocab - at;
+    if (left >= V) return *(const WordsAt*)(row + (uint32_t)at);
+    return __builtin_bit_cast(Words, load_part<V>(row + at, left, -__builtin_inff()));
+}
+
+template <class T>
+__device__ __forceinline__ void store_floats_of(T* row, int at, int vocab, const float* x)
+{
+    constexpr int V = 16 / sizeof(T);
+    const int left = vocab - at;
+    if (left >= V)
+        store_vec<V>(row + (uint32_t)at, narrow_from<V, T>(x));
+    else
+        store_part<V>(row + at, narrow_from<V, T>(x), left);
+}
+
+template <class T>
+__device__ __forceinline__ void zero_row(T* to, int vocab, int lane, int lanes)
+{
+    constexpr int V = 16 / sizeof(T);
     const float none[V] = {};
-    for (int64_t at = (int64_t)lane * V; at < vocab; at += (int64_t)lanes * V) {
-        if (vocab - at >= V)
-            store_vec<V>(to + at, narrow_from<V, T>(none));
-        else
-            store_part<V>(to + at, narrow_from<V, T>(none), (int)(vocab - at));
-    }
+    for (int at = lane * V; at < vocab; at += lanes * V) store_floats_of(to, at, vocab, none);
 }
 
 // WAVES of a row (1: four rows a workgroup), K vectors of 16 bytes a lane; K = 0: a row that is read again.
@@ -137,7 +171,7 @@ __global__ void __launch_bounds__(WAVES == 1 ? 256 : WAVES * kWave)
     constexpr int kThreads = WAVES == 1 ? 256 : kLanes;
     __shared__ float lds[2][WAVES], hit_of[kRows];
     const int lane = WAVES == 1 ? lane_id() : (int)threadIdx.x;
-    const int64_t vocab = a.c.vocab;
+    const int vocab = (int)a.c.vocab;
     const float factor = GRAD ? row_factor<kThreads>(a) : 0.0f;
     double total = 0.0;
     int64_t used = 0;
@@ -148,74 +182,57 @@ __global__ void __launch_bounds__(WAVES == 1 ? 256 : WAVES * kWave)
         T* to = dlogits + row * a.c.dlogits_stride;
         if (target < 0) {
             if (lane == 0 && a.loss) a.loss[row] = 0.0f;
-            if (GRAD) zero_row<V>(to, vocab, lane, kLanes);
+            if (GRAD) zero_row(to, vocab, lane, kLanes);
             continue;
         }
-        float top = -__builtin_inff(), sum = 0.0f;
-        Vec<T, V> z[K ? K : 1];
+        float top = -__builtin_inff(), sum = 0.0f, x[V];
+        Words z[K ? K : 1];
+        // f(vector, its first column) for each of the lane's vectors, from its registers or from memory again
+        auto every = [&](auto&& f) {
+            if constexpr (K > 0) {
+#pragma unroll
+                for (int k = 0; k < K; ++k) {
+                    renew(z[k]);
+                    f(z[k], (k * kLanes + lane) * V);
+                }
+            } else {
+                for (int at = lane * V; at < vocab; at += kLanes * V) f(load_words(from, at, vocab), at);
+            }
+        };
         if constexpr (K > 0) {
 #pragma unroll
-            for (int k = 0; k < K; ++k) {
-                const int64_t at = ((int64_t)k * kLanes + lane) * V, left = vocab - at;
-                z[k] = left >= V ? load_vec<V>(from + at) : load_part<V>(from + at, left > 0 ? (int)left : 0, -__builtin_inff());
-            }
-#pragma unroll
-            for (int k = 0; k < K; ++k)
-#pragma unroll
-                for (int i = 0; i < V; ++i) top = fmaxf(top, (float)z[k][i]);
-        } else {
-            for (int64_t at = (int64_t)lane * V; at < vocab; at += kLanes * V) {
-                const int64_t left = vocab - at;
-                z[0] = left >= V ? load_vec<V>(from + at) : load_part<V>(from + at, (int)left, -__builtin_inff());
-#pragma unroll
-                for (int i = 0; i < V; ++i) top = fmaxf(top, (float)z[0][i]);
-            }
+            for (int k = 0; k < K; ++k) z[k] = load_words(from, (k * kLanes + lane) * V, vocab);
         }
         // The target's logit, from one lane before the last reduction: when rows are written where they were read,
         // no lane may still want it after that.
         if (lane == 0) hit_of[WAVES == 1 ? threadIdx.x / kWave : 0] = (float)from[target];
+        every([&](Words w, int) {
+            as_floats<T>(x, w);
+#pragma unroll
+            for (int i = 0; i < V; ++i) top = fmaxf(top, x[i]);
+        });
         top = group_max<WAVES>(top, lds[0]);
-        if constexpr (K > 0) {
+        every([&](Words w, int) {
+            as_floats<T>(x, w);
 #pragma unroll
-            for (int k = 0; k < K; ++k)
-#pragma unroll
-                for (int i = 0; i < V; ++i) sum = sum + exp_under((float)z[k][i], top);
-        } else {
-            for (int64_t at = (int64_t)lane * V; at < vocab; at += kLanes * V) {
-                const int64_t left = vocab - at;
-                z[0] = left >= V ? load_vec<V>(from + at) : load_part<V>(from + at, (int)left, -__builtin_inff());
-#pragma unroll
-                for (int i = 0; i < V; ++i) sum = sum + exp_under((float)z[0][i], top);
-            }
-        }
+            for (int i = 0; i < V; ++i) sum = sum + exp_under(x[i], top);
+        });
         sum = group_sum<WAVES>(sum, lds[1]);
-        const float loss = logf(sum) - (hit_of[WAVES == 1 ? threadIdx.x / kWave : 0] - top);
+        const float hit = hit_of[WAVES == 1 ? threadIdx.x / kWave : 0];
+        const float loss = logf(sum) - (hit - top);
         total = total + (double)loss;
         ++used;
         if (lane == 0 && a.loss) a.loss[row] = loss;
         if constexpr (GRAD) {
             const float share = factor / sum;
-            auto out = [&](Vec<T, V> v, int64_t at) {
-                float d[V];
+            every([&](Words w, int at) {
+                as_floats<T>(x, w);
 #pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    d[i] = exp_under((float)v[i], top) * share;
-                    if (at + i == target) d[i] = d[i] - factor;
-                }
-                if (vocab - at >= V)
-                    store_vec<V>(to + at, narrow_from<V, T>(d));
-                else
-                    store_part<V>(to + at, narrow_from<V, T>(d), vocab > at ? (int)(vocab - at) : 0);
-            };
-            if constexpr (K > 0) {
-#pragma unroll
-                for (int k = 0; k < K; ++k) out(z[k], ((int64_t)k * kLanes + lane) * V);
-            } else {
-                for (int64_t at = (int64_t)lane * V; at < vocab; at += kLanes * V) {
-                    const int64_t left = vocab - at;
-                    out(left >= V ? load_vec<V>(from + at) : load_part<V>(from + at, (int)left), at);
-                }
-            }
+                for (int i = 0; i < V; ++i) x[i] = exp_under(x[i], top) * share;
+                store_floats_of(to, at, vocab, x);
+            });
+            // the lane that wrote the target's element writes it again, less the factor
+            if (target / V % kLanes == lane) to[target] = (T)(exp_under(hit, top) * share - factor);
         }
         if (WAVES > 1) __syncthreads();                // the next row's reductions write where this one's were read
     }
@@ -260,7 +277,8 @@ struct Shape {
 Shape shape_of(const ea_token_loss_t& c)
 {
     const int64_t v = c.type == EA_F32 ? 4 : 8;
-    const Shape all[] = {{1, 2}, {1, 4}, {4, 2}, {4, 4}, {16, 2}, {16, 4}, {16, 6}, {16, 8}, {16, 12}, {16, 16}};
+    const Shape all[] = {{1, 2}, {1, 4}, {4, 2}, {4, 4}, {16, 2}, {16, 3}, {16, 4},
+                         {16, 5}, {16, 6}, {16, 7}, {16, 8}, {16, 10}, {16, 12}, {16, 14}, {16, 16}};
     for (const Shape& s : all)
         if (c.vocab <= v * kWave * s.waves * s.k) return s;
     return {16, 0};
@@ -296,10 +314,15 @@ hipError_t start_loss(const Loss& a, Shape s, unsigned groups, const void* logit
     EA_SHAPE(4, 2)
     EA_SHAPE(4, 4)
     EA_SHAPE(16, 2)
+    EA_SHAPE(16, 3)
     EA_SHAPE(16, 4)
+    EA_SHAPE(16, 5)
     EA_SHAPE(16, 6)
+    EA_SHAPE(16, 7)
     EA_SHAPE(16, 8)
+    EA_SHAPE(16, 10)
     EA_SHAPE(16, 12)
+    EA_SHAPE(16, 14)
     EA_SHAPE(16, 16)
     EA_SHAPE(16, 0)
 #undef EA_SHAPE
