@@ -76,6 +76,9 @@ int check_recurrence(const ea_recurrence_t* c)
     if (c->gate != EA_GATE_PLAIN && c->gate != EA_GATE_SIGMOID) return fail(EA_ERR_ARG, "unknown gate %d", c->gate);
     if (c->reserved) return fail(EA_ERR_ARG, "reserved must be 0");
     if (c->batch * c->length >= (int64_t)1 << 31) return fail(EA_ERR_UNSUPPORTED, "2^31 rows or more in one call");
+    // 64 channels of up to 128 steps of a sequence are a workgroup's: more than memory holds
+    if (c->batch * (c->length / 128 + 1) * (c->dim / 64 + 1) >= (int64_t)1 << 31)
+        return fail(EA_ERR_UNSUPPORTED, "batch, length and dim are too large for one call");
     return EA_OK;
 }
 

@@ -3,8 +3,6 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
-#include <type_traits>
-
 #include "ea_recurrence.hpp"
 
 namespace ea {
@@ -12,194 +10,145 @@ namespace rec {
 
 namespace {
 
-// A segment's product of gates and the state it ends with from 0: each wave runs over a stretch of consecutive steps.
-template <class X, class G, int C, bool SIGMOID>
-__global__ void __launch_bounds__(kMostWaves* kWave) segment_kernel(Call a, const G* g, const X* x, const float* h0)
+// CHAIN: sequences of more than one chunk.
+template <class X, class G, bool SIGMOID, bool CHAIN>
+__global__ void __launch_bounds__(kMostWaves* kWave, 8)
+    recurrence_kernel(Call a, const G* g, const X* x, const float* h0, X* y, float* states, float* h_last)
 {
-    __shared__ float lds[kMostWaves][2][kWave * C];
-    const int wave = threadIdx.x / kWave, lane = lane_id();
-    const int64_t each = a.c.batch * a.c.dim, units = a.p.strips * a.c.batch * a.p.segments;
-    for (int64_t unit = blockIdx.x; unit < units; unit += gridDim.x) {
-        const Place p = place_of<C>(a, unit);
-        const int64_t stretch = a.p.steps / kMostWaves, row = p.b * a.c.length;
-        float m[C], h[C];
-#pragma unroll
-        for (int i = 0; i < C; ++i) {
-            m[i] = 1.0f;
-            h[i] = 0.0f;
+    constexpr int K = kForwardSteps;
+    __shared__ Exchange lds;
+    const int wave = wave_id(), lane = lane_id(), waves = a.p.waves;
+    const int64_t blocks = (a.c.length + EA_RECURRENCE_BLOCK - 1) / EA_RECURRENCE_BLOCK;
+    for (Items<CHAIN> it(a, &lds.item); it.item < a.items;) {
+        const Place p = place_of(a, it.item, false);
+        it.draw(a);
+        const int64_t t = (int64_t)(p.chunk * waves + wave) * K, row = p.b * a.c.length + t;
+        const int count = steps_at<K>(t, p.n), held = steps_at<K>(t, (int)a.c.length);
+        zero_steps<K>(y, row, a.c.y_stride, a, p, count, held);
+        if (p.chunk > p.last) {
+            __syncthreads();
+            it.next(a);
+            __syncthreads();
+            continue;
         }
-        for (int64_t t = p.from + wave * stretch; t < p.from + (wave + 1) * stretch; t += kSteps) {
-            const int count = steps_at(t, p.n);
-            Vec<G, C> gr[kSteps];
-            Vec<X, C> xr[kSteps];
-            load_steps<C>(gr, g, row + t, a.c.g_stride, p, count);
-            load_steps<C>(xr, x, row + t, a.c.x_stride, p, count);
+        G gr[K];
+        X xr[K];
+        load_steps<K>(gr, g, row, a.c.g_stride, a, p, count);
+        load_steps<K>(xr, x, row, a.c.x_stride, a, p, count);
+        float f[K], v[K], m = 1.0f, e = 0.0f;
 #pragma unroll
-            for (int k = 0; k < kSteps; ++k) {
-                if (k >= count) break;
-#pragma unroll
-                for (int i = 0; i < C; ++i) {
-                    float f, w;
-                    gate_of<SIGMOID>((float)element<C, G>(gr[k], i), f, w);
-                    m[i] = m[i] * f;
-                    h[i] = __builtin_fmaf(f, h[i], w * (float)element<C, X>(xr[k], i));
-                }
-            }
+        for (int k = 0; k < K; ++k) {
+            float w;
+            gate_of<SIGMOID>((float)gr[k], f[k], w);
+            v[k] = w * (float)xr[k];
         }
+        mask_steps<K>(f, v, count);
 #pragma unroll
-        for (int i = 0; i < C; ++i) {
-            lds[wave][0][lane * C + i] = m[i];
-            lds[wave][1][lane * C + i] = h[i];
+        for (int k = 0; k < K; ++k) {
+            m = k ? m * f[k] : f[k];
+            e = k ? __builtin_fmaf(f[k], e, v[k]) : f[k] * 0.0f + v[k];
         }
+        lds.wave[wave][0][lane] = m;
+        lds.wave[wave][1][lane] = e;
+        const bool last = p.chunk == p.last;
+        const int place = CHAIN ? (int)(p.chunk % kGroup) : 0;
         __syncthreads();
-        if (wave == 0) {
-            for (int j = 1; j < kMostWaves; ++j)
-#pragma unroll
-                for (int i = 0; i < C; ++i) {
-                    const float f = lds[j][0][lane * C + i];
-                    m[i] = m[i] * f;
-                    h[i] = behind(f, lds[j][1][lane * C + i], h[i]);
-                }
-            float* to = a.workspace + p.segment * 2 * each;
-            store_floats<C>(to, p.b * a.c.dim + p.at, m, p.channels);
-            store_floats<C>(to + each, p.b * a.c.dim + p.at, h, p.channels);
-            if (p.segment == 0) {                      // h_last may take h0's place
-                load_floats<C>(h, h0, p.b * a.c.dim + p.at, p.channels);
-                store_floats<C>(a.workspace + a.p.segments * 2 * each, p.b * a.c.dim + p.at, h, p.channels);
-            }
+        it.next(a);
+        float h;
+        if (CHAIN) {
+            meet<false>(a, p, lds, 1, p.chunk / kGroup, place, last, h0);
+            __syncthreads();
+            h = fold_chunks(lds, place);
+        } else {
+            h = end_at(h0, a, p);
         }
-        __syncthreads();
+#pragma unroll 4
+        for (int j = 0; j < wave; ++j) h = behind(lds.wave[j][0][lane], lds.wave[j][1][lane], h);
+        if (CHAIN && place == kGroup - 1 && !last && wave == waves - 1 && p.on)
+            hand_out(group_word(a, p, p.chunk / kGroup + 1), behind(m, e, h));
+        if (states && p.on && t % EA_RECURRENCE_BLOCK == 0 && t < a.c.length)
+            states[(p.b * blocks + t / EA_RECURRENCE_BLOCK) * a.c.dim + p.channel] = h;
+        X* to = y + row * a.c.y_stride;
+#pragma unroll
+        for (int k = 0; k < K; ++k, to += a.c.y_stride) {
+            h = __builtin_fmaf(f[k], h, v[k]);
+            store_own<X>(row_of(to, a, k < count), p, (X)h);
+        }
+        __syncthreads();                               // every wave has h0, and what is in LDS
+        if (last && wave == waves - 1 && p.on) {
+            if (h_last) h_last[p.b * a.c.dim + p.channel] = h;
+            if (states)                                // of the chunks behind the last
+                for (int64_t k = ((int64_t)(p.last + 1) * waves * K + EA_RECURRENCE_BLOCK - 1) / EA_RECURRENCE_BLOCK;
+                     k < blocks; ++k)
+                    states[(p.b * blocks + k) * a.c.dim + p.channel] = h;
+        }
     }
 }
 
-template <class X, class G, int C, bool SIGMOID>
-__global__ void __launch_bounds__(kMostWaves* kWave)
-    recurrence_kernel(Call a, const G* g, const X* x, const float* h0, X* y, float* states, float* h_last)
+constexpr int kClearBlock = 256;
+
+// Workgroups of a launch: as many as the CUs hold where chunks are drawn from the counter.
+constexpr int64_t kMostGroupsOf(bool chain)
 {
-    __shared__ Shared<C, 2> lds;
-    const int wave = threadIdx.x / kWave, lane = lane_id(), waves = a.p.waves;
-    const int64_t units = a.p.strips * a.c.batch * a.p.segments, tile = waves * kSteps;
-    const int64_t blocks = (a.c.length + EA_RECURRENCE_BLOCK - 1) / EA_RECURRENCE_BLOCK;
-    int parity = 0;
-    for (int64_t unit = blockIdx.x; unit < units; unit += gridDim.x) {
-        const Place p = place_of<C>(a, unit);
-        const int64_t row = p.b * a.c.length;
-        Vec<G, C> gr[kSteps];
-        Vec<X, C> xr[kSteps];
-        int64_t t = p.from + wave * kSteps;
-        load_steps<C>(gr, g, row + t, a.c.g_stride, p, steps_at(t, p.n));
-        load_steps<C>(xr, x, row + t, a.c.x_stride, p, steps_at(t, p.n));
-        float h[C];
-        fold_segments<C, false>(h, a, p, h0);
-        for (; t - wave * kSteps < p.to; t += tile) {
-            const int count = steps_at(t, p.n);
-            float f[kSteps * C], v[kSteps * C], m[C], e[C];
-#pragma unroll
-            for (int k = 0; k < kSteps; ++k)
-#pragma unroll
-                for (int i = 0; i < C; ++i) {
-                    float w;
-                    gate_of<SIGMOID>((float)element<C, G>(gr[k], i), f[k * C + i], w);
-                    v[k * C + i] = w * (float)element<C, X>(xr[k], i);
-                    if (k >= count) {
-                        f[k * C + i] = 1.0f;
-                        v[k * C + i] = 0.0f;
-                    }
-                }
-            if (t + tile - wave * kSteps < p.to) {     // the next tile's steps, while this one's are worked on
-                const int next = steps_at(t + tile, p.n);
-                load_steps<C>(gr, g, row + t + tile, a.c.g_stride, p, next);
-                load_steps<C>(xr, x, row + t + tile, a.c.x_stride, p, next);
-            }
-#pragma unroll
-            for (int i = 0; i < C; ++i) {
-                m[i] = f[i];
-                e[i] = v[i];
-            }
-#pragma unroll
-            for (int k = 1; k < kSteps; ++k)
-#pragma unroll
-                for (int i = 0; i < C; ++i) {
-                    m[i] = m[i] * f[k * C + i];
-                    e[i] = __builtin_fmaf(f[k * C + i], e[i], v[k * C + i]);
-                }
-#pragma unroll
-            for (int i = 0; i < C; ++i) {
-                lds.v[parity][wave][0][lane * C + i] = m[i];
-                lds.v[parity][wave][1][lane * C + i] = e[i];
-            }
-            __syncthreads();
-            float mine[C];
-            for (int j = 0; j < waves; ++j)
-#pragma unroll
-                for (int i = 0; i < C; ++i) {
-                    if (j == wave) mine[i] = h[i];
-                    h[i] = behind(lds.v[parity][j][0][lane * C + i], lds.v[parity][j][1][lane * C + i], h[i]);
-                }
-            parity ^= 1;
-            if (states && t % EA_RECURRENCE_BLOCK == 0 && t < p.to)
-                store_floats<C>(states, (p.b * blocks + t / EA_RECURRENCE_BLOCK) * a.c.dim + p.at, mine, p.channels);
-#pragma unroll
-            for (int k = 0; k < kSteps; ++k) {
-                if (t + k >= p.to) break;
-                float o[C];
-#pragma unroll
-                for (int i = 0; i < C; ++i) {
-                    mine[i] = __builtin_fmaf(f[k * C + i], mine[i], v[k * C + i]);
-                    o[i] = k < count ? mine[i] : 0.0f;
-                }
-                X* to = y + (row + t + k) * a.c.y_stride + p.at;
-                if (p.channels == C)
-                    store_vec<C>(to, narrow_from<C, X>(o));
-                else
-                    store_part<C>(to, narrow_from<C, X>(o), p.channels);
-            }
-        }
-        __syncthreads();                               // every wave has h0: h_last may take its place
-        if (h_last && wave == 0 && p.segment == a.p.segments - 1)
-            store_floats<C>(h_last, p.b * a.c.dim + p.at, h, p.channels);
-    }
+    return chain ? 512 : 1 << 20;
+}
+
+__global__ void __launch_bounds__(kClearBlock) clear_kernel(uint64_t* words, int64_t count)
+{
+    typedef uint64_t Pair __attribute__((ext_vector_type(2)));
+    for (int64_t i = (int64_t)blockIdx.x * kClearBlock + threadIdx.x; i * 2 < count; i += (int64_t)gridDim.x * kClearBlock)
+        ((Pair*)words)[i] = Pair{0, 0};
 }
 
 }  // namespace
 
-int channels_of(const ea_recurrence_t& c, bool backward)
-{
-    if (c.dim <= kWave) return 1;
-    if (backward) return c.x_type != EA_F32 && c.g_type != EA_F32 ? 2 : 1;
-    return 2;
-}
-
-Plan plan_of(const ea_recurrence_t& c, int channels)
+Plan plan_of(const ea_recurrence_t& c, int steps)
 {
     Plan p;
-    p.strips = (c.dim + kWave * channels - 1) / (kWave * channels);
+    p.strips = (uint32_t)((c.dim + kWave - 1) / kWave);
     p.waves = 1;
-    while (p.waves < kMostWaves && p.waves * kSteps < c.length) p.waves *= 2;
-    p.segments = 1;
-    p.steps = (c.length + kTile - 1) / kTile * kTile;
-    const int64_t units = p.strips * c.batch;
-    if (units > 0 && units < 192 && c.length > 4 * kTile) {
-        int64_t want = (512 + units - 1) / units;
-        const int64_t tiles = (c.length + kTile - 1) / kTile;
-        if (want > tiles / 2) want = tiles / 2;
-        const int64_t each = (tiles + want - 1) / want;
-        p.segments = (tiles + each - 1) / each;
-        p.steps = each * kTile;
-    }
+    while (p.waves < kMostWaves && p.waves * steps < c.length) p.waves *= 2;
+    const int64_t chunk = p.waves * steps;
+    p.chunks = c.length > chunk ? (uint32_t)((c.length + chunk - 1) / chunk) : 1;
     return p;
+}
+
+// An even number: words are cleared in pairs.
+int64_t words_of(const ea_recurrence_t& c, const Plan& p)
+{
+    if (p.chunks == 1) return 0;
+    const int64_t groups = (p.chunks + kGroup - 1) / kGroup;
+    return (kCounterWords + (2 * (int64_t)p.chunks + groups) * c.batch * c.dim + 1) / 2 * 2;
+}
+
+hipError_t begin(Call& a, const ea_recurrence_t& c, int steps, const int32_t* lengths, void* workspace, unsigned* groups,
+                 hipStream_t s)
+{
+    a.c = c;
+    a.p = plan_of(c, steps);
+    a.lengths = lengths;
+    a.words = (uint64_t*)workspace;
+    *groups = 0;
+    if (c.batch == 0) return hipSuccess;
+    const int64_t items = (int64_t)a.p.strips * c.batch * a.p.chunks;
+    a.items = (uint32_t)items;                         // under 2^31: checked with the configuration
+    a.strips = Divisor(a.p.strips);
+    a.batch = Divisor((uint32_t)c.batch);
+    a.chunk = Divisor((uint32_t)(a.p.waves * steps));
+    *groups = (unsigned)(items < kMostGroupsOf(a.p.chunks > 1) ? items : kMostGroupsOf(a.p.chunks > 1));
+    if (a.p.chunks == 1) return hipSuccess;
+    const int64_t count = words_of(c, a.p), clear = (count / 2 + kClearBlock - 1) / kClearBlock;
+    hipLaunchKernelGGL(clear_kernel, dim3((unsigned)(clear < 2048 ? clear : 2048)), dim3(kClearBlock), 0, s, a.words, count);
+    return hipGetLastError();
 }
 
 }  // namespace rec
 
 int64_t recurrence_workspace_bytes(const ea_recurrence_t& c)
 {
-    int64_t most = 0;
-    for (const bool backward : {false, true}) {
-        const int64_t n = rec::plan_of(c, rec::channels_of(c, backward)).segments;
-        most = n > most ? n : most;
-    }
-    return most > 1 ? (2 * most + 1) * c.batch * c.dim * 4 : 0;
+    const int64_t forward = rec::words_of(c, rec::plan_of(c, rec::kForwardSteps));
+    const int64_t backward = rec::words_of(c, rec::plan_of(c, rec::kBackwardSteps));
+    return (forward > backward ? forward : backward) * 8;
 }
 
 hipError_t launch_recurrence(const ea_recurrence_t& c, const void* g, const void* x, const float* h0,
@@ -207,31 +156,22 @@ hipError_t launch_recurrence(const ea_recurrence_t& c, const void* g, const void
                              hipStream_t s)
 {
     using namespace rec;
-    const int channels = channels_of(c, false);
-    const Call a{c, plan_of(c, channels), lengths, (float*)workspace};
-    const int64_t units = a.p.strips * c.batch * a.p.segments;
-    if (units == 0) return hipSuccess;
-    const unsigned groups = (unsigned)(units < kMostUnits ? units : kMostUnits);
-    auto start = [&](auto xt, auto gt, auto ct, auto sigmoid) {
+    Call a;
+    unsigned groups;
+    const hipError_t e = begin(a, c, kForwardSteps, lengths, workspace, &groups, s);
+    if (e != hipSuccess || groups == 0) return e;
+    return with_kinds(c, [&](auto xt, auto gt, auto sigmoid) {
         using X = decltype(xt);
         using G = decltype(gt);
-        constexpr int C = decltype(ct)::value;
         constexpr bool S = decltype(sigmoid)::value;
-        if (a.p.segments > 1)
-            hipLaunchKernelGGL((segment_kernel<X, G, C, S>), dim3(groups), dim3(kMostWaves * kWave), 0, s, a,
-                               (const G*)g, (const X*)x, h0);
-        hipLaunchKernelGGL((recurrence_kernel<X, G, C, S>), dim3(groups), dim3(a.p.waves * kWave), 0, s, a,
-                           (const G*)g, (const X*)x, h0, (X*)y, states, h_last);
+        const dim3 grid(groups), block(a.p.waves * kWave);
+        if (a.p.chunks > 1)
+            hipLaunchKernelGGL((recurrence_kernel<X, G, S, true>), grid, block, 0, s, a, (const G*)g, (const X*)x, h0,
+                               (X*)y, states, h_last);
+        else
+            hipLaunchKernelGGL((recurrence_kernel<X, G, S, false>), grid, block, 0, s, a, (const G*)g, (const X*)x, h0,
+                               (X*)y, states, h_last);
         return hipGetLastError();
-    };
-    return with_type(c.x_type, [&](auto xt) {
-        return with_type(c.g_type, [&](auto gt) {
-            constexpr std::integral_constant<int, 1> one{};
-            constexpr std::integral_constant<int, 2> two{};
-            if (c.gate == EA_GATE_SIGMOID)
-                return channels == 1 ? start(xt, gt, one, std::true_type{}) : start(xt, gt, two, std::true_type{});
-            return channels == 1 ? start(xt, gt, one, std::false_type{}) : start(xt, gt, two, std::false_type{});
-        });
     });
 }
 

@@ -1,93 +1,239 @@
 // ea_recurrence.hpp -- what the gated linear recurrence and its gradient share:
-// the plan of a call, gates, loads of a wave's steps.
+// the plan of a call, gates, loads of a wave's steps, and the states that
+// chunks of a sequence hand on to each other.
 //
-// A workgroup takes 64 * C channels of one sequence, C a lane, and walks over
-// tiles of steps: each of its waves takes kSteps consecutive steps of a tile,
-// reads them ahead of the tile before, and runs them from a state of 0; the
-// product of their gates and the state they end with go to LDS, and after one
-// barrier every wave folds what lies before it, in order, and runs its steps
-// again from the true state.  Where there are too few channels to fill the GPU
-// a sequence is cut into segments: a first launch leaves each segment's product
-// and end state, and every segment's workgroup folds those before it.
+// A workgroup takes a chunk of steps of 64 channels of one sequence, a channel a
+// lane, so that every array passes memory once.  Each of its waves reads a few
+// consecutive steps and runs them from a state of 0; the product of their gates
+// and the state they end with go to LDS, and every wave folds what lies before
+// it, in order, and runs its steps again from the true state.
+//
+// What a chunk starts with comes from the chunks before it through memory.
+// kGroup chunks form a group: a chunk hands out its product and end state as soon
+// as it has them, without waiting for anything, and the last chunk of a group
+// the true state behind it.  So a chunk waits for the state before its group and
+// folds the group's chunks before it, always in this order: the result does not
+// depend on who came first, and a wait passes from group to group only.
+// Workgroups draw their chunks from a counter, in the order of the steps: who
+// waits, waits for workgroups that have begun.  A wait of a good part of a second
+// is given up, and the state is NaN.
 #pragma once
+
+#include <type_traits>
 
 #include "ea_layer.hpp"
 
 namespace ea {
 namespace rec {
 
-constexpr int kSteps = 8;                              // of a wave and tile
 constexpr int kMostWaves = 16;
-constexpr int kTile = kSteps * kMostWaves;             // steps of a tile of a sequence that is longer than one
-constexpr int kGroupWaves = EA_RECURRENCE_BLOCK / kSteps;   // waves between two saved states
+constexpr int kGroup = 16;                             // chunks; one wave waits for each of those before, one for the state
+static_assert(kGroup <= kMostWaves, "a group's earlier chunks and the state before it have a wave each");
 
-struct Plan {
-    int64_t strips;                                    // of 64 * C channels
-    int64_t segments, steps;                           // of a sequence, and steps of each (a multiple of kTile)
-    int waves;
+// Division of numbers under 2^31 by a number known to the host: (h + (n - h) / 2) / 2^shift for the high half h of
+// n * factor, in scalar instructions.
+struct Divisor {
+    uint32_t factor, shift, by;
+    explicit Divisor(uint32_t d = 1) : by(d)
+    {
+        uint32_t bits = 0;
+        while (((uint64_t)1 << bits) < d) ++bits;
+        factor = (uint32_t)((((uint64_t)1 << 32) * (((uint64_t)1 << bits) - d)) / d + 1);
+        shift = bits;
+    }
+    __device__ uint32_t of(uint32_t n) const
+    {
+        const uint32_t h = __umulhi(factor, n);
+        return shift == 0 ? n : (h + ((n - h) >> 1)) >> (shift - 1);
+    }
 };
 
+struct Plan {
+    uint32_t strips;                                   // of 64 channels
+    uint32_t chunks;                                   // of a sequence
+    int waves;                                         // of a chunk
+};
+
+// 64-bit words in the workspace: a counter, then for each chunk, sequence and channel the product and the end state, then
+// for each group the state before it.  The upper half of a word that has been handed out is 1: it and the value in the
+// lower half become visible together, and nothing else has to be ordered.
 struct Call {
     ea_recurrence_t c;
     Plan p;
     const int32_t* lengths;
-    float* workspace;                                  // [segments][2][batch * dim], then [batch * dim]: the start
+    uint64_t* words;
+    uint32_t items;                                    // strips * batch * chunks
+    Divisor strips, batch, chunk;                      // chunk: its steps
 };
+constexpr int64_t kCounterWords = 16;
 
-// The part of the work that workgroup `unit` has: its channels' strip, sequence and segment.
+// The lane's place: sequence, chunk, channel.
 struct Place {
-    int64_t b, segment;
-    int64_t at;                                        // the lane's first channel
-    int channels;                                      // it has, 0 to C
-    int64_t n;                                         // steps of the sequence that count
-    int64_t from, to;                                  // the segment's steps
+    uint32_t b, chunk, channel;
+    bool on;                                           // the lane has a channel
+    int n;                                             // steps of the sequence that count
+    uint32_t last;                                     // the chunk that has the last of them (0 when there is none)
 };
 
-template <int C>
-__device__ __forceinline__ Place place_of(const Call& a, int64_t unit)
+__device__ __forceinline__ Place place_of(const Call& a, uint32_t item, bool reverse)
 {
     Place p;
-    const int64_t strip = unit % a.p.strips, rest = unit / a.p.strips;
-    p.b = rest % a.c.batch;
-    p.segment = rest / a.c.batch;
-    p.at = (strip * kWave + lane_id()) * C;
-    const int64_t left = a.c.dim - p.at;
-    p.channels = left >= C ? C : left > 0 ? (int)left : 0;
-    p.n = a.c.length;
+    const uint32_t rest = a.strips.of(item), strip = item - rest * a.p.strips;
+    p.chunk = a.batch.of(rest);
+    p.b = rest - p.chunk * (uint32_t)a.c.batch;
+    if (reverse) p.chunk = a.p.chunks - 1 - p.chunk;
+    p.channel = strip * kWave + lane_id();
+    p.on = p.channel < (uint32_t)a.c.dim;
+    p.n = (int)a.c.length;
     if (a.lengths) {
-        const int64_t n = a.lengths[p.b];
+        const int n = uniform(a.lengths[p.b]);
         p.n = n < 0 ? 0 : n < p.n ? n : p.n;
     }
-    p.from = p.segment * a.p.steps;
-    p.to = p.from + a.p.steps < a.c.length ? p.from + a.p.steps : a.c.length;
+    p.last = p.n > 0 ? a.chunk.of((uint32_t)p.n - 1) : 0;
     return p;
 }
 
-// The first `count` of a wave's steps from row `row` on, as they are stored; the others are left unset.
-template <int C, class T>
-__device__ __forceinline__ void load_steps(Vec<T, C>* v, const T* p, int64_t row, int64_t stride, const Place& at, int count)
+// The workgroup's pieces of work, in turn.  With chains they are drawn from the counter, each while the one before is
+// worked on: a piece that is drawn and not begun stands behind one that needs nothing from it.
+template <bool CHAIN>
+struct Items {
+    uint32_t item;
+    uint32_t* lds;
+    __device__ void draw(const Call& a)
+    {
+        if (CHAIN && threadIdx.x == 0)
+            *lds = (uint32_t)__hip_atomic_fetch_add((uint32_t*)a.words, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+    __device__ Items(const Call& a, uint32_t* at) : item(blockIdx.x), lds(at)
+    {
+        if (!CHAIN) return;
+        draw(a);
+        __syncthreads();
+        item = (uint32_t)uniform((int)*lds);
+        __syncthreads();
+    }
+    // behind a barrier after draw()
+    __device__ void next(const Call& a)
+    {
+        item = CHAIN ? (uint32_t)uniform((int)*lds) : item + gridDim.x;
+    }
+};
+
+__device__ __forceinline__ uint64_t* chunk_words(const Call& a, const Place& p, uint32_t chunk)
 {
-    if (at.channels == 0) return;
-    const T* from = p + row * stride + at.at;
-    if (at.channels == C && count == kSteps) {
+    return a.words + kCounterWords + ((chunk * a.c.batch + p.b) * a.c.dim + p.channel) * 2;
+}
+
+__device__ __forceinline__ uint64_t* group_word(const Call& a, const Place& p, uint32_t group)
+{
+    return a.words + kCounterWords + (((int64_t)a.p.chunks * 2 + group) * a.c.batch + p.b) * a.c.dim + p.channel;
+}
+
+__device__ __forceinline__ void hand_out(uint64_t* word, float v)
+{
+    __hip_atomic_store(word, (uint64_t)1 << 32 | __float_as_uint(v), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
+constexpr int kMostPolls = 1 << 18;                    // about a microsecond each
+
+// N consecutive words, once all have been handed out.
+template <int N>
+__device__ __forceinline__ void await(float* v, const uint64_t* words, bool on)
+{
+    uint64_t w[N];
+    for (int i = 0;; ++i) {
+        bool ready = true;
 #pragma unroll
-        for (int k = 0; k < kSteps; ++k) v[k] = load_vec<C>(from + k * stride);
+        for (int k = 0; k < N; ++k) {
+            w[k] = on ? __hip_atomic_load(words + k, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : (uint64_t)1 << 32;
+            ready = ready && w[k] >> 32 == 1;
+        }
+        if (__ballot(!ready) == 0) break;
+        if (i == kMostPolls) {
+#pragma unroll
+            for (int k = 0; k < N; ++k)
+                if (w[k] >> 32 != 1) w[k] = 0x7FC00000u;
+            break;
+        }
+        __builtin_amdgcn_s_sleep(1);
+    }
+#pragma unroll
+    for (int k = 0; k < N; ++k) v[k] = __uint_as_float((uint32_t)w[k]);
+}
+
+// A row through a descriptor of its `dim` elements, or of none: lanes without a channel, and steps that do not count, read
+// 0 and write nothing, and neither branches nor addresses take vector registers (108 -> 60 of them in the binary32 forward
+// pass, which lets two workgroups share a CU).
+template <class T>
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t row_of(const T* row, const Call& a, bool on)
+{
+    return __builtin_amdgcn_make_buffer_rsrc((void*)const_cast<T*>(row), 0, on ? (int)(a.c.dim * sizeof(T)) : 0, kRawBuffer);
+}
+
+template <class T>
+__device__ __forceinline__ T load_own(__amdgpu_buffer_rsrc_t row, const Place& at)
+{
+    const uint32_t off = at.channel * (uint32_t)sizeof(T);
+    if constexpr (sizeof(T) == 2)
+        return __builtin_bit_cast(T, (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(row, off, 0, 0));
+    else
+        return __builtin_bit_cast(T, __builtin_amdgcn_raw_buffer_load_b32(row, off, 0, 0));
+}
+
+template <class T>
+__device__ __forceinline__ void store_own(__amdgpu_buffer_rsrc_t row, const Place& at, T v)
+{
+    const uint32_t off = at.channel * (uint32_t)sizeof(T);
+    if constexpr (sizeof(T) == 2)
+        __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(uint16_t, v), row, off, 0, 0);
+    else
+        __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(uint32_t, v), row, off, 0, 0);
+}
+
+// A wave's steps from row `row` on, as they are stored; from step `count` on they are 0.
+template <int K, class T>
+__device__ __forceinline__ void load_steps(T* v, const T* p, int64_t row, int64_t stride, const Call& a, const Place& at,
+                                           int count)
+{
+    const T* from = p + row * stride;
+    if (count == K) {
+#pragma unroll
+        for (int k = 0; k < K; ++k, from += stride) v[k] = load_own<T>(row_of(from, a, true), at);
         return;
     }
 #pragma unroll
-    for (int k = 0; k < kSteps; ++k)
-        if (k < count) v[k] = load_part<C>(from + k * stride, at.channels);
+    for (int k = 0; k < K; ++k, from += stride) v[k] = load_own<T>(row_of(from, a, k < count), at);
 }
 
-// Steps of the wave at step `t` that count, 0 to kSteps.
-__device__ __forceinline__ int steps_at(int64_t t, int64_t n)
+// Steps that do not count keep the state.
+template <int K>
+__device__ __forceinline__ void mask_steps(float* f, float* v, int count)
 {
-    const int64_t left = n - t;
-    return left >= kSteps ? kSteps : left > 0 ? (int)left : 0;
+    if (count == K) return;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        f[k] = k < count ? f[k] : 1.0f;
+        v[k] = k < count ? v[k] : 0.0f;
+    }
 }
 
-// a and w of a gate: 1 / (1 + e) and e / (1 + e) with e = exp(-|g|).  The reciprocal gets a correction step: gates near
-// 1 are multiplied over hundreds of steps, where a unit each would add up.
+// Steps of the wave at step `t` before `end`, 0 to K.
+template <int K>
+__device__ __forceinline__ int steps_at(int64_t t, int end)
+{
+    const int64_t left = end - t;
+    return left >= K ? K : left > 0 ? (int)left : 0;
+}
+
+// Zeros in the wave's steps that a sequence has no use for.
+template <int K, class T>
+__device__ __forceinline__ void zero_steps(T* p, int64_t row, int64_t stride, const Call& a, const Place& at, int from, int to)
+{
+    for (int k = from; k < to; ++k) store_own<T>(row_of(p + (row + k) * stride, a, true), at, (T)0.0f);
+}
+
+// a and w of a gate: e / (1 + e) with e = exp(-|g|) for the smaller of them, and what is left of 1 for the other.  The
+// larger is off by less than a rounding of its own where it is near 1: gates are multiplied over hundreds of steps.
 template <bool SIGMOID>
 __device__ __forceinline__ void gate_of(float g, float& a, float& w)
 {
@@ -97,8 +243,8 @@ __device__ __forceinline__ void gate_of(float g, float& a, float& w)
         return;
     }
     const float e = __builtin_amdgcn_exp2f(-fabsf(g) * 0x1.715476p+0f);
-    const float d = 1.0f + e, q = __builtin_amdgcn_rcpf(d);
-    const float r = __builtin_fmaf(__builtin_fmaf(-d, q, 1.0f), q, q), s = e * r;
+    const float q = __builtin_amdgcn_rcpf(1.0f + e);
+    const float s = e * q, r = __builtin_fmaf(-e, q, 1.0f);
     a = g < 0.0f ? s : r;
     w = g < 0.0f ? r : s;
 }
@@ -110,53 +256,86 @@ __device__ __forceinline__ float behind(float a, float v, float h)
     return h == 0.0f ? v : __builtin_fmaf(a, h, v);
 }
 
-template <int C>
-__device__ __forceinline__ void load_floats(float* x, const float* p, int64_t at, int channels)
+// One lane's value of a [batch, dim] array, 0 where there is none.
+__device__ __forceinline__ float end_at(const float* p, const Call& a, const Place& at)
 {
-#pragma unroll
-    for (int k = 0; k < C; ++k) x[k] = p && k < channels ? p[at + k] : 0.0f;
+    return p && at.on ? p[at.b * a.c.dim + at.channel] : 0.0f;
 }
 
-template <int C>
-__device__ __forceinline__ void store_floats(float* p, int64_t at, const float* x, int channels)
-{
-#pragma unroll
-    for (int k = 0; k < C; ++k)
-        if (k < channels) p[at + k] = x[k];
-}
-
-// The state (or gradient) that segment `p.segment` starts with: the ones before it (or behind, from the last) folded.
-template <int C, bool REVERSE>
-__device__ __forceinline__ void fold_segments(float* h, const Call& a, const Place& p, const float* start)
-{
-    const int64_t each = a.c.batch * a.c.dim, at = p.b * a.c.dim + p.at;
-    if (a.p.segments == 1) {
-        load_floats<C>(h, start, at, p.channels);
-        return;
-    }
-    load_floats<C>(h, a.workspace + a.p.segments * 2 * each, at, p.channels);
-    const int64_t count = REVERSE ? a.p.segments - 1 - p.segment : p.segment;
-#pragma unroll 4
-    for (int64_t i = 0; i < count; ++i) {
-        const float* s = a.workspace + (REVERSE ? a.p.segments - 1 - i : i) * 2 * each;
-        float m[C], v[C];
-        load_floats<C>(m, s, at, p.channels);
-        load_floats<C>(v, s + each, at, p.channels);
-#pragma unroll
-        for (int k = 0; k < C; ++k) h[k] = behind(m[k], v[k], h[k]);
-    }
-}
-
-// Products and end values of each wave's part of a tile, [waves][64 * C] of them.
-template <int C, int N>
-struct Shared {
-    float v[2][kMostWaves][N][kWave * C];
+struct Exchange {
+    float wave[kMostWaves][3][kWave];                  // each wave's product, and what its steps lead to from 0
+    float chunk[kGroup][2][kWave];                     // the same of the group's chunks before this one
+    float start[kWave];                                // the state before the group
+    uint32_t item;
 };
 
-// Channels a lane takes, and the plan with it.
-int channels_of(const ea_recurrence_t& c, bool backward);
-Plan plan_of(const ea_recurrence_t& c, int channels);
-constexpr int64_t kMostUnits = 1 << 20;                // workgroups of a launch; more work goes round
+// Hands out the chunk's product and end value (value `which` of each wave; REVERSE: from its last wave to its first) and
+// gathers the state before its group, `place` chunks behind it and all of those: what fold_chunks() needs after a barrier.
+template <bool REVERSE>
+__device__ __forceinline__ void meet(const Call& a, const Place& p, Exchange& x, int which, uint32_t group, int place,
+                                     bool last, const float* start)
+{
+    const int wave = wave_id(), lane = lane_id();
+    if (wave == 0 && !last && place < kGroup - 1) {
+        float m = 1.0f, v = 0.0f;
+#pragma unroll 4
+        for (int i = 0; i < kMostWaves; ++i) {
+            const int j = REVERSE ? kMostWaves - 1 - i : i;
+            const float f = x.wave[j][0][lane];
+            m = m * f;
+            v = behind(f, x.wave[j][which][lane], v);
+        }
+        if (p.on) {
+            uint64_t* to = chunk_words(a, p, p.chunk);
+            hand_out(to, m);
+            hand_out(to + 1, v);
+        }
+    }
+    if (wave < place) {
+        float v[2];
+        const int back = place - wave;                 // chunks between that one and this
+        await<2>(v, chunk_words(a, p, REVERSE ? p.chunk + back : p.chunk - back), p.on);
+        x.chunk[wave][0][lane] = v[0];
+        x.chunk[wave][1][lane] = v[1];
+    } else if (wave == kMostWaves - 1) {
+        float v;
+        if (group == 0 && place == 0) {
+            v = end_at(start, a, p);
+            if (!last && p.on) hand_out(group_word(a, p, 0), v);
+        } else {
+            await<1>(&v, group_word(a, p, group), p.on);
+        }
+        x.start[lane] = v;
+    }
+}
+
+// The state before the chunk.
+__device__ __forceinline__ float fold_chunks(const Exchange& x, int place)
+{
+    const int lane = lane_id();
+    float h = x.start[lane];
+#pragma unroll 4
+    for (int i = 0; i < place; ++i) h = behind(x.chunk[i][0][lane], x.chunk[i][1][lane], h);
+    return h;
+}
+
+constexpr int kForwardSteps = 16, kBackwardSteps = 8;  // of a wave
+Plan plan_of(const ea_recurrence_t& c, int steps);
+int64_t words_of(const ea_recurrence_t& c, const Plan& p);
+// The call, its words cleared; groups gets the workgroups of its launch, 0 for nothing to do.
+hipError_t begin(Call& a, const ea_recurrence_t& c, int steps, const int32_t* lengths, void* workspace, unsigned* groups,
+                 hipStream_t s);
+
+// f with the types and the gate of a call as constants.
+template <class F>
+hipError_t with_kinds(const ea_recurrence_t& c, F&& f)
+{
+    return with_type(c.x_type, [&](auto x) {
+        return with_type(c.g_type, [&](auto g) {
+            return c.gate == EA_GATE_SIGMOID ? f(x, g, std::true_type{}) : f(x, g, std::false_type{});
+        });
+    });
+}
 
 }  // namespace rec
 }  // namespace ea

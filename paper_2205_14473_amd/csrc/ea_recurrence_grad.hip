@@ -1,11 +1,9 @@
 // ea_recurrence_grad.hip -- the gradient of the gated linear recurrence (see
-// ea_recurrence.hpp): the same tiles from the last to the first.  The state
+// ea_recurrence.hpp): the same chunks from the last to the first.  The state
 // before each step is formed again from the states saved every 64 steps, so
 // that g, x and dy are all that is read.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
-
-#include <type_traits>
 
 #include "ea_recurrence.hpp"
 
@@ -16,189 +14,93 @@ namespace {
 
 // What arrives at step t from behind is e_t = a_{t+1} d_{t+1}, with d_t = dy_t + e_t; over some steps it goes from e to
 // (product of their gates) e + (what they give from e = 0).
-
-template <class X, class G, int C, bool SIGMOID>
-__global__ void __launch_bounds__(kMostWaves* kWave)
-    segment_grad_kernel(Call a, const G* g, const X* dy, const float* dh_last)
-{
-    __shared__ float lds[kMostWaves][2][kWave * C];
-    const int wave = threadIdx.x / kWave, lane = lane_id();
-    const int64_t each = a.c.batch * a.c.dim, units = a.p.strips * a.c.batch * a.p.segments;
-    for (int64_t unit = blockIdx.x; unit < units; unit += gridDim.x) {
-        const Place p = place_of<C>(a, unit);
-        const int64_t stretch = a.p.steps / kMostWaves, row = p.b * a.c.length;
-        float m[C], e[C];
-#pragma unroll
-        for (int i = 0; i < C; ++i) {
-            m[i] = 1.0f;
-            e[i] = 0.0f;
-        }
-        for (int64_t t = p.from + (wave + 1) * stretch - kSteps; t >= p.from + wave * stretch; t -= kSteps) {
-            const int count = steps_at(t, p.n);
-            Vec<G, C> gr[kSteps];
-            Vec<X, C> dr[kSteps];
-            load_steps<C>(gr, g, row + t, a.c.g_stride, p, count);
-            load_steps<C>(dr, dy, row + t, a.c.y_stride, p, count);
-#pragma unroll
-            for (int k = kSteps - 1; k >= 0; --k) {
-                if (k < count) {
-#pragma unroll
-                    for (int i = 0; i < C; ++i) {
-                        float f, w;
-                        gate_of<SIGMOID>((float)element<C, G>(gr[k], i), f, w);
-                        m[i] = m[i] * f;
-                        e[i] = f * ((float)element<C, X>(dr[k], i) + e[i]);
-                    }
-                }
-            }
-        }
-#pragma unroll
-        for (int i = 0; i < C; ++i) {
-            lds[wave][0][lane * C + i] = m[i];
-            lds[wave][1][lane * C + i] = e[i];
-        }
-        __syncthreads();
-        if (wave == kMostWaves - 1) {
-            for (int j = kMostWaves - 2; j >= 0; --j)
-#pragma unroll
-                for (int i = 0; i < C; ++i) {
-                    const float f = lds[j][0][lane * C + i];
-                    m[i] = m[i] * f;
-                    e[i] = behind(f, lds[j][1][lane * C + i], e[i]);
-                }
-            float* to = a.workspace + p.segment * 2 * each;
-            store_floats<C>(to, p.b * a.c.dim + p.at, m, p.channels);
-            store_floats<C>(to + each, p.b * a.c.dim + p.at, e, p.channels);
-            if (p.segment == a.p.segments - 1) {       // dh0 may take dh_last's place
-                load_floats<C>(e, dh_last, p.b * a.c.dim + p.at, p.channels);
-                store_floats<C>(a.workspace + a.p.segments * 2 * each, p.b * a.c.dim + p.at, e, p.channels);
-            }
-        }
-        __syncthreads();
-    }
-}
-
-template <class X, class G, int C, bool SIGMOID>
-__global__ void __launch_bounds__(kMostWaves* kWave)
+template <class X, class G, bool SIGMOID, bool CHAIN>
+__global__ void __launch_bounds__(kMostWaves* kWave, 8)
     recurrence_grad_kernel(Call a, const G* g, const X* x, const float* states, const X* dy, const float* dh_last, G* dg,
                            X* dx, float* dh0)
 {
-    __shared__ Shared<C, 3> lds;
-    const int wave = threadIdx.x / kWave, lane = lane_id(), waves = a.p.waves;
-    const int64_t units = a.p.strips * a.c.batch * a.p.segments, tile = waves * kSteps;
+    constexpr int K = kBackwardSteps, kBlockWaves = EA_RECURRENCE_BLOCK / K;
+    __shared__ Exchange lds;
+    const int wave = wave_id(), lane = lane_id(), waves = a.p.waves;
     const int64_t blocks = (a.c.length + EA_RECURRENCE_BLOCK - 1) / EA_RECURRENCE_BLOCK;
-    int parity = 0;
-    for (int64_t unit = blockIdx.x; unit < units; unit += gridDim.x) {
-        const Place p = place_of<C>(a, unit);
-        const int64_t row = p.b * a.c.length;
-        Vec<G, C> gr[kSteps];
-        Vec<X, C> xr[kSteps], dr[kSteps];
-        float saved[C];
-        const int64_t tiles = (p.to - p.from + tile - 1) / tile;
-        int64_t t = p.from + (tiles - 1) * tile + wave * kSteps;
-        auto load = [&](int64_t t) {
-            const int count = steps_at(t, p.n);
-            load_steps<C>(gr, g, row + t, a.c.g_stride, p, count);
-            load_steps<C>(xr, x, row + t, a.c.x_stride, p, count);
-            load_steps<C>(dr, dy, row + t, a.c.y_stride, p, count);
-            if (count > 0)
-                load_floats<C>(saved, states, (p.b * blocks + t / EA_RECURRENCE_BLOCK) * a.c.dim + p.at, p.channels);
-        };
-        if (tiles > 0) load(t);
-        float e[C];
-        fold_segments<C, true>(e, a, p, dh_last);
-        for (int64_t left = tiles; left > 0; --left, t -= tile) {
-            const int count = steps_at(t, p.n);
-            float f[kSteps * C], w[kSteps * C], u[kSteps * C], d[kSteps * C], h[C], m[C], end[C], back[C];
-#pragma unroll
-            for (int k = 0; k < kSteps; ++k)
-#pragma unroll
-                for (int i = 0; i < C; ++i) {
-                    const int at = k * C + i;
-                    gate_of<SIGMOID>((float)element<C, G>(gr[k], i), f[at], w[at]);
-                    u[at] = (float)element<C, X>(xr[k], i);
-                    d[at] = (float)element<C, X>(dr[k], i);
-                    if (k >= count) {
-                        f[at] = 1.0f;
-                        w[at] = u[at] = d[at] = 0.0f;
-                    }
-                }
-#pragma unroll
-            for (int i = 0; i < C; ++i) {
-                h[i] = count > 0 ? saved[i] : 0.0f;
-                m[i] = 1.0f;
-                end[i] = back[i] = 0.0f;
-            }
-            if (left > 1) load(t - tile);
-#pragma unroll
-            for (int k = 0; k < kSteps; ++k)
-#pragma unroll
-                for (int i = 0; i < C; ++i) {
-                    m[i] = m[i] * f[k * C + i];
-                    end[i] = __builtin_fmaf(f[k * C + i], end[i], w[k * C + i] * u[k * C + i]);
-                }
-#pragma unroll
-            for (int k = kSteps - 1; k >= 0; --k)
-#pragma unroll
-                for (int i = 0; i < C; ++i) back[i] = f[k * C + i] * (d[k * C + i] + back[i]);
-#pragma unroll
-            for (int i = 0; i < C; ++i) {
-                lds.v[parity][wave][0][lane * C + i] = m[i];
-                lds.v[parity][wave][1][lane * C + i] = end[i];
-                lds.v[parity][wave][2][lane * C + i] = back[i];
-            }
+    for (Items<CHAIN> it(a, &lds.item); it.item < a.items;) {
+        const Place p = place_of(a, it.item, true);
+        it.draw(a);
+        const int64_t t = (int64_t)(p.chunk * waves + wave) * K, row = p.b * a.c.length + t;
+        const int count = steps_at<K>(t, p.n), held = steps_at<K>(t, (int)a.c.length);
+        zero_steps<K>(dx, row, a.c.x_stride, a, p, count, held);
+        zero_steps<K>(dg, row, a.c.g_stride, a, p, count, held);
+        if (p.chunk > p.last) {
             __syncthreads();
-            // the state before the wave's first step, from the saved one before it
-            for (int j = wave / kGroupWaves * kGroupWaves; j < wave; ++j)
-#pragma unroll
-                for (int i = 0; i < C; ++i)
-                    h[i] = behind(lds.v[parity][j][0][lane * C + i], lds.v[parity][j][1][lane * C + i], h[i]);
-            float mine[C];
-            for (int j = waves - 1; j >= 0; --j)
-#pragma unroll
-                for (int i = 0; i < C; ++i) {
-                    if (j == wave) mine[i] = e[i];
-                    e[i] = behind(lds.v[parity][j][0][lane * C + i], lds.v[parity][j][2][lane * C + i], e[i]);
-                }
-            parity ^= 1;
-            float before[kSteps * C];
-#pragma unroll
-            for (int k = 0; k < kSteps; ++k)
-#pragma unroll
-                for (int i = 0; i < C; ++i) {
-                    before[k * C + i] = h[i];
-                    h[i] = __builtin_fmaf(f[k * C + i], h[i], w[k * C + i] * u[k * C + i]);
-                }
-#pragma unroll
-            for (int k = kSteps - 1; k >= 0; --k) {
-                float od[C], og[C];
-#pragma unroll
-                for (int i = 0; i < C; ++i) {
-                    const int at = k * C + i;
-                    const float s = d[at] + mine[i];
-                    mine[i] = f[at] * s;
-                    od[i] = w[at] * s;
-                    og[i] = SIGMOID ? s * (before[at] - u[at]) * (f[at] * w[at]) : s * before[at];
-                    if (k >= count) {
-                        mine[i] = s;
-                        od[i] = og[i] = 0.0f;
-                    }
-                }
-                if (t + k < p.to && p.channels > 0) {
-                    X* tx = dx + (row + t + k) * a.c.x_stride + p.at;
-                    G* tg = dg + (row + t + k) * a.c.g_stride + p.at;
-                    if (p.channels == C) {
-                        store_vec<C>(tx, narrow_from<C, X>(od));
-                        store_vec<C>(tg, narrow_from<C, G>(og));
-                    } else {
-                        store_part<C>(tx, narrow_from<C, X>(od), p.channels);
-                        store_part<C>(tg, narrow_from<C, G>(og), p.channels);
-                    }
-                }
-            }
+            it.next(a);
+            __syncthreads();
+            continue;
         }
-        __syncthreads();                               // every wave has dh_last: dh0 may take its place
-        if (dh0 && wave == 0 && p.segment == 0) store_floats<C>(dh0, p.b * a.c.dim + p.at, e, p.channels);
+        G gr[K];
+        X xr[K], dr[K];
+        load_steps<K>(gr, g, row, a.c.g_stride, a, p, count);
+        load_steps<K>(xr, x, row, a.c.x_stride, a, p, count);
+        load_steps<K>(dr, dy, row, a.c.y_stride, a, p, count);
+        float h = 0.0f;
+        if (count > 0 && p.on) h = states[(p.b * blocks + t / EA_RECURRENCE_BLOCK) * a.c.dim + p.channel];
+        float f[K], w[K], u[K], d[K], m = 1.0f, end = 0.0f, back = 0.0f;
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            gate_of<SIGMOID>((float)gr[k], f[k], w[k]);
+            u[k] = (float)xr[k];
+            d[k] = (float)dr[k];
+        }
+        mask_steps<K>(f, u, count);
+        mask_steps<K>(w, d, count);
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            m = m * f[k];
+            end = __builtin_fmaf(f[k], end, w[k] * u[k]);
+        }
+#pragma unroll
+        for (int k = K - 1; k >= 0; --k) back = f[k] * (d[k] + back);
+        lds.wave[wave][0][lane] = m;
+        lds.wave[wave][1][lane] = end;
+        lds.wave[wave][2][lane] = back;
+        const bool first = p.chunk == 0;
+        const uint32_t after = p.last - p.chunk;
+        const int place = CHAIN ? (int)(after % kGroup) : 0;
+        __syncthreads();
+        it.next(a);
+        float e;
+        if (CHAIN) {
+            meet<true>(a, p, lds, 2, after / kGroup, place, first, dh_last);
+            __syncthreads();
+            e = fold_chunks(lds, place);
+        } else {
+            e = end_at(dh_last, a, p);
+        }
+#pragma unroll 4
+        for (int j = waves - 1; j > wave; --j) e = behind(lds.wave[j][0][lane], lds.wave[j][2][lane], e);
+        if (CHAIN && place == kGroup - 1 && !first && wave == 0 && p.on)
+            hand_out(group_word(a, p, after / kGroup + 1), behind(m, back, e));
+        // the state before the wave's first step, from the saved one before it
+#pragma unroll 4
+        for (int j = wave / kBlockWaves * kBlockWaves; j < wave; ++j)
+            h = behind(lds.wave[j][0][lane], lds.wave[j][1][lane], h);
+        // u becomes what the step's gradient is multiplied by for its gate
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            const float before = h;
+            h = __builtin_fmaf(f[k], h, w[k] * u[k]);
+            u[k] = SIGMOID ? (before - u[k]) * (f[k] * w[k]) : before;
+        }
+        X* tx = dx + (row + K - 1) * a.c.x_stride;
+        G* tg = dg + (row + K - 1) * a.c.g_stride;
+#pragma unroll
+        for (int k = K - 1; k >= 0; --k, tx -= a.c.x_stride, tg -= a.c.g_stride) {
+            const float s = d[k] + e;
+            e = f[k] * s;                              // f = 1, d = 0 where the step does not count
+            store_own<X>(row_of(tx, a, k < count), p, (X)(w[k] * s));
+            store_own<G>(row_of(tg, a, k < count), p, (G)(u[k] * s));
+        }
+        __syncthreads();                               // every wave has dh_last, and what is in LDS
+        if (first && wave == 0 && p.on && dh0) dh0[p.b * a.c.dim + p.channel] = e;
     }
 }
 
@@ -210,31 +112,22 @@ hipError_t launch_recurrence_grad(const ea_recurrence_t& c, const void* g, const
                                   float* dh0, void* workspace, hipStream_t s)
 {
     using namespace rec;
-    const int channels = channels_of(c, true);
-    const Call a{c, plan_of(c, channels), lengths, (float*)workspace};
-    const int64_t units = a.p.strips * c.batch * a.p.segments;
-    if (units == 0) return hipSuccess;
-    const unsigned groups = (unsigned)(units < kMostUnits ? units : kMostUnits);
-    auto start = [&](auto xt, auto gt, auto ct, auto sigmoid) {
+    Call a;
+    unsigned groups;
+    const hipError_t status = begin(a, c, kBackwardSteps, lengths, workspace, &groups, s);
+    if (status != hipSuccess || groups == 0) return status;
+    return with_kinds(c, [&](auto xt, auto gt, auto sigmoid) {
         using X = decltype(xt);
         using G = decltype(gt);
-        constexpr int C = decltype(ct)::value;
         constexpr bool S = decltype(sigmoid)::value;
-        if (a.p.segments > 1)
-            hipLaunchKernelGGL((segment_grad_kernel<X, G, C, S>), dim3(groups), dim3(kMostWaves * kWave), 0, s, a,
-                               (const G*)g, (const X*)dy, dh_last);
-        hipLaunchKernelGGL((recurrence_grad_kernel<X, G, C, S>), dim3(groups), dim3(a.p.waves * kWave), 0, s, a,
-                           (const G*)g, (const X*)x, states, (const X*)dy, dh_last, (G*)dg, (X*)dx, dh0);
+        const dim3 grid(groups), block(a.p.waves * kWave);
+        if (a.p.chunks > 1)
+            hipLaunchKernelGGL((recurrence_grad_kernel<X, G, S, true>), grid, block, 0, s, a, (const G*)g, (const X*)x,
+                               states, (const X*)dy, dh_last, (G*)dg, (X*)dx, dh0);
+        else
+            hipLaunchKernelGGL((recurrence_grad_kernel<X, G, S, false>), grid, block, 0, s, a, (const G*)g, (const X*)x,
+                               states, (const X*)dy, dh_last, (G*)dg, (X*)dx, dh0);
         return hipGetLastError();
-    };
-    return with_type(c.x_type, [&](auto xt) {
-        return with_type(c.g_type, [&](auto gt) {
-            constexpr std::integral_constant<int, 1> one{};
-            constexpr std::integral_constant<int, 2> two{};
-            if (c.gate == EA_GATE_SIGMOID)
-                return channels == 1 ? start(xt, gt, one, std::true_type{}) : start(xt, gt, two, std::true_type{});
-            return channels == 1 ? start(xt, gt, one, std::false_type{}) : start(xt, gt, two, std::false_type{});
-        });
     });
 }
 

@@ -204,7 +204,8 @@ def test_growing_gates_from_zero_states_stay_what_the_steps_give():
     g, x = torch.full((1, n, dim), 2.0 ** 20, device="cuda"), torch.zeros((1, n, dim), device="cuda")
     c = config(1, n, dim, torch.float32, torch.float32, PLAIN)
     y, last = torch.full((1, n, dim), 3.0, device="cuda"), torch.empty((1, dim), device="cuda")
-    E.ea_recurrence(c, g, x, None, None, y, None, last, None)
+    ws = torch.empty(max(1, E.ea_recurrence_workspace_bytes(c)), dtype=torch.uint8, device="cuda")
+    E.ea_recurrence(c, g, x, None, None, y, None, last, ws)
     assert bool((y == 0).all()) and bool((last == 0).all())
 
 
