@@ -50,22 +50,21 @@ __global__ void __launch_bounds__(kMostWaves* kWave, 8)
         }
         lds.wave[wave][0][lane] = m;
         lds.wave[wave][1][lane] = e;
-        const bool last = p.chunk == p.last;
-        const int place = CHAIN ? (int)(p.chunk % kGroup) : 0;
+        const Link link = link_of(p, false);
         __syncthreads();
         it.next(a);
         float h;
         if (CHAIN) {
-            meet<false>(a, p, lds, 1, p.chunk / kGroup, place, last, h0);
+            meet<false>(a, p, link, lds, 1, h0);
             __syncthreads();
-            h = fold_chunks(lds, place);
+            h = fold_before(lds, link);
         } else {
             h = end_at(h0, a, p);
         }
 #pragma unroll 4
         for (int j = 0; j < wave; ++j) h = behind(lds.wave[j][0][lane], lds.wave[j][1][lane], h);
-        if (CHAIN && place == kGroup - 1 && !last && wave == waves - 1 && p.on)
-            hand_out(group_word(a, p, p.chunk / kGroup + 1), behind(m, e, h));
+        if (CHAIN && ends_stretch(link) && wave == waves - 1 && p.on)
+            hand_out(stretch_word(a, p, link.stretch + 1), behind(m, e, h));
         if (states && p.on && t % EA_RECURRENCE_BLOCK == 0 && t < a.c.length)
             states[(p.b * blocks + t / EA_RECURRENCE_BLOCK) * a.c.dim + p.channel] = h;
         X* to = y + row * a.c.y_stride;
@@ -75,7 +74,7 @@ __global__ void __launch_bounds__(kMostWaves* kWave, 8)
             store_own<X>(row_of(to, a, k < count), p, (X)h);
         }
         __syncthreads();                               // every wave has h0, and what is in LDS
-        if (last && wave == waves - 1 && p.on) {
+        if (link.last && wave == waves - 1 && p.on) {
             if (h_last) h_last[p.b * a.c.dim + p.channel] = h;
             if (states)                                // of the chunks behind the last
                 for (int64_t k = ((int64_t)(p.last + 1) * waves * K + EA_RECURRENCE_BLOCK - 1) / EA_RECURRENCE_BLOCK;
@@ -110,6 +109,7 @@ Plan plan_of(const ea_recurrence_t& c, int steps)
     while (p.waves < kMostWaves && p.waves * steps < c.length) p.waves *= 2;
     const int64_t chunk = p.waves * steps;
     p.chunks = c.length > chunk ? (uint32_t)((c.length + chunk - 1) / chunk) : 1;
+    p.groups = (p.chunks + kGroup - 1) / kGroup;
     return p;
 }
 
@@ -117,8 +117,8 @@ Plan plan_of(const ea_recurrence_t& c, int steps)
 int64_t words_of(const ea_recurrence_t& c, const Plan& p)
 {
     if (p.chunks == 1) return 0;
-    const int64_t groups = (p.chunks + kGroup - 1) / kGroup;
-    return (kCounterWords + (2 * (int64_t)p.chunks + groups) * c.batch * c.dim + 1) / 2 * 2;
+    const int64_t pairs = (int64_t)p.chunks + p.groups, stretches = (p.groups + kGroup - 1) / kGroup;
+    return (kCounterWords + (2 * pairs + stretches) * c.batch * c.dim + 1) / 2 * 2;
 }
 
 hipError_t begin(Call& a, const ea_recurrence_t& c, int steps, const int32_t* lengths, void* workspace, unsigned* groups,

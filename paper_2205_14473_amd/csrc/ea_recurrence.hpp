@@ -9,11 +9,13 @@
 // it, in order, and runs its steps again from the true state.
 //
 // What a chunk starts with comes from the chunks before it through memory.
-// kGroup chunks form a group: a chunk hands out its product and end state as soon
-// as it has them, without waiting for anything, and the last chunk of a group
-// the true state behind it.  So a chunk waits for the state before its group and
-// folds the group's chunks before it, always in this order: the result does not
-// depend on who came first, and a wait passes from group to group only.
+// kGroup chunks form a group and kGroup groups a stretch.  A chunk hands out its
+// product and end state as soon as it has them, without waiting for anything; the
+// last chunk of a group folds the group's and hands that out; the last chunk of a
+// stretch hands out the true state behind it.  So a chunk takes the state before
+// its stretch and folds the groups, then the chunks before it, always in this
+// order: the result does not depend on who came first, and only from stretch to
+// stretch (65,536 steps forward) does one wait pass on to the next.
 // Workgroups draw their chunks from a counter, in the order of the steps: who
 // waits, waits for workgroups that have begun.  A wait of a good part of a second
 // is given up, and the state is NaN.
@@ -28,7 +30,7 @@ namespace rec {
 
 constexpr int kMostWaves = 16;
 constexpr int kGroup = 16;                             // chunks; one wave waits for each of those before, one for the state
-static_assert(kGroup <= kMostWaves, "a group's earlier chunks and the state before it have a wave each");
+static_assert(kGroup <= kMostWaves, "a group's earlier chunks have a wave each, and so have the state before and its groups");
 
 // Division of numbers under 2^31 by a number known to the host: (h + (n - h) / 2) / 2^shift for the high half h of
 // n * factor, in scalar instructions.
@@ -50,12 +52,12 @@ struct Divisor {
 
 struct Plan {
     uint32_t strips;                                   // of 64 channels
-    uint32_t chunks;                                   // of a sequence
+    uint32_t chunks, groups;                           // of a sequence
     int waves;                                         // of a chunk
 };
 
 // 64-bit words in the workspace: a counter, then for each chunk, sequence and channel the product and the end state, then
-// for each group the state before it.  The upper half of a word that has been handed out is 1: it and the value in the
+// the same for each group, then for each stretch the state before it.  The upper half of a word that has been handed out is 1: it and the value in the
 // lower half become visible together, and nothing else has to be ordered.
 struct Call {
     ea_recurrence_t c;
@@ -119,14 +121,16 @@ struct Items {
     }
 };
 
-__device__ __forceinline__ uint64_t* chunk_words(const Call& a, const Place& p, uint32_t chunk)
+// Words of the lane's channel: two of chunk `at` of all, or of group at - chunks; one of stretch `at`.
+__device__ __forceinline__ uint64_t* pair_of(const Call& a, const Place& p, uint32_t at)
 {
-    return a.words + kCounterWords + ((chunk * a.c.batch + p.b) * a.c.dim + p.channel) * 2;
+    return a.words + kCounterWords + (((int64_t)at * a.c.batch + p.b) * a.c.dim + p.channel) * 2;
 }
 
-__device__ __forceinline__ uint64_t* group_word(const Call& a, const Place& p, uint32_t group)
+__device__ __forceinline__ uint64_t* stretch_word(const Call& a, const Place& p, uint32_t stretch)
 {
-    return a.words + kCounterWords + (((int64_t)a.p.chunks * 2 + group) * a.c.batch + p.b) * a.c.dim + p.channel;
+    const int64_t pairs = (int64_t)a.p.chunks + a.p.groups;
+    return a.words + kCounterWords + ((pairs * 2 + stretch) * a.c.batch + p.b) * a.c.dim + p.channel;
 }
 
 __device__ __forceinline__ void hand_out(uint64_t* word, float v)
@@ -138,28 +142,35 @@ constexpr int kMostPolls = 1 << 18;                    // about a microsecond ea
 
 // N consecutive words, once all have been handed out.
 template <int N>
-__device__ __forceinline__ void await(float* v, const uint64_t* words, bool on)
-{
+struct Wanted {
     uint64_t w[N];
-    for (int i = 0;; ++i) {
-        bool ready = true;
+    __device__ void ask(const uint64_t* from, bool on)
+    {
 #pragma unroll
-        for (int k = 0; k < N; ++k) {
-            w[k] = on ? __hip_atomic_load(words + k, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : (uint64_t)1 << 32;
-            ready = ready && w[k] >> 32 == 1;
-        }
-        if (__ballot(!ready) == 0) break;
-        if (i == kMostPolls) {
-#pragma unroll
-            for (int k = 0; k < N; ++k)
-                if (w[k] >> 32 != 1) w[k] = 0x7FC00000u;
-            break;
-        }
-        __builtin_amdgcn_s_sleep(1);
+        for (int k = 0; k < N; ++k)
+            w[k] = on ? __hip_atomic_load(from + k, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : (uint64_t)1 << 32;
     }
+    __device__ bool ready() const
+    {
+        bool all = true;
 #pragma unroll
-    for (int k = 0; k < N; ++k) v[k] = __uint_as_float((uint32_t)w[k]);
-}
+        for (int k = 0; k < N; ++k) all = all && w[k] >> 32 == 1;
+        return all;
+    }
+    __device__ void wait(const uint64_t* from, bool on)
+    {
+        for (int i = 0; __ballot(!ready()) != 0; ++i) {
+            if (i == kMostPolls) {
+#pragma unroll
+                for (int k = 0; k < N; ++k) w[k] = 0x7FC00000u;
+                break;
+            }
+            __builtin_amdgcn_s_sleep(1);
+            ask(from, on);
+        }
+    }
+    __device__ float value(int k) const { return __uint_as_float((uint32_t)w[k]); }
+};
 
 // A row through a descriptor of its `dim` elements, or of none: lanes without a channel, and steps that do not count, read
 // 0 and write nothing, and neither branches nor addresses take vector registers (108 -> 60 of them in the binary32 forward
@@ -265,19 +276,33 @@ __device__ __forceinline__ float end_at(const float* p, const Call& a, const Pla
 struct Exchange {
     float wave[kMostWaves][3][kWave];                  // each wave's product, and what its steps lead to from 0
     float chunk[kGroup][2][kWave];                     // the same of the group's chunks before this one
-    float start[kWave];                                // the state before the group
+    float group[kGroup][2][kWave];                     // of the stretch's groups before this one
+    float start[kWave];                                // the state before the stretch
     uint32_t item;
 };
 
+// A chunk's place in its chain.
+struct Link {
+    int chunk, group;                                  // of its group, of its stretch
+    uint32_t groups, stretch;                          // groups before its own, stretches before its own
+    bool first, last;
+};
+
+__device__ __forceinline__ Link link_of(const Place& p, bool reverse)
+{
+    const uint32_t at = reverse ? p.last - p.chunk : p.chunk, groups = at / kGroup;
+    return Link{(int)(at % kGroup), (int)(groups % kGroup), groups, groups / kGroup, at == 0, at == p.last};
+}
+
 // Hands out the chunk's product and end value (value `which` of each wave; REVERSE: from its last wave to its first) and
-// gathers the state before its group, `place` chunks behind it and all of those: what fold_chunks() needs after a barrier.
+// gathers in LDS what fold_before() needs behind a barrier.
 template <bool REVERSE>
-__device__ __forceinline__ void meet(const Call& a, const Place& p, Exchange& x, int which, uint32_t group, int place,
-                                     bool last, const float* start)
+__device__ __forceinline__ void meet(const Call& a, const Place& p, const Link& l, Exchange& x, int which, const float* start)
 {
     const int wave = wave_id(), lane = lane_id();
-    if (wave == 0 && !last && place < kGroup - 1) {
-        float m = 1.0f, v = 0.0f;
+    const bool ends = l.chunk == kGroup - 1 && !l.last;
+    float m = 1.0f, v = 0.0f;
+    if (wave == 0 && !l.last) {
 #pragma unroll 4
         for (int i = 0; i < kMostWaves; ++i) {
             const int j = REVERSE ? kMostWaves - 1 - i : i;
@@ -285,38 +310,76 @@ __device__ __forceinline__ void meet(const Call& a, const Place& p, Exchange& x,
             m = m * f;
             v = behind(f, x.wave[j][which][lane], v);
         }
-        if (p.on) {
-            uint64_t* to = chunk_words(a, p, p.chunk);
+        if (p.on && !ends) {
+            uint64_t* to = pair_of(a, p, p.chunk);
             hand_out(to, m);
             hand_out(to + 1, v);
         }
     }
-    if (wave < place) {
-        float v[2];
-        const int back = place - wave;                 // chunks between that one and this
-        await<2>(v, chunk_words(a, p, REVERSE ? p.chunk + back : p.chunk - back), p.on);
-        x.chunk[wave][0][lane] = v[0];
-        x.chunk[wave][1][lane] = v[1];
-    } else if (wave == kMostWaves - 1) {
-        float v;
-        if (group == 0 && place == 0) {
-            v = end_at(start, a, p);
-            if (!last && p.on) hand_out(group_word(a, p, 0), v);
-        } else {
-            await<1>(&v, group_word(a, p, group), p.on);
+    // Each wave waits for one chunk, then one group; the last one for the state before the stretch.
+    if (wave < l.chunk) {
+        const int back = l.chunk - wave;               // chunks between that one and this
+        const uint64_t* from = pair_of(a, p, REVERSE ? p.chunk + back : p.chunk - back);
+        Wanted<2> chunk;
+        chunk.ask(from, p.on);
+        chunk.wait(from, p.on);
+        x.chunk[wave][0][lane] = chunk.value(0);
+        x.chunk[wave][1][lane] = chunk.value(1);
+    }
+    if (ends && l.group < kGroup - 1) {                // the group's, before anything else is waited for
+        __syncthreads();
+        if (wave == 0 && p.on) {
+            float gm = 1.0f, gv = 0.0f;
+#pragma unroll 4
+            for (int i = 0; i < kGroup - 1; ++i) {
+                gm = gm * x.chunk[i][0][lane];
+                gv = behind(x.chunk[i][0][lane], x.chunk[i][1][lane], gv);
+            }
+            uint64_t* to = pair_of(a, p, a.p.chunks + l.groups);
+            hand_out(to, gm * m);
+            hand_out(to + 1, behind(m, v, gv));
         }
-        x.start[lane] = v;
+    }
+    if (wave < l.group) {
+        const uint64_t* from = pair_of(a, p, a.p.chunks + l.groups - l.group + wave);
+        Wanted<2> group;
+        group.ask(from, p.on);
+        group.wait(from, p.on);
+        x.group[wave][0][lane] = group.value(0);
+        x.group[wave][1][lane] = group.value(1);
+    }
+    if (wave == kMostWaves - 1) {
+        // The first chunk passes on what it starts with, too: the last one may write its own in the same place.
+        if (l.first) {
+            const float h = end_at(start, a, p);
+            if (p.on && !l.last) hand_out(stretch_word(a, p, 0), h);
+            x.start[lane] = h;
+        } else {
+            const uint64_t* from = stretch_word(a, p, l.stretch);
+            Wanted<1> state;
+            state.ask(from, p.on);
+            state.wait(from, p.on);
+            x.start[lane] = state.value(0);
+        }
     }
 }
 
 // The state before the chunk.
-__device__ __forceinline__ float fold_chunks(const Exchange& x, int place)
+__device__ __forceinline__ float fold_before(const Exchange& x, const Link& l)
 {
     const int lane = lane_id();
     float h = x.start[lane];
 #pragma unroll 4
-    for (int i = 0; i < place; ++i) h = behind(x.chunk[i][0][lane], x.chunk[i][1][lane], h);
+    for (int i = 0; i < l.group; ++i) h = behind(x.group[i][0][lane], x.group[i][1][lane], h);
+#pragma unroll 4
+    for (int i = 0; i < l.chunk; ++i) h = behind(x.chunk[i][0][lane], x.chunk[i][1][lane], h);
     return h;
+}
+
+// Whether the true state behind the chunk is handed out.
+__device__ __forceinline__ bool ends_stretch(const Link& l)
+{
+    return l.chunk == kGroup - 1 && l.group == kGroup - 1 && !l.last;
 }
 
 constexpr int kForwardSteps = 16, kBackwardSteps = 8;  // of a wave

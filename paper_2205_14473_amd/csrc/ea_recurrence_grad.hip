@@ -62,23 +62,21 @@ __global__ void __launch_bounds__(kMostWaves* kWave, 8)
         lds.wave[wave][0][lane] = m;
         lds.wave[wave][1][lane] = end;
         lds.wave[wave][2][lane] = back;
-        const bool first = p.chunk == 0;
-        const uint32_t after = p.last - p.chunk;
-        const int place = CHAIN ? (int)(after % kGroup) : 0;
+        const Link link = link_of(p, true);
         __syncthreads();
         it.next(a);
         float e;
         if (CHAIN) {
-            meet<true>(a, p, lds, 2, after / kGroup, place, first, dh_last);
+            meet<true>(a, p, link, lds, 2, dh_last);
             __syncthreads();
-            e = fold_chunks(lds, place);
+            e = fold_before(lds, link);
         } else {
             e = end_at(dh_last, a, p);
         }
 #pragma unroll 4
         for (int j = waves - 1; j > wave; --j) e = behind(lds.wave[j][0][lane], lds.wave[j][2][lane], e);
-        if (CHAIN && place == kGroup - 1 && !first && wave == 0 && p.on)
-            hand_out(group_word(a, p, after / kGroup + 1), behind(m, back, e));
+        if (CHAIN && ends_stretch(link) && wave == 0 && p.on)
+            hand_out(stretch_word(a, p, link.stretch + 1), behind(m, back, e));
         // the state before the wave's first step, from the saved one before it
 #pragma unroll 4
         for (int j = wave / kBlockWaves * kBlockWaves; j < wave; ++j)
@@ -100,7 +98,7 @@ __global__ void __launch_bounds__(kMostWaves* kWave, 8)
             store_own<G>(row_of(tg, a, k < count), p, (G)(u[k] * s));
         }
         __syncthreads();                               // every wave has dh_last, and what is in LDS
-        if (first && wave == 0 && p.on && dh0) dh0[p.b * a.c.dim + p.channel] = e;
+        if (link.last && wave == 0 && p.on && dh0) dh0[p.b * a.c.dim + p.channel] = e;
     }
 }
 

@@ -1,6 +1,7 @@
 """The gated linear recurrence and its gradient against 64 bits, step by step: lengths from 0 and 1 to several tiles
 and segments, types, odd widths, row gaps, padded sequences, states carried over, in place, gates of 0 and 1 and past
 the tables' ends, NaN behind a sequence's end, other streams, graphs."""
+import numpy as np
 import pytest
 
 torch = pytest.importorskip("torch")
@@ -196,6 +197,44 @@ def test_gates_at_their_ends(n):
     R.within(y, f.y, f.bound + 2.0 ** -120, "y")
     R.within(dx, want.dx, want.dx_bound + 2.0 ** -120, "dx")
     R.within(dg, want.dg, want.dg_bound + 2.0 ** -120, "dg")
+
+
+@pytest.mark.parametrize("dim,n,lengths", [(70, 70_001, [70_001, 66_000]), (3, 140_000, [131_073, 140_000, 1]), (130, 33_000, [33_000])])
+def test_long_sequences_in_whole_numbers(dim, n, lengths):
+    """Gates of 1, -1 and now and then 0 over small whole numbers: every sum is exact in binary32, in any order, and the
+    results are equal to those of the steps.  Long enough for chunks, groups and several stretches of them."""
+    rng = np.random.default_rng(n)
+    b = len(lengths)
+    a = rng.choice([1, 1, 1, -1], (b, n, dim)) * (rng.random((b, n, dim)) > 0.002)
+    x, dy = rng.integers(-2, 3, (b, n, dim)), rng.integers(-2, 3, (b, n, dim))
+    h0, dh = rng.integers(-9, 10, (b, dim)), rng.integers(-9, 10, (b, dim))
+    y, before, dx, dg = (np.zeros((b, n, dim), np.int64) for _ in range(4))
+    last, first = h0.copy(), dh.copy()
+    for i, steps in enumerate(lengths):
+        h = h0[i]
+        for t in range(steps):
+            before[i, t] = h
+            h = a[i, t] * h + x[i, t]
+            y[i, t] = h
+        last[i], e = h, dh[i]
+        for t in range(steps - 1, -1, -1):
+            d = dy[i, t] + e
+            dx[i, t], dg[i, t] = d, d * before[i, t]
+            e = a[i, t] * d
+        first[i] = e
+    assert max(abs(v).max() for v in (y, dx, dg)) < 1 << 24
+    c = config(b, n, dim, torch.float32, torch.float32, PLAIN)
+    ws = torch.empty(E.ea_recurrence_workspace_bytes(c), dtype=torch.uint8, device="cuda")
+    dev = lambda v: torch.from_numpy(v).float().cuda()  # noqa: E731
+    gd, xd, got = dev(a), dev(x), torch.empty((b, n, dim), device="cuda")
+    ld = torch.tensor(lengths, dtype=torch.int32, device="cuda")
+    states, hl = torch.empty((b, -(-n // 64), dim), device="cuda"), torch.empty((b, dim), device="cuda")
+    E.ea_recurrence(c, gd, xd, dev(h0), ld, got, states, hl, ws)
+    assert torch.equal(got.cpu().long(), torch.from_numpy(y)) and torch.equal(hl.cpu().long(), torch.from_numpy(last))
+    gx, gg = torch.empty_like(got), torch.empty_like(got)
+    E.ea_recurrence_grad(c, gd, xd, states, ld, dev(dy), dev(dh), gg, gx, hl, ws)
+    assert torch.equal(gx.cpu().long(), torch.from_numpy(dx)) and torch.equal(gg.cpu().long(), torch.from_numpy(dg))
+    assert torch.equal(hl.cpu().long(), torch.from_numpy(first))
 
 
 def test_growing_gates_from_zero_states_stay_what_the_steps_give():
