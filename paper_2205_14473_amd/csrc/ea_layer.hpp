@@ -71,16 +71,20 @@ __device__ __forceinline__ void set_element(Vec<T, N>& v, int k, T x)
         v[k] = x;
 }
 
-// The first `n` (0 to N) elements; the rest read as `rest`, and are not written.
+// The first `n` elements; the rest read as `rest`, and are not written.  All loads are made at once, the rest's from the first
+// element: a branch around each would make a row wait N times for memory.
 template <int N, class T>
 __device__ __forceinline__ Vec<T, N> load_part(const T* p, int n, float rest = 0.0f)
 {
     Vec<T, N> v;
 #pragma unroll
-    for (int k = 0; k < N; ++k) {
-        T x = (T)rest;
-        if (k < n) x = p[k];
-        set_element<N, T>(v, k, x);
+    for (int k = 0; k < N; ++k) set_element<N, T>(v, k, (T)rest);
+    if (n > 0) {
+        T x[N];
+#pragma unroll
+        for (int k = 0; k < N; ++k) x[k] = p[k < n ? k : 0];
+#pragma unroll
+        for (int k = 0; k < N; ++k) set_element<N, T>(v, k, k < n ? x[k] : (T)rest);
     }
     return v;
 }

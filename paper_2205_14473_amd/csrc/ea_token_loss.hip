@@ -20,8 +20,8 @@ namespace {
 constexpr float kLog2e = 0x1.715476p+0f;
 constexpr int kCountBlock = 1024;
 constexpr int64_t kMostCounts = 256;                   // workgroups that count
-constexpr int64_t kOwnCount = 4096;                    // targets that every workgroup counts by itself
-constexpr int64_t kMostGroups = 2048;                  // workgroups of the main pass, each with a sum of its own
+constexpr int64_t kOwnCount = 8;                       // targets a thread, up to which every workgroup counts all itself
+constexpr int64_t kMostWaves = 4096;                   // of the main pass, 16 a CU: each row's group of them leaves one sum
 constexpr int kEndBlock = 256;
 
 // Workspace: the counting groups' counts, then each main group's sum and count.
@@ -40,10 +40,11 @@ struct Loss {
     int32_t parts;
 };
 
-__device__ __forceinline__ int64_t target_at(const Loss& a, int64_t row)
+// The target of a row, -1 where it does not count.
+__device__ __forceinline__ int target_at(const Loss& a, int64_t row)
 {
     const int64_t t = a.c.index_bits == 64 ? ((const int64_t*)a.targets)[row] : (int64_t)((const int32_t*)a.targets)[row];
-    return t >= 0 && t < a.c.vocab ? t : -1;
+    return t >= 0 && t < a.c.vocab ? (int)t : -1;
 }
 
 // The workgroup's sum of integers; every thread gets it.
@@ -78,7 +79,11 @@ __device__ __forceinline__ float row_factor(const Loss& a)
     if (a.counts) {
         for (int i = threadIdx.x; i < a.parts; i += THREADS) n += a.counts[i];
     } else {
-        for (int64_t i = threadIdx.x; i < a.c.rows; i += THREADS) n += target_at(a, i) >= 0;
+#pragma unroll
+        for (int k = 0; k < kOwnCount; ++k) {
+            const int64_t i = (int64_t)k * THREADS + threadIdx.x;
+            if (i < a.c.rows) n += target_at(a, i) >= 0;
+        }
     }
     n = group_count<THREADS>(n);
     return n > 0 ? (float)((double)a.c.scale / (double)n) : 0.0f;
@@ -134,110 +139,191 @@ __device__ __forceinline__ void as_floats(float* x, Words w)
     widen_to<V, T>(x, __builtin_bit_cast(Vec<T, V>, w));
 }
 
-template <class T>
-__device__ __forceinline__ Words load_words(const T* row, int at, int vocab)
+// A row as a wave sees it: vectors of 16 bytes on a grid of cache lines, the first of which may begin before the row and
+// the last end behind it.  (8,192 rows of 50,257 logits of 16 bits, with the gradient: 442 us with vectors from the row's
+// own start on, 404 with the 16-byte grid, 358 here.)
+// Bytes of the grid's cells: short rows, one wave each, take a vector's, which costs them fewer vectors.
+constexpr int cell_of(int waves)
 {
-    constexpr int V = 16 / sizeof(T);
-    const int left = vocab - at;
-    if (left >= V) return *(const WordsAt*)(row + (uint32_t)at);
-    return __builtin_bit_cast(Words, load_part<V>(row + at, left, -__builtin_inff()));
+    return waves == 1 ? 16 : 128;
 }
 
 template <class T>
-__device__ __forceinline__ void store_floats_of(T* row, int at, int vocab, const float* x)
+struct Grid {
+    T* row;                                            // the cell that holds the row's start
+    int head, end;                                     // the row's elements from there on: [head, end)
+    // the same cells of another row
+    template <class O>
+    __device__ Grid(T* p, const Grid<O>& like) : row(p - like.head), head(like.head), end(like.end)
+    {
+    }
+    __device__ Grid(T* p, int vocab, int cell)
+    {
+        head = (int)((uintptr_t)p % (uintptr_t)cell / sizeof(T));
+        row = p - head;
+        end = vocab + head;
+    }
+};
+
+// The wave's 64 vectors from element `at` on: all inside, none, or some of their elements.  The piece's address is a
+// scalar, kept one for each piece (opaque), and the lane's part of it the same for all: otherwise every piece's address
+// takes two registers, which are a third of those that hold the row.
+template <class T>
+__device__ __forceinline__ T* piece(T* row, int at)
+{
+    T* p = row + at;
+    asm volatile("" : "+s"(p));
+    return p;
+}
+
+// The wave's vectors, -infinity outside the row.  One that holds an element of the row is read whole: it lies in one
+// cell of 16 bytes, and so in memory that is allocated if the element is, and what it holds of others has no effect.
+template <class T>
+__device__ __forceinline__ Words load_words(const Grid<const T>& g, int at)
 {
     constexpr int V = 16 / sizeof(T);
-    const int left = vocab - at;
-    if (left >= V)
-        store_vec<V>(row + (uint32_t)at, narrow_from<V, T>(x));
-    else
-        store_part<V>(row + at, narrow_from<V, T>(x), left);
+    const T* p = piece(g.row, at);
+    const uint32_t off = (uint32_t)lane_id() * 16u;
+    if (at >= g.head && at + kWave * V <= g.end) return *(const Words*)((const char*)p + off);
+    const int mine = at + lane_id() * V;
+    Words w = {};
+    if (mine + V > g.head && mine < g.end) w = *(const Words*)((const char*)p + off);
+    Vec<T, V> v = __builtin_bit_cast(Vec<T, V>, w);
+#pragma unroll
+    for (int k = 0; k < V; ++k) v[k] = mine + k >= g.head && mine + k < g.end ? v[k] : (T)-__builtin_inff();
+    return __builtin_bit_cast(Words, v);
 }
 
 template <class T>
-__device__ __forceinline__ void zero_row(T* to, int vocab, int lane, int lanes)
+__device__ __forceinline__ void store_floats_of(const Grid<T>& g, int at, const float* x)
+{
+    constexpr int V = 16 / sizeof(T);
+    T* p = piece(g.row, at);
+    const Vec<T, V> v = narrow_from<V, T>(x);
+    const uint32_t off = (uint32_t)lane_id() * 16u;
+    if (at >= g.head && at + kWave * V <= g.end) {
+        *(WordsAt*)((char*)p + off) = __builtin_bit_cast(Words, v);
+        return;
+    }
+    const int mine = at + lane_id() * V;
+    if (mine >= g.head && mine + V <= g.end) {
+        *(WordsAt*)((char*)p + off) = __builtin_bit_cast(Words, v);
+    } else {
+        T* q = (T*)((char*)p + off);
+#pragma unroll
+        for (int k = 0; k < V; ++k)
+            if (mine + k >= g.head && mine + k < g.end) q[k] = v[k];
+    }
+}
+
+template <class T>
+__device__ __forceinline__ void zero_row(const Grid<T>& g, int first, int lanes)
 {
     constexpr int V = 16 / sizeof(T);
     const float none[V] = {};
-    for (int at = lane * V; at < vocab; at += lanes * V) store_floats_of(to, at, vocab, none);
+    for (int at = first; at < g.end; at += lanes * V) store_floats_of(g, at, none);
 }
 
 // WAVES of a row (1: four rows a workgroup), K vectors of 16 bytes a lane; K = 0: a row that is read again.
 template <class T, int WAVES, int K, bool GRAD>
-__global__ void __launch_bounds__(WAVES == 1 ? 256 : WAVES * kWave)
+__global__ void __launch_bounds__(WAVES == 1 ? 256 : WAVES * kWave, 4)
     loss_kernel(Loss a, const T* logits, T* dlogits)
 {
     constexpr int V = 16 / sizeof(T), kRows = WAVES == 1 ? 4 : 1, kLanes = WAVES * kWave;
     constexpr int kThreads = WAVES == 1 ? 256 : kLanes;
     __shared__ float lds[2][WAVES], hit_of[kRows];
     const int lane = WAVES == 1 ? lane_id() : (int)threadIdx.x;
+    const int slot = WAVES == 1 ? wave_id() : 0, first = WAVES == 1 ? 0 : wave_id() * kWave * V;
     const int vocab = (int)a.c.vocab;
+    const int64_t step = (int64_t)gridDim.x * kRows;
+    int64_t row = (int64_t)blockIdx.x * kRows + slot;
+    int target = uniform(row < a.c.rows ? target_at(a, row) : -1);
+    const T* from = logits + (row < a.c.rows ? row : 0) * a.c.logits_stride;
+    Words z[K ? K : 1];
+    auto load = [&](const T* p) {
+        const Grid<const T> g(p, vocab, cell_of(WAVES));
+#pragma unroll
+        for (int k = 0; k < K; ++k) z[k] = load_words(g, k * kLanes * V + first);
+    };
+    if (K > 0) load(from);
     const float factor = GRAD ? row_factor<kThreads>(a) : 0.0f;
     double total = 0.0;
     int64_t used = 0;
-    for (int64_t row = (int64_t)blockIdx.x * kRows + (WAVES == 1 ? threadIdx.x / kWave : 0); row < a.c.rows;
-         row += (int64_t)gridDim.x * kRows) {
-        const int64_t target = target_at(a, row);
-        const T* from = logits + row * a.c.logits_stride;
+    while (row < a.c.rows) {
+        // The next row's vectors follow this one's into the same registers as they are used for the last time (where none
+        // follows, or one that does not count, this one's again, from the cache).
+        const int64_t row_after = row + step;
+        const int target_after = uniform(row_after < a.c.rows ? target_at(a, row_after) : -1);
+        const T* after = target_after >= 0 ? logits + row_after * a.c.logits_stride : from;
         T* to = dlogits + row * a.c.dlogits_stride;
         if (target < 0) {
             if (lane == 0 && a.loss) a.loss[row] = 0.0f;
-            if (GRAD) zero_row(to, vocab, lane, kLanes);
-            continue;
-        }
-        float top = -__builtin_inff(), sum = 0.0f, x[V];
-        Words z[K ? K : 1];
-        // f(vector, its first column) for each of the lane's vectors, from its registers or from memory again
-        auto every = [&](auto&& f) {
-            if constexpr (K > 0) {
+            if (GRAD) zero_row(Grid<T>(to, vocab, cell_of(WAVES)), first, kLanes);
+            if (K > 0) load(after);
+        } else {
+            const Grid<const T> in(from, vocab, cell_of(WAVES)), next(after, vocab, cell_of(WAVES));
+            float top = -__builtin_inff(), sum = 0.0f, x[V];
+            // f(vector, the wave's first element of it on the grid) for each of the lane's vectors, from its registers or
+            // from memory again
+            auto every = [&](auto&& f, bool last) {
+                if constexpr (K > 0) {
 #pragma unroll
-                for (int k = 0; k < K; ++k) {
-                    renew(z[k]);
-                    f(z[k], (k * kLanes + lane) * V);
+                    for (int k = 0; k < K; ++k) {
+                        const int at = k * kLanes * V + first;
+                        renew(z[k]);
+                        if (at < in.end) f(z[k], at);
+                        if (last) z[k] = load_words(next, at);
+                    }
+                } else {
+                    for (int at = first; at < in.end; at += kLanes * V) f(load_words(in, at), at);
                 }
-            } else {
-                for (int at = lane * V; at < vocab; at += kLanes * V) f(load_words(from, at, vocab), at);
+            };
+            // The target's logit, from one lane before the last reduction: when rows are written where they were read,
+            // no lane may still want it after that.
+            if (lane == 0) hit_of[slot] = (float)from[target];
+            every(
+                [&](Words w, int) {
+                    as_floats<T>(x, w);
+#pragma unroll
+                    for (int i = 0; i < V; ++i) top = fmaxf(top, x[i]);
+                },
+                false);
+            top = group_max<WAVES>(top, lds[0]);
+            every(
+                [&](Words w, int) {
+                    as_floats<T>(x, w);
+#pragma unroll
+                    for (int i = 0; i < V; ++i) sum = sum + exp_under(x[i], top);
+                },
+                !GRAD);
+            sum = group_sum<WAVES>(sum, lds[1]);
+            const float hit = hit_of[slot], loss = logf(sum) - (hit - top);
+            total = total + (double)loss;
+            ++used;
+            if (lane == 0 && a.loss) a.loss[row] = loss;
+            if constexpr (GRAD) {
+                const float share = factor / sum;
+                // the gradient's rows on the same grid as the logits, whether it is theirs or not
+                const Grid<T> out(to, in);
+                every(
+                    [&](Words w, int at) {
+                        as_floats<T>(x, w);
+#pragma unroll
+                        for (int i = 0; i < V; ++i) x[i] = exp_under(x[i], top) * share;
+                        store_floats_of(out, at, x);
+                    },
+                    true);
+                // the lane that wrote the target's element writes it again, less the factor
+                if ((target + in.head) / V % kLanes == lane) to[target] = (T)(exp_under(hit, top) * share - factor);
             }
-        };
-        if constexpr (K > 0) {
-#pragma unroll
-            for (int k = 0; k < K; ++k) z[k] = load_words(from, (k * kLanes + lane) * V, vocab);
+            if (WAVES > 1) __syncthreads();            // the next row's reductions write where this one's were read
         }
-        // The target's logit, from one lane before the last reduction: when rows are written where they were read,
-        // no lane may still want it after that.
-        if (lane == 0) hit_of[WAVES == 1 ? threadIdx.x / kWave : 0] = (float)from[target];
-        every([&](Words w, int) {
-            as_floats<T>(x, w);
-#pragma unroll
-            for (int i = 0; i < V; ++i) top = fmaxf(top, x[i]);
-        });
-        top = group_max<WAVES>(top, lds[0]);
-        every([&](Words w, int) {
-            as_floats<T>(x, w);
-#pragma unroll
-            for (int i = 0; i < V; ++i) sum = sum + exp_under(x[i], top);
-        });
-        sum = group_sum<WAVES>(sum, lds[1]);
-        const float hit = hit_of[WAVES == 1 ? threadIdx.x / kWave : 0];
-        const float loss = logf(sum) - (hit - top);
-        total = total + (double)loss;
-        ++used;
-        if (lane == 0 && a.loss) a.loss[row] = loss;
-        if constexpr (GRAD) {
-            const float share = factor / sum;
-            every([&](Words w, int at) {
-                as_floats<T>(x, w);
-#pragma unroll
-                for (int i = 0; i < V; ++i) x[i] = exp_under(x[i], top) * share;
-                store_floats_of(to, at, vocab, x);
-            });
-            // the lane that wrote the target's element writes it again, less the factor
-            if (target / V % kLanes == lane) to[target] = (T)(exp_under(hit, top) * share - factor);
-        }
-        if (WAVES > 1) __syncthreads();                // the next row's reductions write where this one's were read
+        row = row_after;
+        target = target_after;
+        from = after;
     }
     // one sum for each row's group of waves
-    if (lane == 0) a.sums[(int64_t)blockIdx.x * kRows + (WAVES == 1 ? threadIdx.x / kWave : 0)] = Sums{total, used};
+    if (lane == 0) a.sums[(int64_t)blockIdx.x * kRows + slot] = Sums{total, used};
 }
 
 // The groups' sums, in their order.
@@ -269,25 +355,48 @@ int64_t at_most(int64_t n, int64_t most)
     return n < most ? n : most;
 }
 
-// Waves of a row and vectors a lane: the smallest that hold it, or 16 and 0 where none does.
+// Waves of a row and vectors a lane: the first that holds it, or 16 and 0 where none does.  Few waves with many vectors
+// each: rows of their own work beside each other on a CU, one reading or writing while another reduces.
 struct Shape {
     int waves, k;
 };
 
+#define EA_SHAPES                                                                                                  \
+    EA_SHAPE(1, 2)                                                                                                 \
+    EA_SHAPE(1, 4)                                                                                                 \
+    EA_SHAPE(1, 8)                                                                                                 \
+    EA_SHAPE(4, 4)                                                                                                 \
+    EA_SHAPE(4, 6)                                                                                                 \
+    EA_SHAPE(4, 8)                                                                                                 \
+    EA_SHAPE(4, 12)                                                                                                \
+    EA_SHAPE(4, 16)                                                                                                \
+    EA_SHAPE(8, 10)                                                                                                \
+    EA_SHAPE(8, 12)                                                                                                \
+    EA_SHAPE(8, 13)                                                                                                \
+    EA_SHAPE(8, 14)                                                                                                \
+    EA_SHAPE(8, 16)                                                                                                \
+    EA_SHAPE(16, 10)                                                                                               \
+    EA_SHAPE(16, 12)                                                                                               \
+    EA_SHAPE(16, 14)                                                                                               \
+    EA_SHAPE(16, 16)
+
 Shape shape_of(const ea_token_loss_t& c)
 {
     const int64_t v = c.type == EA_F32 ? 4 : 8;
-    const Shape all[] = {{1, 2}, {1, 4}, {4, 2}, {4, 4}, {16, 2}, {16, 3}, {16, 4},
-                         {16, 5}, {16, 6}, {16, 7}, {16, 8}, {16, 10}, {16, 12}, {16, 14}, {16, 16}};
+    const Shape all[] = {
+#define EA_SHAPE(W, K) {W, K},
+        EA_SHAPES
+#undef EA_SHAPE
+    };
     for (const Shape& s : all)
-        if (c.vocab <= v * kWave * s.waves * s.k) return s;
+        if (c.vocab + cell_of(s.waves) / 16 * v - 1 <= v * kWave * s.waves * s.k) return s;   // wherever in a cell a row starts
     return {16, 0};
 }
 
 // Workgroups of the main pass, and the sums they leave.
 int64_t groups_of(const ea_token_loss_t& c, Shape s)
 {
-    return s.waves == 1 ? at_most((c.rows + 3) / 4, kMostGroups) : at_most(c.rows, kMostGroups);
+    return s.waves == 1 ? at_most((c.rows + 3) / 4, kMostWaves / 2) : at_most(c.rows, kMostWaves / s.waves);
 }
 
 int64_t sums_of(const ea_token_loss_t& c, Shape s)
@@ -297,7 +406,8 @@ int64_t sums_of(const ea_token_loss_t& c, Shape s)
 
 int64_t counting_groups(const ea_token_loss_t& c)
 {
-    return c.rows > kOwnCount ? at_most((c.rows + kCountBlock * 4 - 1) / (kCountBlock * 4), kMostCounts) : 0;
+    const int waves = shape_of(c).waves, threads = waves == 1 ? 256 : waves * kWave;
+    return c.rows > kOwnCount * threads ? at_most((c.rows + kCountBlock * 4 - 1) / (kCountBlock * 4), kMostCounts) : 0;
 }
 
 template <class T, bool GRAD>
@@ -309,21 +419,7 @@ hipError_t start_loss(const Loss& a, Shape s, unsigned groups, const void* logit
                            (const T*)logits, (T*)dlogits);                                                        \
         return hipGetLastError();                                                                                 \
     }
-    EA_SHAPE(1, 2)
-    EA_SHAPE(1, 4)
-    EA_SHAPE(4, 2)
-    EA_SHAPE(4, 4)
-    EA_SHAPE(16, 2)
-    EA_SHAPE(16, 3)
-    EA_SHAPE(16, 4)
-    EA_SHAPE(16, 5)
-    EA_SHAPE(16, 6)
-    EA_SHAPE(16, 7)
-    EA_SHAPE(16, 8)
-    EA_SHAPE(16, 10)
-    EA_SHAPE(16, 12)
-    EA_SHAPE(16, 14)
-    EA_SHAPE(16, 16)
+    EA_SHAPES
     EA_SHAPE(16, 0)
 #undef EA_SHAPE
     return hipErrorInvalidValue;
