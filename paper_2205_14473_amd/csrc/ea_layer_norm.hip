@@ -20,51 +20,82 @@ namespace {
 constexpr int kHeldColumns = 16;                       // a lane's, at most
 constexpr int kLongBlock = 1024;                       // threads of a row that is not held
 
-template <class X, class Y>
+// Elements of a vector: 16 bytes of the narrower type, or four where rows are no whole number of those (TAIL).
+template <class X, class Y, bool TAIL>
 constexpr int vec_of()
 {
-    return sizeof(X) == 2 && sizeof(Y) == 2 ? 8 : 4;
+    return !TAIL && sizeof(X) == 2 && sizeof(Y) == 2 ? 8 : 4;
 }
 
-// Elements of a vector at column `at` that lie inside the row.
-template <int V>
-__device__ __forceinline__ int inside(int64_t at, int64_t dim)
+// A vector moved down by some of its elements, zeros behind.
+template <int V, class T>
+__device__ __forceinline__ Vec<T, V> moved_down(Vec<T, V> v, int by)
 {
-    const int64_t left = dim - at;
-    return left >= V ? V : left > 0 ? (int)left : 0;
+    const int bits = by * 8 * (int)sizeof(T), rest = bits & 63;
+    if constexpr (sizeof(v) == 16) {
+        typedef uint64_t Two __attribute__((ext_vector_type(2)));
+        const Two w = __builtin_bit_cast(Two, v);
+        const uint64_t low = bits < 64 ? w[0] : w[1], high = bits < 64 ? w[1] : 0;
+        const Two moved = {(low >> rest) | (rest ? high << (64 - rest) : 0), high >> rest};
+        return __builtin_bit_cast(Vec<T, V>, moved);
+    } else {
+        return __builtin_bit_cast(Vec<T, V>, __builtin_bit_cast(uint64_t, v) >> rest);
+    }
+}
+
+constexpr int kTail = 1, kTiny = 2;
+
+// The row's vector at column `at`, zeros behind its end.  tail: it may cross the end; it is then the row's last whole one,
+// moved down, so that a vector is one load and nothing outside the row is read (kTiny: the row may be shorter than one).  (Elements one by one for rows of no whole
+// number of vectors: 65,536 x 1,001 bfloat16 135 us, its gradient 378; FIGURES this way.)
+template <int V, class T>
+__device__ __forceinline__ void load_row(float* x, const T* row, int at, int dim, int tail)
+{
+    if constexpr (sizeof(T) * V > 16) {
+        load_row<V / 2>(x, row, at, dim, tail);
+        load_row<V / 2>(x + V / 2, row, at + V / 2, dim, tail);
+    } else {
+        Vec<T, V> v = {};
+        if (tail == kTiny && dim < V) {
+            v = load_part<V>(row + at, dim - at);
+        } else if (at < dim) {
+            const int from = !tail || at < dim - V ? at : dim - V;
+            v = *(const typename VecOf<T, V>::unaligned*)((const char*)row + (uint32_t)from * (uint32_t)sizeof(T));
+            if (tail) v = moved_down<V, T>(v, at - from);
+        }
+        widen_to<V, T>(x, v);
+    }
 }
 
 template <int V, class T>
-__device__ __forceinline__ void load_some_of(float* x, const T* row, int64_t at, int n)
+__device__ __forceinline__ void store_row(T* row, int at, const float* x, int dim, bool tail)
 {
-    if (n == V)
-        widen_to<V, T>(x, load_vec<V>(row + at));
-    else
-        widen_to<V, T>(x, load_part<V>(row + at, n));
-}
-
-template <int V, class T>
-__device__ __forceinline__ void store_some_of(T* row, int64_t at, const float* x, int n)
-{
-    if (n == V)
-        store_vec<V>(row + at, narrow_from<V, T>(x));
-    else
-        store_part<V>(row + at, narrow_from<V, T>(x), n);
+    T* to = (T*)((char*)row + (uint32_t)at * (uint32_t)sizeof(T));
+    if (at < dim && (!tail || at + V <= dim))
+        store_vec<V>(to, narrow_from<V, T>(x));
+    else if (tail && at < dim)
+        store_part<V>(to, narrow_from<V, T>(x), dim - at);
 }
 
 // weight or bias, or what stands for it where there is none
 template <int V>
-__device__ __forceinline__ void load_weights(float* x, const void* w, int32_t type, int64_t at, int n, float none)
+__device__ __forceinline__ void load_weights(float* x, const void* w, int32_t type, int at, int dim, float none, int tail)
 {
 #pragma unroll
     for (int k = 0; k < V; ++k) x[k] = none;
-    if (!w || n == 0) return;
+    if (!w) return;
     if (type == EA_F32)
-        load_some_of<V>(x, (const float*)w, at, n);
+        load_row<V>(x, (const float*)w, at, dim, tail);
     else if (type == EA_BF16)
-        load_some_of<V>(x, (const bf16*)w, at, n);
+        load_row<V>(x, (const bf16*)w, at, dim, tail);
     else
-        load_some_of<V>(x, (const f16*)w, at, n);
+        load_row<V>(x, (const f16*)w, at, dim, tail);
+}
+
+// Floats of a partial row of dweight, and of dbias behind it: whole vectors, what lies behind the columns is not looked at.
+__host__ __device__ constexpr int64_t partial_row(int64_t dim)
+{
+    return (dim + 7) / 8 * 8;
 }
 
 // Sums of one or two values over the waves of a row; every thread gets them.
@@ -74,7 +105,7 @@ __device__ __forceinline__ void row_sums(float& a, float& b, float2* lds)
     a = wave_sum(a);
     b = wave_sum(b);
     if (WAVES == 1) return;
-    const int wave = threadIdx.x / kWave;
+    const int wave = wave_id();
     if (lane_id() == 0) lds[wave] = make_float2(a, b);
     __syncthreads();
     a = b = 0.0f;
@@ -97,30 +128,27 @@ __device__ __forceinline__ float row_sum(float a, float2* lds)
 
 // ---- forward --------------------------------------------------------------------
 
-template <class X, class Y, int WAVES, int K>
+template <class X, class Y, bool TAIL, int WAVES, int K>
 __global__ void __launch_bounds__(WAVES == 1 ? 256 : WAVES * kWave)
     norm_kernel(ea_layer_norm_t c, const X* x, const void* weight, const void* bias, Y* y, float* mean, float* rstd)
 {
-    constexpr int V = vec_of<X, Y>();
-    constexpr int kRows = WAVES == 1 ? 4 : 1;          // of a workgroup
+    constexpr int V = vec_of<X, Y, TAIL>(), kRows = WAVES == 1 ? 4 : 1;          // of a workgroup
     __shared__ float2 lds[WAVES];
-    const int lane = WAVES == 1 ? lane_id() : (int)threadIdx.x;
+    const int lane = WAVES == 1 ? lane_id() : (int)threadIdx.x, dim = (int)c.dim;
     float w[K * V], b[K * V];
-    int n[K];
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-        const int64_t at = (int64_t)(k * WAVES * kWave + lane) * V;
-        n[k] = inside<V>(at, c.dim);
-        load_weights<V>(w + k * V, weight, c.w_type, at, n[k], 1.0f);
-        load_weights<V>(b + k * V, bias, c.w_type, at, n[k], 0.0f);
+        const int at = (k * WAVES * kWave + lane) * V;
+        load_weights<V>(w + k * V, weight, c.w_type, at, dim, 1.0f, !TAIL || k < K - 1 ? 0 : WAVES * K == 1 ? kTiny : kTail);
+        load_weights<V>(b + k * V, bias, c.w_type, at, dim, 0.0f, !TAIL || k < K - 1 ? 0 : WAVES * K == 1 ? kTiny : kTail);
     }
-    const float each = 1.0f / (float)c.dim;
-    for (int64_t row = (int64_t)blockIdx.x * kRows + (WAVES == 1 ? threadIdx.x / kWave : 0); row < c.rows;
+    const float each = 1.0f / (float)dim;
+    for (int64_t row = (int64_t)blockIdx.x * kRows + (WAVES == 1 ? wave_id() : 0); row < c.rows;
          row += (int64_t)gridDim.x * kRows) {
         float v[K * V], sum = 0.0f;
 #pragma unroll
         for (int k = 0; k < K; ++k)
-            load_some_of<V>(v + k * V, x + row * c.x_stride, (int64_t)(k * WAVES * kWave + lane) * V, n[k]);
+            load_row<V>(v + k * V, x + row * c.x_stride, (k * WAVES * kWave + lane) * V, dim, !TAIL || k < K - 1 ? 0 : WAVES * K == 1 ? kTiny : kTail);
 #pragma unroll
         for (int k = 0; k < K * V; ++k) sum = sum + v[k];
         const float mu = row_sum<WAVES>(sum, lds) * each;
@@ -128,14 +156,14 @@ __global__ void __launch_bounds__(WAVES == 1 ? 256 : WAVES * kWave)
 #pragma unroll
         for (int k = 0; k < K * V; ++k) {
             v[k] = v[k] - mu;
-            if (k % V < n[k / V]) squares = __builtin_fmaf(v[k], v[k], squares);
+            if (((k / V) * WAVES * kWave + lane) * V + (TAIL && k / V == K - 1 ? k % V : 0) < dim) squares = __builtin_fmaf(v[k], v[k], squares);
         }
         const float r = 1.0f / sqrtf(row_sum<WAVES>(squares, lds) * each + c.eps);
 #pragma unroll
         for (int k = 0; k < K * V; ++k) v[k] = __builtin_fmaf(v[k] * r, w[k], b[k]);
 #pragma unroll
         for (int k = 0; k < K; ++k)
-            store_some_of<V>(y + row * c.y_stride, (int64_t)(k * WAVES * kWave + lane) * V, v + k * V, n[k]);
+            store_row<V>(y + row * c.y_stride, (k * WAVES * kWave + lane) * V, v + k * V, dim, !TAIL || k < K - 1 ? 0 : WAVES * K == 1 ? kTiny : kTail);
         if (lane == 0) {
             if (mean) mean[row] = mu;
             if (rstd) rstd[row] = r;
@@ -144,40 +172,39 @@ __global__ void __launch_bounds__(WAVES == 1 ? 256 : WAVES * kWave)
 }
 
 // Rows too long to hold: a workgroup a row, read once for each sum and once more.
-template <class X, class Y>
+template <class X, class Y, bool TAIL>
 __global__ void __launch_bounds__(kLongBlock)
     norm_long_kernel(ea_layer_norm_t c, const X* x, const void* weight, const void* bias, Y* y, float* mean, float* rstd)
 {
-    constexpr int V = vec_of<X, Y>();
+    constexpr int V = vec_of<X, Y, TAIL>();
     __shared__ float2 lds[kLongBlock / kWave];
-    const float each = 1.0f / (float)c.dim;
+    const int dim = (int)c.dim;
+    const float each = 1.0f / (float)dim;
     for (int64_t row = blockIdx.x; row < c.rows; row += gridDim.x) {
         const X* from = x + row * c.x_stride;
         Y* to = y + row * c.y_stride;
         float v[V], sum = 0.0f, squares = 0.0f;
-        for (int64_t at = threadIdx.x * V; at < c.dim; at += kLongBlock * V) {
-            load_some_of<V>(v, from, at, inside<V>(at, c.dim));
+        for (int at = threadIdx.x * V; at < dim; at += kLongBlock * V) {
+            load_row<V>(v, from, at, dim, TAIL ? kTail : 0);
 #pragma unroll
             for (int k = 0; k < V; ++k) sum = sum + v[k];
         }
         const float mu = row_sum<kLongBlock / kWave>(sum, lds) * each;
-        for (int64_t at = threadIdx.x * V; at < c.dim; at += kLongBlock * V) {
-            const int n = inside<V>(at, c.dim);
-            load_some_of<V>(v, from, at, n);
+        for (int at = threadIdx.x * V; at < dim; at += kLongBlock * V) {
+            load_row<V>(v, from, at, dim, TAIL ? kTail : 0);
 #pragma unroll
             for (int k = 0; k < V; ++k)
-                if (k < n) squares = __builtin_fmaf(v[k] - mu, v[k] - mu, squares);
+                if (!TAIL || at + k < dim) squares = __builtin_fmaf(v[k] - mu, v[k] - mu, squares);
         }
         const float r = 1.0f / sqrtf(row_sum<kLongBlock / kWave>(squares, lds) * each + c.eps);
-        for (int64_t at = threadIdx.x * V; at < c.dim; at += kLongBlock * V) {
-            const int n = inside<V>(at, c.dim);
+        for (int at = threadIdx.x * V; at < dim; at += kLongBlock * V) {
             float w[V], b[V];
-            load_weights<V>(w, weight, c.w_type, at, n, 1.0f);
-            load_weights<V>(b, bias, c.w_type, at, n, 0.0f);
-            load_some_of<V>(v, from, at, n);
+            load_weights<V>(w, weight, c.w_type, at, dim, 1.0f, TAIL ? kTail : 0);
+            load_weights<V>(b, bias, c.w_type, at, dim, 0.0f, TAIL ? kTail : 0);
+            load_row<V>(v, from, at, dim, TAIL ? kTail : 0);
 #pragma unroll
             for (int k = 0; k < V; ++k) v[k] = __builtin_fmaf((v[k] - mu) * r, w[k], b[k]);
-            store_some_of<V>(to, at, v, n);
+            store_row<V>(to, at, v, dim, TAIL ? kTail : 0);
         }
         if (threadIdx.x == 0) {
             if (mean) mean[row] = mu;
@@ -188,34 +215,31 @@ __global__ void __launch_bounds__(kLongBlock)
 
 // ---- gradient ---------------------------------------------------------------------
 
-template <class X, class Y, int WAVES, int K>
-__global__ void __launch_bounds__(WAVES == 1 ? 256 : WAVES * kWave)
+template <class X, class Y, bool TAIL, int WAVES, int K>
+__global__ void __launch_bounds__(WAVES == 1 ? 256 : WAVES * kWave, 4)
     norm_grad_kernel(ea_layer_norm_t c, const X* x, const Y* dy, const void* weight, const float* mean,
                      const float* rstd, const X* add, X* dx, float* partial)
 {
-    constexpr int V = vec_of<X, Y>();
-    constexpr int kRows = WAVES == 1 ? 4 : 1;
+    constexpr int V = vec_of<X, Y, TAIL>(), kRows = WAVES == 1 ? 4 : 1;
     __shared__ float2 lds[WAVES];
-    const int lane = WAVES == 1 ? lane_id() : (int)threadIdx.x;
+    const int lane = WAVES == 1 ? lane_id() : (int)threadIdx.x, dim = (int)c.dim;
     float w[K * V], dw[K * V], db[K * V];
-    int n[K];
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-        const int64_t at = (int64_t)(k * WAVES * kWave + lane) * V;
-        n[k] = inside<V>(at, c.dim);
-        load_weights<V>(w + k * V, weight, c.w_type, at, n[k], 1.0f);
+        const int at = (k * WAVES * kWave + lane) * V;
+        load_weights<V>(w + k * V, weight, c.w_type, at, dim, 1.0f, !TAIL || k < K - 1 ? 0 : WAVES * K == 1 ? kTiny : kTail);
     }
 #pragma unroll
     for (int k = 0; k < K * V; ++k) dw[k] = db[k] = 0.0f;
-    const float each = 1.0f / (float)c.dim;
-    for (int64_t row = (int64_t)blockIdx.x * kRows + (WAVES == 1 ? threadIdx.x / kWave : 0); row < c.rows;
+    const float each = 1.0f / (float)dim;
+    for (int64_t row = (int64_t)blockIdx.x * kRows + (WAVES == 1 ? wave_id() : 0); row < c.rows;
          row += (int64_t)gridDim.x * kRows) {
         float v[K * V], d[K * V];
 #pragma unroll
         for (int k = 0; k < K; ++k) {
-            const int64_t at = (int64_t)(k * WAVES * kWave + lane) * V;
-            load_some_of<V>(v + k * V, x + row * c.x_stride, at, n[k]);
-            load_some_of<V>(d + k * V, dy + row * c.y_stride, at, n[k]);
+            const int at = (k * WAVES * kWave + lane) * V;
+            load_row<V>(v + k * V, x + row * c.x_stride, at, dim, !TAIL || k < K - 1 ? 0 : WAVES * K == 1 ? kTiny : kTail);
+            load_row<V>(d + k * V, dy + row * c.y_stride, at, dim, !TAIL || k < K - 1 ? 0 : WAVES * K == 1 ? kTiny : kTail);
         }
         const float mu = mean[row], r = rstd[row];
         float first = 0.0f, second = 0.0f;
@@ -233,23 +257,24 @@ __global__ void __launch_bounds__(WAVES == 1 ? 256 : WAVES * kWave)
         second = second * each;
 #pragma unroll
         for (int k = 0; k < K; ++k) {
-            const int64_t at = (int64_t)(k * WAVES * kWave + lane) * V;
+            const int at = (k * WAVES * kWave + lane) * V;
             float o[V];
-            if (add) load_some_of<V>(o, add + row * c.x_stride, at, n[k]);
+            if (add) load_row<V>(o, add + row * c.x_stride, at, dim, !TAIL || k < K - 1 ? 0 : WAVES * K == 1 ? kTiny : kTail);
 #pragma unroll
             for (int i = 0; i < V; ++i) {
                 const float g = (d[k * V + i] - first - v[k * V + i] * second) * r;
                 o[i] = add ? o[i] + g : g;
             }
-            store_some_of<V>(dx + row * c.x_stride, at, o, n[k]);
+            store_row<V>(dx + row * c.x_stride, at, o, dim, !TAIL || k < K - 1 ? 0 : WAVES * K == 1 ? kTiny : kTail);
         }
     }
     if (!partial) return;
     // A workgroup of one-wave rows joins its waves' sums, wave by wave.
-    float* mine = partial + (int64_t)blockIdx.x * 2 * c.dim;
+    const int64_t held = partial_row(c.dim);
+    float* mine = partial + (int64_t)blockIdx.x * 2 * held;
     if constexpr (WAVES == 1) {
         __shared__ float sums[4][2 * K * V][kWave];
-        const int wave = threadIdx.x / kWave;
+        const int wave = wave_id();
 #pragma unroll
         for (int k = 0; k < K * V; ++k) {
             sums[wave][k][lane] = dw[k];
@@ -268,30 +293,30 @@ __global__ void __launch_bounds__(WAVES == 1 ? 256 : WAVES * kWave)
     }
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-        const int64_t at = (int64_t)(k * WAVES * kWave + lane) * V;
-        store_some_of<V>(mine, at, dw + k * V, n[k]);
-        store_some_of<V>(mine + c.dim, at, db + k * V, n[k]);
+        const int at = (k * WAVES * kWave + lane) * V;
+        store_row<V>(mine, at, dw + k * V, dim, 0);
+        store_row<V>(mine + held, at, db + k * V, dim, 0);
     }
 }
 
-template <class X, class Y>
+template <class X, class Y, bool TAIL>
 __global__ void __launch_bounds__(kLongBlock)
     norm_grad_long_kernel(ea_layer_norm_t c, const X* x, const Y* dy, const void* weight, const float* mean,
                           const float* rstd, const X* add, X* dx)
 {
-    constexpr int V = vec_of<X, Y>();
+    constexpr int V = vec_of<X, Y, TAIL>();
     __shared__ float2 lds[kLongBlock / kWave];
-    const float each = 1.0f / (float)c.dim;
+    const int dim = (int)c.dim;
+    const float each = 1.0f / (float)dim;
     for (int64_t row = blockIdx.x; row < c.rows; row += gridDim.x) {
         const float mu = mean[row], r = rstd[row];
         const X* from = x + row * c.x_stride;
         const Y* grad = dy + row * c.y_stride;
         float v[V], d[V], w[V], first = 0.0f, second = 0.0f;
-        for (int64_t at = threadIdx.x * V; at < c.dim; at += kLongBlock * V) {
-            const int n = inside<V>(at, c.dim);
-            load_weights<V>(w, weight, c.w_type, at, n, 1.0f);
-            load_some_of<V>(v, from, at, n);
-            load_some_of<V>(d, grad, at, n);
+        for (int at = threadIdx.x * V; at < dim; at += kLongBlock * V) {
+            load_weights<V>(w, weight, c.w_type, at, dim, 1.0f, TAIL ? kTail : 0);
+            load_row<V>(v, from, at, dim, TAIL ? kTail : 0);
+            load_row<V>(d, grad, at, dim, TAIL ? kTail : 0);
 #pragma unroll
             for (int k = 0; k < V; ++k) {
                 first = first + d[k] * w[k];
@@ -301,19 +326,18 @@ __global__ void __launch_bounds__(kLongBlock)
         row_sums<kLongBlock / kWave>(first, second, lds);
         first = first * each;
         second = second * each;
-        for (int64_t at = threadIdx.x * V; at < c.dim; at += kLongBlock * V) {
-            const int n = inside<V>(at, c.dim);
+        for (int at = threadIdx.x * V; at < dim; at += kLongBlock * V) {
             float o[V];
-            load_weights<V>(w, weight, c.w_type, at, n, 1.0f);
-            load_some_of<V>(v, from, at, n);
-            load_some_of<V>(d, grad, at, n);
-            if (add) load_some_of<V>(o, add + row * c.x_stride, at, n);
+            load_weights<V>(w, weight, c.w_type, at, dim, 1.0f, TAIL ? kTail : 0);
+            load_row<V>(v, from, at, dim, TAIL ? kTail : 0);
+            load_row<V>(d, grad, at, dim, TAIL ? kTail : 0);
+            if (add) load_row<V>(o, add + row * c.x_stride, at, dim, TAIL ? kTail : 0);
 #pragma unroll
             for (int k = 0; k < V; ++k) {
                 const float g = (d[k] * w[k] - first - (v[k] - mu) * r * second) * r;
                 o[k] = add ? o[k] + g : g;
             }
-            store_some_of<V>(dx + row * c.x_stride, at, o, n);
+            store_row<V>(dx + row * c.x_stride, at, o, dim, TAIL ? kTail : 0);
         }
     }
 }
@@ -321,30 +345,30 @@ __global__ void __launch_bounds__(kLongBlock)
 // The weights' terms of long rows: a workgroup's columns over a run of rows.
 constexpr int kColumnBlock = 256;
 
-template <class X, class Y>
+template <class X, class Y, bool TAIL>
 __global__ void __launch_bounds__(kColumnBlock)
     norm_columns_kernel(ea_layer_norm_t c, const X* x, const Y* dy, const float* mean, const float* rstd, float* partial,
                         int64_t run)
 {
-    constexpr int V = vec_of<X, Y>();
-    const int64_t at = ((int64_t)blockIdx.x * kColumnBlock + threadIdx.x) * V;
-    const int n = inside<V>(at, c.dim);
-    if (n == 0) return;
+    constexpr int V = vec_of<X, Y, TAIL>();
+    const int at = (int)(blockIdx.x * kColumnBlock + threadIdx.x) * V, dim = (int)c.dim;
+    if (at >= dim) return;
     float dw[V] = {}, db[V] = {}, v[V], d[V];
     const int64_t end = (blockIdx.y + 1) * run < c.rows ? (blockIdx.y + 1) * run : c.rows;
     for (int64_t row = blockIdx.y * run; row < end; ++row) {
         const float mu = mean[row], r = rstd[row];
-        load_some_of<V>(v, x + row * c.x_stride, at, n);
-        load_some_of<V>(d, dy + row * c.y_stride, at, n);
+        load_row<V>(v, x + row * c.x_stride, at, dim, TAIL ? kTail : 0);
+        load_row<V>(d, dy + row * c.y_stride, at, dim, TAIL ? kTail : 0);
 #pragma unroll
         for (int k = 0; k < V; ++k) {
             db[k] = db[k] + d[k];
             dw[k] = __builtin_fmaf(d[k], (v[k] - mu) * r, dw[k]);
         }
     }
-    float* mine = partial + (int64_t)blockIdx.y * 2 * c.dim;
-    store_some_of<V>(mine, at, dw, n);
-    store_some_of<V>(mine + c.dim, at, db, n);
+    const int64_t held = partial_row(c.dim);
+    float* mine = partial + (int64_t)blockIdx.y * 2 * held;
+    store_row<V>(mine, at, dw, dim, 0);
+    store_row<V>(mine + held, at, db, dim, 0);
 }
 
 // The partial rows' sums: 16 columns of dweight and dbias, taken as one row, a workgroup.
@@ -358,9 +382,11 @@ __global__ void __launch_bounds__(kJoinColumns* kJoinRows)
     const int col = threadIdx.x % kJoinColumns, lane = threadIdx.x / kJoinColumns;
     const int64_t at = (int64_t)blockIdx.x * kJoinColumns + col;
     float sum = 0.0f;
+    const int64_t held = partial_row(dim), i = at < dim ? at : at - dim;
     if (at < 2 * dim) {
+        const float* from = partial + (at < dim ? 0 : held) + i;
 #pragma unroll 4
-        for (int64_t k = lane; k < parts; k += kJoinRows) sum = sum + partial[k * 2 * dim + at];
+        for (int64_t k = lane; k < parts; k += kJoinRows) sum = sum + from[k * 2 * held];
     }
     lds[lane][col] = sum;
     __syncthreads();
@@ -370,7 +396,6 @@ __global__ void __launch_bounds__(kJoinColumns* kJoinRows)
     }
     if (lane > 0 || at >= 2 * dim) return;
     void* to = at < dim ? dweight : dbias;
-    const int64_t i = at < dim ? at : at - dim;
     if (!to) return;
     sum = lds[0][col];
     set_element_at(to, type, i, accumulate ? element_at(to, type, i) + sum : sum);
@@ -378,44 +403,46 @@ __global__ void __launch_bounds__(kJoinColumns* kJoinRows)
 
 // ---- launches -----------------------------------------------------------------------
 
-// Waves of a row, and vectors of V elements a lane holds of it.
+// Waves of a row and vectors a lane holds of it (0 waves: the row is not held), the fewest that hold it, so that only a lane's
+// last vector may cross the row's end; whether one does.
 struct Shape {
     int waves, k;
+    bool tail;
 };
 
-Shape shape_of(int64_t dim, int v)
+Shape shape_of(const ea_layer_norm_t& c)
 {
+    const int whole = c.x_type != EA_F32 && c.y_type != EA_F32 ? 8 : 4;
+    const bool tail = c.dim % whole != 0;
+    const int v = tail ? 4 : whole;
     for (int waves = 1; waves <= 16; waves *= 4)
-        for (int k = 1; k <= kHeldColumns / v; ++k)
-            if (dim <= (int64_t)waves * kWave * k * v) return {waves, k};
-    return {0, 0};
+        for (int k = 1; k * v <= kHeldColumns; ++k)
+            if (c.dim <= (int64_t)waves * kWave * k * v) return {waves, k, tail};
+    return {0, 0, tail};
 }
 
-int vec_of_types(const ea_layer_norm_t& c)
-{
-    return c.x_type != EA_F32 && c.y_type != EA_F32 ? 8 : 4;
-}
-
-// f with the waves and vectors as constants.
+// f with the tail, the waves and the vectors a lane as constants.
 template <int V, class F>
 hipError_t with_shape(Shape s, F&& f)
 {
-#define EA_SHAPE(W, K) \
-    if (s.waves == W && s.k == K) return f(std::integral_constant<int, W>{}, std::integral_constant<int, K>{})
-    EA_SHAPE(1, 1);
-    EA_SHAPE(1, 2);
-    EA_SHAPE(4, 1);
-    EA_SHAPE(4, 2);
-    EA_SHAPE(16, 1);
-    EA_SHAPE(16, 2);
+#define EA_SHAPE(T, W, K)                           \
+    if (s.tail == T && s.waves == W && s.k == K)    \
+    return f(std::integral_constant<bool, T>{}, std::integral_constant<int, W>{}, std::integral_constant<int, K>{})
+#define EA_WAVES(T, K)   \
+    EA_SHAPE(T, 1, K);   \
+    EA_SHAPE(T, 4, K);   \
+    EA_SHAPE(T, 16, K)
+    EA_WAVES(false, 1);
+    EA_WAVES(false, 2);
     if constexpr (V == 4) {
-        EA_SHAPE(1, 3);
-        EA_SHAPE(1, 4);
-        EA_SHAPE(4, 3);
-        EA_SHAPE(4, 4);
-        EA_SHAPE(16, 3);
-        EA_SHAPE(16, 4);
+        EA_WAVES(false, 3);
+        EA_WAVES(false, 4);
     }
+    EA_WAVES(true, 1);
+    EA_WAVES(true, 2);
+    EA_WAVES(true, 3);
+    EA_WAVES(true, 4);
+#undef EA_WAVES
 #undef EA_SHAPE
     return hipErrorInvalidValue;
 }
@@ -446,28 +473,30 @@ int64_t runs_of(const ea_layer_norm_t& c)
 
 int64_t layer_norm_workspace_bytes(const ea_layer_norm_t& c)
 {
-    const Shape s = shape_of(c.dim, vec_of_types(c));
-    return (s.waves ? grad_groups_of(c, s) : runs_of(c)) * 2 * c.dim * 4;
+    const Shape s = shape_of(c);
+    return (s.waves ? grad_groups_of(c, s) : runs_of(c)) * 2 * partial_row(c.dim) * 4;
 }
 
 hipError_t launch_layer_norm(const ea_layer_norm_t& c, const void* x, const void* weight, const void* bias, void* y,
                              float* mean, float* rstd, hipStream_t s)
 {
     if (c.rows == 0) return hipSuccess;
+    const Shape shape = shape_of(c);
     return with_type(c.x_type, [&](auto xt) {
         return with_type(c.y_type, [&](auto yt) {
             using X = decltype(xt);
             using Y = decltype(yt);
-            const Shape shape = shape_of(c.dim, vec_of<X, Y>());
             if (!shape.waves) {
-                hipLaunchKernelGGL((norm_long_kernel<X, Y>), dim3((unsigned)at_most(c.rows, 1024)), dim3(kLongBlock), 0,
-                                   s, c, (const X*)x, weight, bias, (Y*)y, mean, rstd);
+                auto* kernel = shape.tail ? norm_long_kernel<X, Y, true> : norm_long_kernel<X, Y, false>;
+                hipLaunchKernelGGL(kernel, dim3((unsigned)at_most(c.rows, 1024)), dim3(kLongBlock), 0, s, c, (const X*)x,
+                                   weight, bias, (Y*)y, mean, rstd);
                 return hipGetLastError();
             }
             const unsigned groups = (unsigned)norm_groups_of(c, shape);
-            return with_shape<vec_of<X, Y>()>(shape, [&](auto w, auto k) {
+            return with_shape<vec_of<X, Y, false>()>(shape, [&](auto t, auto w, auto k) {
                 constexpr int W = decltype(w)::value, K = decltype(k)::value;
-                hipLaunchKernelGGL((norm_kernel<X, Y, W, K>), dim3(groups), dim3(W == 1 ? 256 : W * kWave), 0, s, c,
+                constexpr bool T = decltype(t)::value;
+                hipLaunchKernelGGL((norm_kernel<X, Y, T, W, K>), dim3(groups), dim3(W == 1 ? 256 : W * kWave), 0, s, c,
                                    (const X*)x, weight, bias, (Y*)y, mean, rstd);
                 return hipGetLastError();
             });
@@ -480,33 +509,31 @@ hipError_t launch_layer_norm_grad(const ea_layer_norm_t& c, const void* x, const
                                   void* dbias, bool accumulate, void* workspace, hipStream_t s)
 {
     float* partial = dweight || dbias ? (float*)workspace : nullptr;
-    int64_t parts = 0;
+    const Shape shape = shape_of(c);
+    const int64_t parts = c.rows == 0 ? 0 : shape.waves ? grad_groups_of(c, shape) : runs_of(c);
     hipError_t e = hipSuccess;
     if (c.rows > 0)
         e = with_type(c.x_type, [&](auto xt) {
             return with_type(c.y_type, [&](auto yt) {
                 using X = decltype(xt);
                 using Y = decltype(yt);
-                constexpr int V = vec_of<X, Y>();
-                const Shape shape = shape_of(c.dim, V);
-                if (!shape.waves) {
-                    parts = runs_of(c);
-                    const int64_t run = (c.rows + parts - 1) / parts;
-                    const unsigned strips = (unsigned)((c.dim + kColumnBlock * V - 1) / (kColumnBlock * V));
+                    if (!shape.waves) {
+                    const int64_t run = (c.rows + parts - 1) / parts, strip = kColumnBlock * (shape.tail ? 4 : vec_of<X, Y, false>());
+                    auto* columns = shape.tail ? norm_columns_kernel<X, Y, true> : norm_columns_kernel<X, Y, false>;
+                    auto* rows = shape.tail ? norm_grad_long_kernel<X, Y, true> : norm_grad_long_kernel<X, Y, false>;
                     // first: dx may take dy's place
                     if (partial)
-                        hipLaunchKernelGGL((norm_columns_kernel<X, Y>), dim3(strips, (unsigned)parts),
+                        hipLaunchKernelGGL(columns, dim3((unsigned)((c.dim + strip - 1) / strip), (unsigned)parts),
                                            dim3(kColumnBlock), 0, s, c, (const X*)x, (const Y*)dy, mean, rstd, partial,
                                            run);
-                    hipLaunchKernelGGL((norm_grad_long_kernel<X, Y>), dim3((unsigned)at_most(c.rows, 1024)),
-                                       dim3(kLongBlock), 0, s, c, (const X*)x, (const Y*)dy, weight, mean, rstd,
-                                       (const X*)add, (X*)dx);
+                    hipLaunchKernelGGL(rows, dim3((unsigned)at_most(c.rows, 1024)), dim3(kLongBlock), 0, s, c,
+                                       (const X*)x, (const Y*)dy, weight, mean, rstd, (const X*)add, (X*)dx);
                     return hipGetLastError();
                 }
-                parts = grad_groups_of(c, shape);
-                return with_shape<V>(shape, [&](auto w, auto k) {
+                return with_shape<vec_of<X, Y, false>()>(shape, [&](auto t, auto w, auto k) {
                     constexpr int W = decltype(w)::value, K = decltype(k)::value;
-                    hipLaunchKernelGGL((norm_grad_kernel<X, Y, W, K>), dim3((unsigned)parts),
+                constexpr bool T = decltype(t)::value;
+                    hipLaunchKernelGGL((norm_grad_kernel<X, Y, T, W, K>), dim3((unsigned)parts),
                                        dim3(W == 1 ? 256 : W * kWave), 0, s, c, (const X*)x, (const Y*)dy, weight, mean,
                                        rstd, (const X*)add, (X*)dx, partial);
                     return hipGetLastError();

@@ -20,7 +20,7 @@ namespace {
 constexpr float kLog2e = 0x1.715476p+0f;
 constexpr int kCountBlock = 1024;
 constexpr int64_t kMostCounts = 256;                   // workgroups that count
-constexpr int64_t kOwnCount = 8;                       // targets a thread, up to which every workgroup counts all itself
+constexpr int64_t kOwnCount = 16;                      // targets a thread, up to which every workgroup counts all itself
 constexpr int64_t kMostWaves = 4096;                   // of the main pass, 16 a CU: each row's group of them leaves one sum
 constexpr int kEndBlock = 256;
 
