@@ -43,16 +43,16 @@ __all__ = list(_EXPORTS + _TRAIN_EXPORTS + _LAYER_EXPORTS)
 
 def __getattr__(name):
     if name in _EXPORTS:
-        from . import _binding
-        return getattr(_binding, name)
-    if name in _TRAIN_EXPORTS:
-        from . import _train
-        return getattr(_train, name)
-    if name in _LAYER_EXPORTS:
-        from . import _layer
-        return getattr(_layer, name)
-    raise AttributeError(f"module {__name__!r} has no attribute {name!r}")
+        from . import _binding as module
+    elif name in _TRAIN_EXPORTS:
+        from . import _train as module
+    elif name in _LAYER_EXPORTS:
+        from . import _layer as module
+    else:
+        raise AttributeError(f"module {__name__!r} has no attribute {name!r}")
+    value = globals()[name] = getattr(module, name)     # found at once from now on: small calls take a few microseconds
+    return value
 
 
 def __dir__():
-    return sorted(list(globals()) + list(_EXPORTS + _TRAIN_EXPORTS + _LAYER_EXPORTS))
+    return sorted(set(globals()) | set(_EXPORTS + _TRAIN_EXPORTS + _LAYER_EXPORTS))

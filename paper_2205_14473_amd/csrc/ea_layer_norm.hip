@@ -27,6 +27,9 @@ constexpr int vec_of()
     return !TAIL && sizeof(X) == 2 && sizeof(Y) == 2 ? 8 : 4;
 }
 
+template <class X, class Y, bool TAIL>
+constexpr int kVec = vec_of<X, Y, TAIL>();
+
 // A vector moved down by some of its elements, zeros behind.
 template <int V, class T>
 __device__ __forceinline__ Vec<T, V> moved_down(Vec<T, V> v, int by)
@@ -45,9 +48,31 @@ __device__ __forceinline__ Vec<T, V> moved_down(Vec<T, V> v, int by)
 
 constexpr int kTail = 1, kTiny = 2;
 
-// The row's vector at column `at`, zeros behind its end.  tail: it may cross the end; it is then the row's last whole one,
-// moved down, so that a vector is one load and nothing outside the row is read (kTiny: the row may be shorter than one).  (Elements one by one for rows of no whole
-// number of vectors: 65,536 x 1,001 bfloat16 135 us, its gradient 378; FIGURES this way.)
+// The tail of a lane's vector k of K.
+template <bool TAIL, int WAVES, int K>
+__device__ __forceinline__ constexpr int tail_of(int k)
+{
+    return !TAIL || k < K - 1 ? 0 : WAVES * K == 1 ? kTiny : kTail;
+}
+
+// The row's vector at column `at`, zeros behind its end.  tail: it may cross the end; it is then the row's last whole
+// one, moved down, so that a vector is one load and nothing outside the row is read (kTiny: the row may be shorter than
+// one).  (Elements one by one for rows of no whole number of vectors: 65,536 x 1,001 bfloat16 135 us and 378 the
+// gradient, this way 47 and 106.)
+template <int V, class T>
+__device__ __forceinline__ Vec<T, V> row_vec(const T* row, int at, int dim, int tail)
+{
+    Vec<T, V> v = {};
+    if (tail == kTiny && dim < V) {
+        v = load_part<V>(row + at, dim - at);
+    } else if (at < dim) {
+        const int from = !tail || at < dim - V ? at : dim - V;
+        v = *(const typename VecOf<T, V>::unaligned*)((const char*)row + (uint32_t)from * (uint32_t)sizeof(T));
+        if (tail) v = moved_down<V, T>(v, at - from);
+    }
+    return v;
+}
+
 template <int V, class T>
 __device__ __forceinline__ void load_row(float* x, const T* row, int at, int dim, int tail)
 {
@@ -55,15 +80,7 @@ __device__ __forceinline__ void load_row(float* x, const T* row, int at, int dim
         load_row<V / 2>(x, row, at, dim, tail);
         load_row<V / 2>(x + V / 2, row, at + V / 2, dim, tail);
     } else {
-        Vec<T, V> v = {};
-        if (tail == kTiny && dim < V) {
-            v = load_part<V>(row + at, dim - at);
-        } else if (at < dim) {
-            const int from = !tail || at < dim - V ? at : dim - V;
-            v = *(const typename VecOf<T, V>::unaligned*)((const char*)row + (uint32_t)from * (uint32_t)sizeof(T));
-            if (tail) v = moved_down<V, T>(v, at - from);
-        }
-        widen_to<V, T>(x, v);
+        widen_to<V, T>(x, row_vec<V>(row, at, dim, tail));
     }
 }
 
@@ -79,7 +96,8 @@ __device__ __forceinline__ void store_row(T* row, int at, const float* x, int di
 
 // weight or bias, or what stands for it where there is none
 template <int V>
-__device__ __forceinline__ void load_weights(float* x, const void* w, int32_t type, int at, int dim, float none, int tail)
+__device__ __forceinline__ void load_weights(float* x, const void* w, int32_t type, int at, int dim, float none,
+                                             int tail)
 {
 #pragma unroll
     for (int k = 0; k < V; ++k) x[k] = none;
@@ -92,7 +110,8 @@ __device__ __forceinline__ void load_weights(float* x, const void* w, int32_t ty
         load_row<V>(x, (const f16*)w, at, dim, tail);
 }
 
-// Floats of a partial row of dweight, and of dbias behind it: whole vectors, what lies behind the columns is not looked at.
+// Floats of a partial row of dweight, and of dbias behind it: whole vectors, what lies behind the columns is not looked
+// at.
 __host__ __device__ constexpr int64_t partial_row(int64_t dim)
 {
     return (dim + 7) / 8 * 8;
@@ -139,8 +158,8 @@ __global__ void __launch_bounds__(WAVES == 1 ? 256 : WAVES * kWave)
 #pragma unroll
     for (int k = 0; k < K; ++k) {
         const int at = (k * WAVES * kWave + lane) * V;
-        load_weights<V>(w + k * V, weight, c.w_type, at, dim, 1.0f, !TAIL || k < K - 1 ? 0 : WAVES * K == 1 ? kTiny : kTail);
-        load_weights<V>(b + k * V, bias, c.w_type, at, dim, 0.0f, !TAIL || k < K - 1 ? 0 : WAVES * K == 1 ? kTiny : kTail);
+        load_weights<V>(w + k * V, weight, c.w_type, at, dim, 1.0f, tail_of<TAIL, WAVES, K>(k));
+        load_weights<V>(b + k * V, bias, c.w_type, at, dim, 0.0f, tail_of<TAIL, WAVES, K>(k));
     }
     const float each = 1.0f / (float)dim;
     for (int64_t row = (int64_t)blockIdx.x * kRows + (WAVES == 1 ? wave_id() : 0); row < c.rows;
@@ -148,7 +167,8 @@ __global__ void __launch_bounds__(WAVES == 1 ? 256 : WAVES * kWave)
         float v[K * V], sum = 0.0f;
 #pragma unroll
         for (int k = 0; k < K; ++k)
-            load_row<V>(v + k * V, x + row * c.x_stride, (k * WAVES * kWave + lane) * V, dim, !TAIL || k < K - 1 ? 0 : WAVES * K == 1 ? kTiny : kTail);
+            load_row<V>(v + k * V, x + row * c.x_stride, (k * WAVES * kWave + lane) * V, dim,
+                        tail_of<TAIL, WAVES, K>(k));
 #pragma unroll
         for (int k = 0; k < K * V; ++k) sum = sum + v[k];
         const float mu = row_sum<WAVES>(sum, lds) * each;
@@ -156,14 +176,16 @@ __global__ void __launch_bounds__(WAVES == 1 ? 256 : WAVES * kWave)
 #pragma unroll
         for (int k = 0; k < K * V; ++k) {
             v[k] = v[k] - mu;
-            if (((k / V) * WAVES * kWave + lane) * V + (TAIL && k / V == K - 1 ? k % V : 0) < dim) squares = __builtin_fmaf(v[k], v[k], squares);
+            if (((k / V) * WAVES * kWave + lane) * V + (TAIL && k / V == K - 1 ? k % V : 0) < dim)
+                squares = __builtin_fmaf(v[k], v[k], squares);
         }
         const float r = 1.0f / sqrtf(row_sum<WAVES>(squares, lds) * each + c.eps);
 #pragma unroll
         for (int k = 0; k < K * V; ++k) v[k] = __builtin_fmaf(v[k] * r, w[k], b[k]);
 #pragma unroll
         for (int k = 0; k < K; ++k)
-            store_row<V>(y + row * c.y_stride, (k * WAVES * kWave + lane) * V, v + k * V, dim, !TAIL || k < K - 1 ? 0 : WAVES * K == 1 ? kTiny : kTail);
+            store_row<V>(y + row * c.y_stride, (k * WAVES * kWave + lane) * V, v + k * V, dim,
+                         tail_of<TAIL, WAVES, K>(k));
         if (lane == 0) {
             if (mean) mean[row] = mu;
             if (rstd) rstd[row] = r;
@@ -174,7 +196,8 @@ __global__ void __launch_bounds__(WAVES == 1 ? 256 : WAVES * kWave)
 // Rows too long to hold: a workgroup a row, read once for each sum and once more.
 template <class X, class Y, bool TAIL>
 __global__ void __launch_bounds__(kLongBlock)
-    norm_long_kernel(ea_layer_norm_t c, const X* x, const void* weight, const void* bias, Y* y, float* mean, float* rstd)
+    norm_long_kernel(ea_layer_norm_t c, const X* x, const void* weight, const void* bias, Y* y, float* mean,
+                     float* rstd)
 {
     constexpr int V = vec_of<X, Y, TAIL>();
     __shared__ float2 lds[kLongBlock / kWave];
@@ -215,40 +238,86 @@ __global__ void __launch_bounds__(kLongBlock)
 
 // ---- gradient ---------------------------------------------------------------------
 
+// Whether the next row's vectors are asked for before this row's sums are formed.  The registers for them pay where a
+// lane holds few columns (131,072 x 256 bfloat16 65 us without, 55 with) and for rows with a tail, whose loads are more
+// and smaller (65,536 x 1,001 119 without, 106 with); not for 16 whole columns a lane (32,768 x 1,024 float32 104
+// without, 112 with; 65,536 x 1,024 bfloat16 107 either way), nor for 16 waves, which have 128 registers each (4,096 x
+// 16,384 149 without, 196 with).
+constexpr bool grad_ahead(int waves, int columns, bool tail)
+{
+    return waves <= 4 && (columns <= 8 || tail);
+}
+
+// Waves of a SIMD that the gradient's registers leave room for (four and spills for 1,001 columns: 230 us).
+constexpr int grad_waves(int waves, int columns, bool tail)
+{
+    return grad_ahead(waves, columns, tail) && columns > 8 ? 3 : 4;
+}
+
 template <class X, class Y, bool TAIL, int WAVES, int K>
-__global__ void __launch_bounds__(WAVES == 1 ? 256 : WAVES * kWave, 4)
+__global__ void __launch_bounds__(WAVES == 1 ? 256 : WAVES * kWave, (grad_waves(WAVES, K * kVec<X, Y, TAIL>, TAIL)))
     norm_grad_kernel(ea_layer_norm_t c, const X* x, const Y* dy, const void* weight, const float* mean,
                      const float* rstd, const X* add, X* dx, float* partial)
 {
     constexpr int V = vec_of<X, Y, TAIL>(), kRows = WAVES == 1 ? 4 : 1;
+    // The weights wait in LDS then.
+    constexpr bool kAhead = grad_ahead(WAVES, K * V, TAIL);
     __shared__ float2 lds[WAVES];
+    __shared__ float weights[kAhead ? WAVES * kWave * K * V : 1];
     const int lane = WAVES == 1 ? lane_id() : (int)threadIdx.x, dim = (int)c.dim;
-    float w[K * V], dw[K * V], db[K * V];
+    const int64_t step = (int64_t)gridDim.x * kRows;
+    int64_t row = (int64_t)blockIdx.x * kRows + (WAVES == 1 ? wave_id() : 0);
+    Vec<X, V> xr[K];
+    Vec<Y, V> yr[K];
+    auto load = [&](int64_t from) {
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            const int at = (k * WAVES * kWave + lane) * V, tail = tail_of<TAIL, WAVES, K>(k);
+            xr[k] = row_vec<V>(x + from * c.x_stride, at, dim, tail);
+            yr[k] = row_vec<V>(dy + from * c.y_stride, at, dim, tail);
+        }
+    };
+    if (kAhead) load(row < c.rows ? row : 0);
+    float w[kAhead ? 1 : K * V], dw[K * V], db[K * V];
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-        const int at = (k * WAVES * kWave + lane) * V;
-        load_weights<V>(w + k * V, weight, c.w_type, at, dim, 1.0f, !TAIL || k < K - 1 ? 0 : WAVES * K == 1 ? kTiny : kTail);
+        const int at = (k * WAVES * kWave + lane) * V, tail = tail_of<TAIL, WAVES, K>(k);
+        if constexpr (kAhead) {
+            float some[V];
+            load_weights<V>(some, weight, c.w_type, at, dim, 1.0f, tail);
+            if (WAVES > 1 || wave_id() == 0) {
+#pragma unroll
+                for (int i = 0; i < V; ++i) weights[at + i] = some[i];
+            }
+        } else {
+            load_weights<V>(w + k * V, weight, c.w_type, at, dim, 1.0f, tail);
+        }
     }
+    if (kAhead) __syncthreads();
 #pragma unroll
     for (int k = 0; k < K * V; ++k) dw[k] = db[k] = 0.0f;
     const float each = 1.0f / (float)dim;
-    for (int64_t row = (int64_t)blockIdx.x * kRows + (WAVES == 1 ? wave_id() : 0); row < c.rows;
-         row += (int64_t)gridDim.x * kRows) {
+    for (; row < c.rows; row += step) {
+        if (!kAhead) load(row);
+        const float mu = mean[row], r = rstd[row];
         float v[K * V], d[K * V];
+        Vec<X, V> ar[K];
 #pragma unroll
         for (int k = 0; k < K; ++k) {
-            const int at = (k * WAVES * kWave + lane) * V;
-            load_row<V>(v + k * V, x + row * c.x_stride, at, dim, !TAIL || k < K - 1 ? 0 : WAVES * K == 1 ? kTiny : kTail);
-            load_row<V>(d + k * V, dy + row * c.y_stride, at, dim, !TAIL || k < K - 1 ? 0 : WAVES * K == 1 ? kTiny : kTail);
+            const int at = (k * WAVES * kWave + lane) * V, tail = tail_of<TAIL, WAVES, K>(k);
+            widen_to<V, X>(v + k * V, xr[k]);
+            widen_to<V, Y>(d + k * V, yr[k]);
+            if (kAhead && add) ar[k] = row_vec<V>(add + row * c.x_stride, at, dim, tail);
         }
-        const float mu = mean[row], r = rstd[row];
+        // (the last row's turn asks for that row again)
+        if (kAhead) load(row + step < c.rows ? row + step : row);
         float first = 0.0f, second = 0.0f;
 #pragma unroll
         for (int k = 0; k < K * V; ++k) {
             v[k] = (v[k] - mu) * r;
             db[k] = db[k] + d[k];
             dw[k] = __builtin_fmaf(d[k], v[k], dw[k]);
-            d[k] = d[k] * w[k];
+            d[k] = d[k] * (kAhead ? weights[(k / V * WAVES * kWave + lane) * V + k % V] : w[kAhead ? 0 : k]);
             first = first + d[k];
             second = __builtin_fmaf(d[k], v[k], second);
         }
@@ -257,15 +326,15 @@ __global__ void __launch_bounds__(WAVES == 1 ? 256 : WAVES * kWave, 4)
         second = second * each;
 #pragma unroll
         for (int k = 0; k < K; ++k) {
-            const int at = (k * WAVES * kWave + lane) * V;
+            const int at = (k * WAVES * kWave + lane) * V, tail = tail_of<TAIL, WAVES, K>(k);
             float o[V];
-            if (add) load_row<V>(o, add + row * c.x_stride, at, dim, !TAIL || k < K - 1 ? 0 : WAVES * K == 1 ? kTiny : kTail);
+            if (add) widen_to<V, X>(o, kAhead ? ar[k] : row_vec<V>(add + row * c.x_stride, at, dim, tail));
 #pragma unroll
             for (int i = 0; i < V; ++i) {
                 const float g = (d[k * V + i] - first - v[k * V + i] * second) * r;
                 o[i] = add ? o[i] + g : g;
             }
-            store_row<V>(dx + row * c.x_stride, at, o, dim, !TAIL || k < K - 1 ? 0 : WAVES * K == 1 ? kTiny : kTail);
+            store_row<V>(dx + row * c.x_stride, at, o, dim, tail);
         }
     }
     if (!partial) return;
@@ -347,8 +416,8 @@ constexpr int kColumnBlock = 256;
 
 template <class X, class Y, bool TAIL>
 __global__ void __launch_bounds__(kColumnBlock)
-    norm_columns_kernel(ea_layer_norm_t c, const X* x, const Y* dy, const float* mean, const float* rstd, float* partial,
-                        int64_t run)
+    norm_columns_kernel(ea_layer_norm_t c, const X* x, const Y* dy, const float* mean, const float* rstd,
+                        float* partial, int64_t run)
 {
     constexpr int V = vec_of<X, Y, TAIL>();
     const int at = (int)(blockIdx.x * kColumnBlock + threadIdx.x) * V, dim = (int)c.dim;
@@ -403,8 +472,8 @@ __global__ void __launch_bounds__(kJoinColumns* kJoinRows)
 
 // ---- launches -----------------------------------------------------------------------
 
-// Waves of a row and vectors a lane holds of it (0 waves: the row is not held), the fewest that hold it, so that only a lane's
-// last vector may cross the row's end; whether one does.
+// Waves of a row and vectors a lane holds of it (0 waves: the row is not held), the fewest that hold it, so that only a
+// lane's last vector may cross the row's end; whether one does.
 struct Shape {
     int waves, k;
     bool tail;
@@ -460,7 +529,9 @@ int64_t norm_groups_of(const ea_layer_norm_t& c, Shape s)
 
 int64_t grad_groups_of(const ea_layer_norm_t& c, Shape s)
 {
-    return s.waves == 1 ? at_most((c.rows + 3) / 4, 1024) : at_most(c.rows, s.waves == 4 ? 1024 : 256);
+    const int columns = s.k * (s.tail || c.x_type == EA_F32 || c.y_type == EA_F32 ? 4 : 8);
+    const int64_t held = s.waves == 16 ? 256 : 256 * grad_waves(s.waves, columns, s.tail);
+    return at_most(s.waves == 1 ? (c.rows + 3) / 4 : c.rows, held);
 }
 
 // Runs of rows of long rows' column sums.
@@ -488,8 +559,8 @@ hipError_t launch_layer_norm(const ea_layer_norm_t& c, const void* x, const void
             using Y = decltype(yt);
             if (!shape.waves) {
                 auto* kernel = shape.tail ? norm_long_kernel<X, Y, true> : norm_long_kernel<X, Y, false>;
-                hipLaunchKernelGGL(kernel, dim3((unsigned)at_most(c.rows, 1024)), dim3(kLongBlock), 0, s, c, (const X*)x,
-                                   weight, bias, (Y*)y, mean, rstd);
+                hipLaunchKernelGGL(kernel, dim3((unsigned)at_most(c.rows, 1024)), dim3(kLongBlock), 0, s, c,
+                                   (const X*)x, weight, bias, (Y*)y, mean, rstd);
                 return hipGetLastError();
             }
             const unsigned groups = (unsigned)norm_groups_of(c, shape);
@@ -517,8 +588,9 @@ hipError_t launch_layer_norm_grad(const ea_layer_norm_t& c, const void* x, const
             return with_type(c.y_type, [&](auto yt) {
                 using X = decltype(xt);
                 using Y = decltype(yt);
-                    if (!shape.waves) {
-                    const int64_t run = (c.rows + parts - 1) / parts, strip = kColumnBlock * (shape.tail ? 4 : vec_of<X, Y, false>());
+                if (!shape.waves) {
+                    const int64_t run = (c.rows + parts - 1) / parts;
+                    const int64_t strip = kColumnBlock * (shape.tail ? 4 : vec_of<X, Y, false>());
                     auto* columns = shape.tail ? norm_columns_kernel<X, Y, true> : norm_columns_kernel<X, Y, false>;
                     auto* rows = shape.tail ? norm_grad_long_kernel<X, Y, true> : norm_grad_long_kernel<X, Y, false>;
                     // first: dx may take dy's place
@@ -532,7 +604,7 @@ hipError_t launch_layer_norm_grad(const ea_layer_norm_t& c, const void* x, const
                 }
                 return with_shape<vec_of<X, Y, false>()>(shape, [&](auto t, auto w, auto k) {
                     constexpr int W = decltype(w)::value, K = decltype(k)::value;
-                constexpr bool T = decltype(t)::value;
+                    constexpr bool T = decltype(t)::value;
                     hipLaunchKernelGGL((norm_grad_kernel<X, Y, T, W, K>), dim3((unsigned)parts),
                                        dim3(W == 1 ? 256 : W * kWave), 0, s, c, (const X*)x, (const Y*)dy, weight, mean,
                                        rstd, (const X*)add, (X*)dx, partial);

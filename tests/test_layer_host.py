@@ -166,6 +166,9 @@ def test_arguments_are_refused(E):
     long = rec_config(E, batch=1, length=5000)
     assert ops["rec"].call(long, workspace=None) == ARG and ops["rec_grad"].call(long, workspace=P + 8) == ALIGN
     assert ops["rec"].call(rec_config(E, batch=1 << 16, length=1 << 15)) == UNSUPPORTED
+    wide = dict(dim=1 << 20, x_stride=1 << 20, g_stride=1 << 20, y_stride=1 << 20)
+    large = rec_config(E, batch=1 << 10, length=1 << 20, **wide)
+    assert ops["rec"].call(large) == UNSUPPORTED and ops["rec_grad"].call(large) == UNSUPPORTED
     # one array in two roles needs one type and stride
     for name, out, kw in (("norm", "y", dict(y_type=E.EA_BF16)), ("norm", "y", dict(y_stride=8)),
                           ("drop", "y", dict(y_type=E.EA_BF16)), ("drop", "y", dict(x_stride=8)),
@@ -191,11 +194,14 @@ def test_nothing_to_do_needs_no_arrays(E):
 def test_sizes(E):
     for rows, dim in ((1, 1), (10, 768), (10 ** 6, 4096), (2 ** 31 - 1, 2 ** 20)):
         n = E.ea_layer_norm_workspace_bytes(norm_config(E, rows=rows, dim=dim, x_stride=dim, y_stride=dim))
-        assert 0 < n <= 8 * dim * min(rows, 4096)
-    for b, n, dim in ((1, 1, 1), (3, 64, 5), (3, 65, 5), (1, 65_536, 1024), (2 ** 10, 2 ** 20, 2 ** 20)):
+        assert 0 < n <= 8 * -(-dim // 8) * 8 * min(rows, 4096)
+    for b, n, dim in ((1, 1, 1), (3, 64, 5), (3, 65, 5), (1, 65_536, 1024), (2 ** 10, 2 ** 10, 2 ** 20)):
         c = rec_config(E, batch=b, length=n, dim=dim, x_stride=dim, g_stride=dim, y_stride=dim)
         assert E.ea_recurrence_states_bytes(c) == 4 * b * -(-n // 64) * dim
-        assert 0 <= E.ea_recurrence_workspace_bytes(c) <= 4 * b * dim * (2 * 1100 + 1)
+        # a product and an end value for every 128 steps and every group of 16 such, of 8 bytes each, and a state for
+        # every stretch of groups
+        chunks = -(-n // 128)
+        assert 0 <= E.ea_recurrence_workspace_bytes(c) <= 8 * (16 + b * dim * (2 * chunks + 2 * -(-chunks // 16) + chunks))
     for rows, vocab in ((1, 1), (2048, 32_000), (2 ** 31 - 1, 2 ** 24)):
         n = E.ea_token_loss_workspace_bytes(loss_config(E, rows=rows, vocab=vocab, logits_stride=vocab, dlogits_stride=vocab))
         assert 0 < n <= 16 * (9000 + 256)
