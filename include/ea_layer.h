@@ -17,7 +17,8 @@
  * nearest even once, at the end.
  *
  * Rows: `x_stride` and its like are the elements from one row to the next, at
- * least the row's width; elements between rows are neither read nor written.
+ * least the row's width; elements between rows are not written, and what they
+ * hold has no effect.
  * Arrays that a call writes do not overlap any other array of the call, but
  * where it says so.  A workspace's contents do not matter; calls that share one
  * are ordered by the caller.
@@ -55,8 +56,9 @@ typedef struct ea_layer_norm {
  *   y (device, rows, write; may be x when types and strides are the same),
  *   mean, rstd (device, rows floats each, write; may be NULL, but the gradient
  *   needs them).
- * A row that holds an infinity or NaN gives NaN, in that row only; one whose
- * squares overflow binary32 has rstd = 0 and y = bias. */
+ * A row that holds an infinity or NaN, or whose sum overflows binary32, gives
+ * NaN, in that row only; one whose squares alone overflow has rstd = 0 and
+ * y = bias. */
 int ea_layer_norm(const ea_layer_norm_t *c, const void *x, const void *weight, const void *bias, void *y, float *mean,
                   float *rstd, void *stream);
 
@@ -141,7 +143,8 @@ typedef struct ea_recurrence {
 /* Bytes of the saved states: batch * ceil(length / 64) * dim floats. */
 int64_t ea_recurrence_states_bytes(const ea_recurrence_t *c);
 
-/* Device workspace (bytes) of ea_recurrence and of ea_recurrence_grad. */
+/* Device workspace (bytes) of ea_recurrence and of ea_recurrence_grad: 0 up to
+ * 128 steps. */
 int64_t ea_recurrence_workspace_bytes(const ea_recurrence_t *c);
 
 /* For every sequence and channel, h in binary32:
@@ -151,6 +154,9 @@ int64_t ea_recurrence_workspace_bytes(const ea_recurrence_t *c);
  * Sequences are cut into pieces whose gates are multiplied: with plain gates
  * a product over some of the steps that leaves binary32's range gives
  * infinities or NaN, or 0, even where the steps one by one would not.
+ * Pieces hand their states on through the workspace, within one launch, and wait
+ * for each other: calls that may run at the same time need a workspace each.  (A
+ * state that does not come for a good part of a second is taken as NaN.)
  *   g, x (device, batch * length rows), h0 (device, batch * dim floats, or NULL:
  *   zeros), lengths (device, batch int32, or NULL), y (device, batch * length
  *   rows, write), states (device, batch * ceil(length / 64) * dim floats, write;
@@ -207,7 +213,9 @@ int64_t ea_token_loss_workspace_bytes(const ea_token_loss_t *c);
  *                   (a row of zeros where it does not count)
  * Logits of -infinity have probability 0.  A row that counts and holds NaN or
  * +infinity, or nothing but -infinity, gives NaN in its loss and its whole
- * gradient; rows that do not count are not read.
+ * gradient; what a row holds that does not count has no effect.  Logits are read
+ * in whole aligned 16 bytes, so that up to 15 bytes on either side of a row may be
+ * read too, with no effect.
  *   logits (device, rows), targets (device, rows), loss (device, rows floats,
  *   write, or NULL), total (device, one float, write), count (device, one int32,
  *   write, or NULL), dlogits (device, rows, write, or NULL; may be logits when

@@ -71,8 +71,8 @@ __device__ __forceinline__ void set_element(Vec<T, N>& v, int k, T x)
         v[k] = x;
 }
 
-// The first `n` elements; the rest read as `rest`, and are not written.  All loads are made at once, the rest's from the first
-// element: a branch around each would make a row wait N times for memory.
+// The first `n` elements; the rest read as `rest`, and are not written.  All loads are made at once, the rest's from the
+// first element: a branch around each would make a row wait N times for memory.
 template <int N, class T>
 __device__ __forceinline__ Vec<T, N> load_part(const T* p, int n, float rest = 0.0f)
 {

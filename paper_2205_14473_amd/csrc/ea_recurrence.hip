@@ -95,7 +95,8 @@ constexpr int64_t kMostGroupsOf(bool chain)
 __global__ void __launch_bounds__(kClearBlock) clear_kernel(uint64_t* words, int64_t count)
 {
     typedef uint64_t Pair __attribute__((ext_vector_type(2)));
-    for (int64_t i = (int64_t)blockIdx.x * kClearBlock + threadIdx.x; i * 2 < count; i += (int64_t)gridDim.x * kClearBlock)
+    for (int64_t i = (int64_t)blockIdx.x * kClearBlock + threadIdx.x; i * 2 < count;
+         i += (int64_t)gridDim.x * kClearBlock)
         ((Pair*)words)[i] = Pair{0, 0};
 }
 
@@ -121,8 +122,8 @@ int64_t words_of(const ea_recurrence_t& c, const Plan& p)
     return (kCounterWords + (2 * pairs + stretches) * c.batch * c.dim + 1) / 2 * 2;
 }
 
-hipError_t begin(Call& a, const ea_recurrence_t& c, int steps, const int32_t* lengths, void* workspace, unsigned* groups,
-                 hipStream_t s)
+hipError_t begin(Call& a, const ea_recurrence_t& c, int steps, const int32_t* lengths, void* workspace,
+                 unsigned* groups, hipStream_t s)
 {
     a.c = c;
     a.p = plan_of(c, steps);
@@ -138,7 +139,8 @@ hipError_t begin(Call& a, const ea_recurrence_t& c, int steps, const int32_t* le
     *groups = (unsigned)(items < kMostGroupsOf(a.p.chunks > 1) ? items : kMostGroupsOf(a.p.chunks > 1));
     if (a.p.chunks == 1) return hipSuccess;
     const int64_t count = words_of(c, a.p), clear = (count / 2 + kClearBlock - 1) / kClearBlock;
-    hipLaunchKernelGGL(clear_kernel, dim3((unsigned)(clear < 2048 ? clear : 2048)), dim3(kClearBlock), 0, s, a.words, count);
+    hipLaunchKernelGGL(clear_kernel, dim3((unsigned)(clear < 2048 ? clear : 2048)), dim3(kClearBlock), 0, s, a.words,
+                       count);
     return hipGetLastError();
 }
 

@@ -16,8 +16,8 @@ namespace {
 // (product of their gates) e + (what they give from e = 0).
 template <class X, class G, bool SIGMOID, bool CHAIN>
 __global__ void __launch_bounds__(kMostWaves* kWave, 8)
-    recurrence_grad_kernel(Call a, const G* g, const X* x, const float* states, const X* dy, const float* dh_last, G* dg,
-                           X* dx, float* dh0)
+    recurrence_grad_kernel(Call a, const G* g, const X* x, const float* states, const X* dy, const float* dh_last,
+                           G* dg, X* dx, float* dh0)
 {
     constexpr int K = kBackwardSteps, kBlockWaves = EA_RECURRENCE_BLOCK / K;
     __shared__ Exchange lds;
