@@ -25,11 +25,11 @@ LIB = os.path.join(PKG, "libea.so")
 SOURCES = [os.path.join(CSRC, f) for f in ("ea_kernels.hip", "ea_half_c1.hip", "ea_half_c2.hip", "ea_half_c4.hip",
                                             "ea_half_c8.hip", "ea_half_wide_c12.hip", "ea_half_wide_c48.hip",
                                             "ea_sym_c4.hip", "ea_sym_c8.hip", "ea_toy.hip", "ea_adamw.hip", "ea_embed.hip",
-                                            "ea_layer_norm.hip", "ea_dropout.hip", "ea_recurrence.hip",
-                                            "ea_recurrence_grad.hip", "ea_token_loss.hip",
+                                            "ea_layer_norm.hip", "ea_layer_norm_grad.hip", "ea_dropout.hip",
+                                            "ea_recurrence.hip", "ea_recurrence_grad.hip", "ea_token_loss.hip",
                                             "ea_api.cpp", "ea_train_api.cpp", "ea_layer_api.cpp")]
 HEADERS = [os.path.join(CSRC, f) for f in ("ea_device.hpp", "ea_launch.hpp", "ea_round.hpp", "ea_train.hpp", "ea_check.hpp",
-                                            "ea_layer.hpp", "ea_recurrence.hpp")] + \
+                                            "ea_layer.hpp", "ea_layer_norm.hpp", "ea_recurrence.hpp")] + \
     [os.path.join(ROOT, "include", f) for f in ("ea.h", "ea_train.h", "ea_layer.h")]
 ARCH = "gfx950"
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")

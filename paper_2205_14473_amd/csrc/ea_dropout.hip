@@ -6,7 +6,7 @@
 // alone, so strides, types and the launch do not change which are dropped.
 //
 // Bound by bytes: with draws of 16 bits an application's forty multiplications serve
-// eight elements.  50,003 x 1,001 binary16: 36 us for the gradient, 5.5 TB/s; 2,048 x
+// eight elements.  50,003 x 1,001 binary16: 34 us for the gradient, 5.9 TB/s; 2,048 x
 // 768 binary32 with the residual: 5 us, most of it the launch.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -42,7 +42,8 @@ __device__ __forceinline__ float dropped(const Drop& c, A x, B residual, bool ad
 }
 
 // A: type read, B: type written and of the residual.  DENSE: no elements between rows, so element n lies at n.
-template <class A, class B, bool DENSE>
+// ONCE: the result goes past the caches.
+template <class A, class B, bool DENSE, bool ONCE>
 __global__ void __launch_bounds__(kDropBlock) dropout_kernel(Drop c, const A* in, const B* residual, B* out)
 {
     const uint32_t t = c.t_dev ? *c.t_dev : c.t;
@@ -65,7 +66,7 @@ __global__ void __launch_bounds__(kDropBlock) dropout_kernel(Drop c, const A* in
 #pragma unroll
             for (int k = 0; k < kDraws; ++k)
                 y[k] = (B)dropped(c, x[k], res[k], residual != nullptr, word[k / 2], k & 1);
-            store_vec<8>(out + to, y);
+            store_vec<8, ONCE>(out + to, y);
             continue;
         }
 #pragma unroll
@@ -108,13 +109,14 @@ hipError_t launch_dropout(const ea_dropout_t& c, bool backward, uint32_t t, cons
         return with_type(backward ? c.x_type : c.y_type, [&](auto b) {
             using A = decltype(a);
             using B = decltype(b);
-            if (dense)
-                hipLaunchKernelGGL((dropout_kernel<A, B, true>), dim3((unsigned)blocks), dim3(kDropBlock), 0, s, d,
-                                   (const A*)in, (const B*)residual, (B*)out);
-            else
-                hipLaunchKernelGGL((dropout_kernel<A, B, false>), dim3((unsigned)blocks), dim3(kDropBlock), 0, s, d,
-                                   (const A*)in, (const B*)residual, (B*)out);
-            return hipGetLastError();
+            return with_bool(dense, [&](auto packed) {
+                return with_bool(past_caches(d.total, backward ? c.x_type : c.y_type), [&](auto once) {
+                    hipLaunchKernelGGL((dropout_kernel<A, B, decltype(packed)::value, decltype(once)::value>),
+                                       dim3((unsigned)blocks), dim3(kDropBlock), 0, s, d, (const A*)in,
+                                       (const B*)residual, (B*)out);
+                    return hipGetLastError();
+                });
+            });
         });
     });
 }

@@ -5,6 +5,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "ea_device.hpp"
 #include "ea_layer.h"
 #include "ea_train.hpp"
@@ -33,23 +35,32 @@ __device__ __forceinline__ Vec<T, N> load_vec(const T* p)
     return *(const typename VecOf<T, N>::unaligned*)p;
 }
 
-template <int N, class T>
+// ONCE: past the caches.
+template <int N, bool ONCE = false, class T>
 __device__ __forceinline__ void store_vec(T* p, Vec<T, N> v)
 {
-    *(typename VecOf<T, N>::unaligned*)p = v;
+    typedef typename VecOf<T, N>::unaligned At;
+    if (ONCE)
+        __builtin_nontemporal_store(v, (At*)p);
+    else
+        *(At*)p = v;
 }
 
-// The same for data that a pass reads or writes once: it leaves the caches to others.
-template <int N, class T>
-__device__ __forceinline__ Vec<T, N> load_vec_once(const T* p)
+// Arrays from this size on are written past the caches: little of them would be left in the last one when the next call
+// reads them, and what is there makes way.  (Norm, recurrence, dropout, loss and their gradients in a row, arrays of
+// 16 MiB each: 131 us, and 138 past the caches; of 64 MiB: 333 and 329; of 256 MiB: 1,091 and 1,070.  Loads past them,
+// too, gain where an array comes from memory, and lose more where the call before left it: 333 and 348 at 64 MiB.)
+constexpr int64_t kOnceBytes = (int64_t)64 << 20;
+
+inline bool past_caches(int64_t elements, int32_t type)
 {
-    return __builtin_nontemporal_load((const typename VecOf<T, N>::unaligned*)p);
+    return elements >= kOnceBytes / (type == EA_F32 ? 4 : 2);
 }
 
-template <int N, class T>
-__device__ __forceinline__ void store_vec_once(T* p, Vec<T, N> v)
+template <class F>
+hipError_t with_bool(bool on, F&& f)
 {
-    __builtin_nontemporal_store(v, (typename VecOf<T, N>::unaligned*)p);
+    return on ? f(std::true_type{}) : f(std::false_type{});
 }
 
 // Element k of a vector, also of one of a single element.
@@ -71,8 +82,8 @@ __device__ __forceinline__ void set_element(Vec<T, N>& v, int k, T x)
         v[k] = x;
 }
 
-// The first `n` elements; the rest read as `rest`, and are not written.  All loads are made at once, the rest's from the
-// first element: a branch around each would make a row wait N times for memory.
+// The first `n` elements; the rest read as `rest`, and are not written.  All loads are made at once, the rest's from
+// the first element: a branch around each would make a row wait N times for memory.
 template <int N, class T>
 __device__ __forceinline__ Vec<T, N> load_part(const T* p, int n, float rest = 0.0f)
 {

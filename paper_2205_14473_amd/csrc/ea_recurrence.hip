@@ -10,8 +10,8 @@ namespace rec {
 
 namespace {
 
-// CHAIN: sequences of more than one chunk.
-template <class X, class G, bool SIGMOID, bool CHAIN>
+// CHAIN: sequences of more than one chunk.  ONCE: y goes past the caches.
+template <class X, class G, bool SIGMOID, bool CHAIN, bool ONCE>
 __global__ void __launch_bounds__(kMostWaves* kWave, 8)
     recurrence_kernel(Call a, const G* g, const X* x, const float* h0, X* y, float* states, float* h_last)
 {
@@ -24,7 +24,7 @@ __global__ void __launch_bounds__(kMostWaves* kWave, 8)
         it.draw(a);
         const int64_t t = (int64_t)(p.chunk * waves + wave) * K, row = p.b * a.c.length + t;
         const int count = steps_at<K>(t, p.n), held = steps_at<K>(t, (int)a.c.length);
-        zero_steps<K>(y, row, a.c.y_stride, a, p, count, held);
+        zero_steps<ONCE>(y, row, a.c.y_stride, a, p, count, held);
         if (p.chunk > p.last) {
             __syncthreads();
             it.next(a);
@@ -71,7 +71,7 @@ __global__ void __launch_bounds__(kMostWaves* kWave, 8)
 #pragma unroll
         for (int k = 0; k < K; ++k, to += a.c.y_stride) {
             h = __builtin_fmaf(f[k], h, v[k]);
-            store_own<X>(row_of(to, a, k < count), p, (X)h);
+            store_own<ONCE>(row_of(to, a, k < count), p, (X)h);
         }
         __syncthreads();                               // every wave has h0, and what is in LDS
         if (link.last && wave == waves - 1 && p.on) {
@@ -167,13 +167,13 @@ hipError_t launch_recurrence(const ea_recurrence_t& c, const void* g, const void
         using G = decltype(gt);
         constexpr bool S = decltype(sigmoid)::value;
         const dim3 grid(groups), block(a.p.waves * kWave);
-        if (a.p.chunks > 1)
-            hipLaunchKernelGGL((recurrence_kernel<X, G, S, true>), grid, block, 0, s, a, (const G*)g, (const X*)x, h0,
-                               (X*)y, states, h_last);
-        else
-            hipLaunchKernelGGL((recurrence_kernel<X, G, S, false>), grid, block, 0, s, a, (const G*)g, (const X*)x, h0,
-                               (X*)y, states, h_last);
-        return hipGetLastError();
+        return with_bool(a.p.chunks > 1, [&](auto chain) {
+            return with_bool(past_caches(c.batch * c.length * c.dim, c.x_type), [&](auto once) {
+                hipLaunchKernelGGL((recurrence_kernel<X, G, S, decltype(chain)::value, decltype(once)::value>), grid,
+                                   block, 0, s, a, (const G*)g, (const X*)x, h0, (X*)y, states, h_last);
+                return hipGetLastError();
+            });
+        });
     });
 }
 

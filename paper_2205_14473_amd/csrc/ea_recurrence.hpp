@@ -21,12 +21,13 @@
 // is given up, and the state is NaN.
 //
 // Bound by bytes and by what the exchange costs on top of them.  One sequence of
-// 65,536 steps of 1,024 bfloat16 channels, states saved: 128 us, 3.2 TB/s; its
-// gradient for 32 padded sequences of 2,048 steps (gates in binary32) 170 us; 2 x
-// 16,384 x 768 binary32 with plain gates, the gradient, 122 us.  Steps as segments
-// of whole sequences, the ends of which a first pass forms: 220 / 190 / 171 us.
-// Groups alone, without stretches, 124 / 168 / 122, but a wait that passes on every
-// 4,096 steps.  Three chunks in registers and one workgroup a CU, to have loads on
+// 65,536 steps of 1,024 bfloat16 channels, states saved: 124 us, 3.3 TB/s; the
+// gradient of 32 padded sequences of 2,048 steps (gates in binary32) 160 us, 4.5 TB/s;
+// that of 2 x 16,384 x 768 binary32 with plain gates 117 us, 4.3 TB/s.  Other ways,
+// before the results went past the caches (128 / 170 / 122 us then): steps as segments
+// of whole sequences, the ends of which a first pass forms: 220 / 190 / 171.  Groups
+// alone, without stretches: 124 / 168 / 122, but a wait that passes on every 4,096
+// steps.  Three chunks in registers and one workgroup a CU, to have loads on
 // their way during the exchange: 140 / 214 / 115; a wave of its own for the exchange:
 // 207 / 333 / 160.
 #pragma once
@@ -202,14 +203,21 @@ __device__ __forceinline__ T load_own(__amdgpu_buffer_rsrc_t row, const Place& a
         return __builtin_bit_cast(T, __builtin_amdgcn_raw_buffer_load_b32(row, off, 0, 0));
 }
 
-template <class T>
+constexpr int kPastCaches = 2;                         // of a buffer store
+
+template <int HOW, class T>
+__device__ __forceinline__ void store_how(__amdgpu_buffer_rsrc_t row, uint32_t off, T v)
+{
+    if constexpr (sizeof(T) == 2)
+        __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(uint16_t, v), row, off, 0, HOW);
+    else
+        __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(uint32_t, v), row, off, 0, HOW);
+}
+
+template <bool ONCE = false, class T>
 __device__ __forceinline__ void store_own(__amdgpu_buffer_rsrc_t row, const Place& at, T v)
 {
-    const uint32_t off = at.channel * (uint32_t)sizeof(T);
-    if constexpr (sizeof(T) == 2)
-        __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(uint16_t, v), row, off, 0, 0);
-    else
-        __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(uint32_t, v), row, off, 0, 0);
+    store_how<ONCE ? kPastCaches : 0>(row, at.channel * (uint32_t)sizeof(T), v);
 }
 
 // A wave's steps from row `row` on, as they are stored; from step `count` on they are 0.
@@ -248,11 +256,11 @@ __device__ __forceinline__ int steps_at(int64_t t, int end)
 }
 
 // Zeros in the wave's steps that a sequence has no use for.
-template <int K, class T>
+template <bool ONCE, class T>
 __device__ __forceinline__ void zero_steps(T* p, int64_t row, int64_t stride, const Call& a, const Place& at, int from,
                                            int to)
 {
-    for (int k = from; k < to; ++k) store_own<T>(row_of(p + (row + k) * stride, a, true), at, (T)0.0f);
+    for (int k = from; k < to; ++k) store_own<ONCE>(row_of(p + (row + k) * stride, a, true), at, (T)0.0f);
 }
 
 // a and w of a gate: e / (1 + e) with e = exp(-|g|) for the smaller of them, and what is left of 1 for the other.  The

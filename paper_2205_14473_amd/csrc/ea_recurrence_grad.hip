@@ -13,8 +13,8 @@ namespace rec {
 namespace {
 
 // What arrives at step t from behind is e_t = a_{t+1} d_{t+1}, with d_t = dy_t + e_t; over some steps it goes from e to
-// (product of their gates) e + (what they give from e = 0).
-template <class X, class G, bool SIGMOID, bool CHAIN>
+// (product of their gates) e + (what they give from e = 0).  ONCE: dx and dg go past the caches.
+template <class X, class G, bool SIGMOID, bool CHAIN, bool ONCE>
 __global__ void __launch_bounds__(kMostWaves* kWave, 8)
     recurrence_grad_kernel(Call a, const G* g, const X* x, const float* states, const X* dy, const float* dh_last,
                            G* dg, X* dx, float* dh0)
@@ -28,8 +28,8 @@ __global__ void __launch_bounds__(kMostWaves* kWave, 8)
         it.draw(a);
         const int64_t t = (int64_t)(p.chunk * waves + wave) * K, row = p.b * a.c.length + t;
         const int count = steps_at<K>(t, p.n), held = steps_at<K>(t, (int)a.c.length);
-        zero_steps<K>(dx, row, a.c.x_stride, a, p, count, held);
-        zero_steps<K>(dg, row, a.c.g_stride, a, p, count, held);
+        zero_steps<ONCE>(dx, row, a.c.x_stride, a, p, count, held);
+        zero_steps<ONCE>(dg, row, a.c.g_stride, a, p, count, held);
         if (p.chunk > p.last) {
             __syncthreads();
             it.next(a);
@@ -94,8 +94,8 @@ __global__ void __launch_bounds__(kMostWaves* kWave, 8)
         for (int k = K - 1; k >= 0; --k, tx -= a.c.x_stride, tg -= a.c.g_stride) {
             const float s = d[k] + e;
             e = f[k] * s;                              // f = 1, d = 0 where the step does not count
-            store_own<X>(row_of(tx, a, k < count), p, (X)(w[k] * s));
-            store_own<G>(row_of(tg, a, k < count), p, (G)(u[k] * s));
+            store_own<ONCE>(row_of(tx, a, k < count), p, (X)(w[k] * s));
+            store_own<ONCE>(row_of(tg, a, k < count), p, (G)(u[k] * s));
         }
         __syncthreads();                               // every wave has dh_last, and what is in LDS
         if (link.last && wave == 0 && p.on && dh0) dh0[p.b * a.c.dim + p.channel] = e;
@@ -119,13 +119,14 @@ hipError_t launch_recurrence_grad(const ea_recurrence_t& c, const void* g, const
         using G = decltype(gt);
         constexpr bool S = decltype(sigmoid)::value;
         const dim3 grid(groups), block(a.p.waves * kWave);
-        if (a.p.chunks > 1)
-            hipLaunchKernelGGL((recurrence_grad_kernel<X, G, S, true>), grid, block, 0, s, a, (const G*)g, (const X*)x,
-                               states, (const X*)dy, dh_last, (G*)dg, (X*)dx, dh0);
-        else
-            hipLaunchKernelGGL((recurrence_grad_kernel<X, G, S, false>), grid, block, 0, s, a, (const G*)g, (const X*)x,
-                               states, (const X*)dy, dh_last, (G*)dg, (X*)dx, dh0);
-        return hipGetLastError();
+        return with_bool(a.p.chunks > 1, [&](auto chain) {
+            return with_bool(past_caches(c.batch * c.length * c.dim, c.x_type), [&](auto once) {
+                hipLaunchKernelGGL((recurrence_grad_kernel<X, G, S, decltype(chain)::value, decltype(once)::value>),
+                                   grid, block, 0, s, a, (const G*)g, (const X*)x, states, (const X*)dy, dh_last,
+                                   (G*)dg, (X*)dx, dh0);
+                return hipGetLastError();
+            });
+        });
     });
 }
 

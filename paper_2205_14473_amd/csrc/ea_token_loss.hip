@@ -8,9 +8,9 @@
 // are counted by a launch of their own.
 //
 // Bound by bytes: the logits once, their gradient once.  8,192 rows of 50,257
-// bfloat16 logits with the gradient: 323 us, 5.1 TB/s (1,131 when the exponentials
+// bfloat16 logits with the gradient: 317 us, 5.2 TB/s (1,131 when the exponentials
 // of a pass were kept for the next, which spilled; 458 when each pass makes its
-// own).  2,048 rows of 32,000 binary32: 113 us, 4.6 TB/s.
+// own).  2,048 rows of 32,000 binary32: 106 us, 5.0 TB/s.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -132,7 +132,6 @@ __device__ __forceinline__ float exp_under(float z, float top)
 // Four words of a row made opaque: what a pass made of them (as floats, and their exponentials) is made anew by the
 // next one.  Kept, it would take two to four times the registers of the row itself.
 typedef uint32_t Words __attribute__((ext_vector_type(4)));
-typedef Words WordsAt __attribute__((aligned(2)));
 
 __device__ __forceinline__ void renew(Words& w)
 {
@@ -201,7 +200,7 @@ __device__ __forceinline__ Words load_words(const Grid<const T>& g, int at)
     return __builtin_bit_cast(Words, v);
 }
 
-template <class T>
+template <bool ONCE, class T>
 __device__ __forceinline__ void store_floats_of(const Grid<T>& g, int at, const float* x)
 {
     constexpr int V = 16 / sizeof(T);
@@ -209,12 +208,12 @@ __device__ __forceinline__ void store_floats_of(const Grid<T>& g, int at, const 
     const Vec<T, V> v = narrow_from<V, T>(x);
     const uint32_t off = (uint32_t)lane_id() * 16u;
     if (at >= g.head && at + kWave * V <= g.end) {
-        *(WordsAt*)((char*)p + off) = __builtin_bit_cast(Words, v);
+        store_vec<V, ONCE>((T*)((char*)p + off), v);
         return;
     }
     const int mine = at + lane_id() * V;
     if (mine >= g.head && mine + V <= g.end) {
-        *(WordsAt*)((char*)p + off) = __builtin_bit_cast(Words, v);
+        store_vec<V, ONCE>((T*)((char*)p + off), v);
     } else {
         T* q = (T*)((char*)p + off);
 #pragma unroll
@@ -223,16 +222,17 @@ __device__ __forceinline__ void store_floats_of(const Grid<T>& g, int at, const 
     }
 }
 
-template <class T>
+template <bool ONCE, class T>
 __device__ __forceinline__ void zero_row(const Grid<T>& g, int first, int lanes)
 {
     constexpr int V = 16 / sizeof(T);
     const float none[V] = {};
-    for (int at = first; at < g.end; at += lanes * V) store_floats_of(g, at, none);
+    for (int at = first; at < g.end; at += lanes * V) store_floats_of<ONCE>(g, at, none);
 }
 
 // WAVES of a row (1: four rows a workgroup), K vectors of 16 bytes a lane; K = 0: a row that is read again.
-template <class T, int WAVES, int K, bool GRAD>
+// ONCE: the gradient goes past the caches.
+template <class T, int WAVES, int K, bool GRAD, bool ONCE>
 __global__ void __launch_bounds__(WAVES == 1 ? 256 : WAVES * kWave, 4)
     loss_kernel(Loss a, const T* logits, T* dlogits)
 {
@@ -265,7 +265,7 @@ __global__ void __launch_bounds__(WAVES == 1 ? 256 : WAVES * kWave, 4)
         T* to = dlogits + row * a.c.dlogits_stride;
         if (target < 0) {
             if (lane == 0 && a.loss) a.loss[row] = 0.0f;
-            if (GRAD) zero_row(Grid<T>(to, vocab, cell_of(WAVES)), first, kLanes);
+            if (GRAD) zero_row<ONCE>(Grid<T>(to, vocab, cell_of(WAVES)), first, kLanes);
             if (K > 0) load(after);
         } else {
             const Grid<const T> in(from, vocab, cell_of(WAVES)), next(after, vocab, cell_of(WAVES));
@@ -318,7 +318,7 @@ __global__ void __launch_bounds__(WAVES == 1 ? 256 : WAVES * kWave, 4)
                         as_floats<T>(x, w);
 #pragma unroll
                         for (int i = 0; i < V; ++i) x[i] = exp_under(x[i], top) * share;
-                        store_floats_of(out, at, x);
+                        store_floats_of<ONCE>(out, at, x);
                     },
                     true);
                 // the lane that wrote the target's element writes it again, less the factor
@@ -419,13 +419,13 @@ int64_t counting_groups(const ea_token_loss_t& c)
     return c.rows > kOwnCount * threads ? at_most((c.rows + kCountBlock * 4 - 1) / (kCountBlock * 4), kMostCounts) : 0;
 }
 
-template <class T, bool GRAD>
+template <class T, bool GRAD, bool ONCE>
 hipError_t start_loss(const Loss& a, Shape s, unsigned groups, const void* logits, void* dlogits, hipStream_t st)
 {
 #define EA_SHAPE(W, K)                                                                                            \
     if (s.waves == W && s.k == K) {                                                                               \
-        hipLaunchKernelGGL((loss_kernel<T, W, K, GRAD>), dim3(groups), dim3(W == 1 ? 256 : W * kWave), 0, st, a,  \
-                           (const T*)logits, (T*)dlogits);                                                        \
+        hipLaunchKernelGGL((loss_kernel<T, W, K, GRAD, ONCE>), dim3(groups), dim3(W == 1 ? 256 : W * kWave), 0,   \
+                           st, a, (const T*)logits, (T*)dlogits);                                                 \
         return hipGetLastError();                                                                                 \
     }
     EA_SHAPES
@@ -462,8 +462,10 @@ hipError_t launch_token_loss(const ea_token_loss_t& c, const void* logits, const
         e = with_type(c.type, [&](auto t) {
             using T = decltype(t);
             const unsigned groups = (unsigned)groups_of(c, shape);
-            return dlogits ? start_loss<T, true>(a, shape, groups, logits, dlogits, s)
-                           : start_loss<T, false>(a, shape, groups, logits, dlogits, s);
+            if (!dlogits) return start_loss<T, false, false>(a, shape, groups, logits, dlogits, s);
+            return with_bool(past_caches(c.rows * c.vocab, c.type), [&](auto once) {
+                return start_loss<T, true, decltype(once)::value>(a, shape, groups, logits, dlogits, s);
+            });
         });
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL(loss_end_kernel, dim3(1), dim3(kEndBlock), 0, s, a, sums_of(c, shape), total, count);
