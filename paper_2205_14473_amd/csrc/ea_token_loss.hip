@@ -3,9 +3,9 @@
 //
 // A row is held in registers, as it is stored, by 1, 4 or 16 waves: its largest
 // logit and the sum of exponentials are reductions, and the gradient leaves the
-// same registers.  Longer rows are read twice.  The mean's gradient needs the
-// number of tokens that count first: a workgroup counts few targets itself, many
-// are counted by a launch of their own.
+// same registers.  Longer rows are cut into pieces and read twice.  The mean's
+// gradient needs the number of tokens that count first: a workgroup counts few
+// targets itself, many are counted by a launch of their own.
 //
 // Bound by bytes: the logits once, their gradient once.  8,192 rows of 50,257
 // bfloat16 logits with the gradient: 317 us, 5.2 TB/s (1,131 when the exponentials
@@ -29,7 +29,8 @@ constexpr int64_t kOwnCount = 16;                      // targets a thread up to
 constexpr int64_t kMostWaves = 4096;                   // of the main pass, 16 a CU: each row's waves leave one sum
 constexpr int kEndBlock = 256;
 
-// Workspace: the counting groups' counts, then each main group's sum and count.
+// Workspace: the counting groups' counts, then each main group's sum and count (for rows in pieces each row's, then
+// each piece's largest logit and sum, then each row's target's logit).
 struct Sums {
     double loss;
     int64_t count;
@@ -43,6 +44,9 @@ struct Loss {
     int64_t* counts;                                   // of `parts` groups, or NULL: the targets are few
     Sums* sums;
     int32_t parts;
+    int32_t pieces;                                    // of a row
+    float2* ends;                                      // each piece's largest logit and sum
+    float* hits;                                       // each row's target's logit
 };
 
 // The target of a row, -1 where it does not count.
@@ -230,7 +234,7 @@ __device__ __forceinline__ void zero_row(const Grid<T>& g, int first, int lanes)
     for (int at = first; at < g.end; at += lanes * V) store_floats_of<ONCE>(g, at, none);
 }
 
-// WAVES of a row (1: four rows a workgroup), K vectors of 16 bytes a lane; K = 0: a row that is read again.
+// WAVES of a row (1: four rows a workgroup), K vectors of 16 bytes a lane.
 // ONCE: the gradient goes past the caches.
 template <class T, int WAVES, int K, bool GRAD, bool ONCE>
 __global__ void __launch_bounds__(WAVES == 1 ? 256 : WAVES * kWave, 4)
@@ -246,13 +250,13 @@ __global__ void __launch_bounds__(WAVES == 1 ? 256 : WAVES * kWave, 4)
     int64_t row = (int64_t)blockIdx.x * kRows + slot;
     int target = uniform(row < a.c.rows ? target_at(a, row) : -1);
     const T* from = logits + (row < a.c.rows ? row : 0) * a.c.logits_stride;
-    Words z[K ? K : 1];
+    Words z[K];
     auto load = [&](const T* p) {
         const Grid<const T> g(p, vocab, cell_of(WAVES));
 #pragma unroll
         for (int k = 0; k < K; ++k) z[k] = load_words(g, k * kLanes * V + first);
     };
-    if (K > 0) load(from);
+    load(from);
     const float factor = GRAD ? row_factor<kThreads>(a) : 0.0f;
     double total = 0.0;
     int64_t used = 0;
@@ -266,23 +270,18 @@ __global__ void __launch_bounds__(WAVES == 1 ? 256 : WAVES * kWave, 4)
         if (target < 0) {
             if (lane == 0 && a.loss) a.loss[row] = 0.0f;
             if (GRAD) zero_row<ONCE>(Grid<T>(to, vocab, cell_of(WAVES)), first, kLanes);
-            if (K > 0) load(after);
+            load(after);
         } else {
             const Grid<const T> in(from, vocab, cell_of(WAVES)), next(after, vocab, cell_of(WAVES));
             float top = -__builtin_inff(), sum = 0.0f, x[V];
-            // f(vector, the wave's first element of it on the grid) for each of the lane's vectors, from its registers
-            // or from memory again
+            // f(vector, the wave's first element of it on the grid) for each of the lane's vectors
             auto every = [&](auto&& f, bool last) {
-                if constexpr (K > 0) {
 #pragma unroll
-                    for (int k = 0; k < K; ++k) {
-                        const int at = k * kLanes * V + first;
-                        renew(z[k]);
-                        if (at < in.end) f(z[k], at);
-                        if (last) z[k] = load_words(next, at);
-                    }
-                } else {
-                    for (int at = first; at < in.end; at += kLanes * V) f(load_words(in, at), at);
+                for (int k = 0; k < K; ++k) {
+                    const int at = k * kLanes * V + first;
+                    renew(z[k]);
+                    if (at < in.end) f(z[k], at);
+                    if (last) z[k] = load_words(next, at);
                 }
             };
             // The target's logit, from one lane before the last reduction: when rows are written where they were read,
@@ -334,6 +333,121 @@ __global__ void __launch_bounds__(WAVES == 1 ? 256 : WAVES * kWave, 4)
     if (lane == 0) a.sums[(int64_t)blockIdx.x * kRows + slot] = Sums{total, used};
 }
 
+// Rows too long for registers, in pieces of a workgroup each: the largest logit of a piece and its sum under that,
+// then, from those of all pieces, in one order, the loss and the piece's gradient.  (A workgroup a row that reads it again,
+// eight vectors ahead, against pieces: 1 row of 250,000 binary32 logits 45 us and 14; 60 of 200,001 47 and 26; 1,000 of
+// 100,000 221 and 206.)
+constexpr int kPieceWaves = 4, kPieceVectors = 8, kPieceThreads = kPieceWaves * kWave;
+
+template <class T>
+constexpr int kPiece = kPieceThreads * kPieceVectors * 16 / (int)sizeof(T);      // elements
+
+template <class T>
+__global__ void __launch_bounds__(kPieceThreads) loss_ends_kernel(Loss a, const T* logits)
+{
+    constexpr int V = 16 / sizeof(T);
+    __shared__ float lds[2][kPieceWaves];
+    const int64_t items = a.c.rows * a.pieces;
+    for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
+        const int64_t row = item / a.pieces;
+        const int target = uniform(target_at(a, row));
+        if (target < 0) continue;
+        const T* from = logits + row * a.c.logits_stride;
+        const Grid<const T> g(from, (int)a.c.vocab, cell_of(kPieceWaves));
+        const int start = (int)(item - row * a.pieces) * kPiece<T>, first = start + wave_id() * kWave * V;
+        Words z[kPieceVectors];
+#pragma unroll
+        for (int k = 0; k < kPieceVectors; ++k) z[k] = load_words(g, first + k * kPieceThreads * V);
+        float x[V], top = -__builtin_inff(), sum = 0.0f;
+#pragma unroll
+        for (int k = 0; k < kPieceVectors; ++k) {
+            as_floats<T>(x, z[k]);
+#pragma unroll
+            for (int i = 0; i < V; ++i) top = fmaxf(top, x[i]);
+        }
+        top = group_max<kPieceWaves>(top, lds[0]);
+        const float base = top == -__builtin_inff() ? 0.0f : top;      // nothing but -infinity: a sum of 0 (NaN: NaN)
+#pragma unroll
+        for (int k = 0; k < kPieceVectors; ++k) {
+            renew(z[k]);
+            as_floats<T>(x, z[k]);
+#pragma unroll
+            for (int i = 0; i < V; ++i) sum = sum + exp_under(x[i], base);
+        }
+        sum = group_sum<kPieceWaves>(sum, lds[1]);
+        if (threadIdx.x == 0) {
+            a.ends[item] = make_float2(top, sum);
+            const int at = target + g.head - start;
+            if (at >= 0 && at < kPiece<T>) a.hits[row] = (float)from[target];
+        }
+        __syncthreads();                               // the next piece's reductions write where this one's were read
+    }
+}
+
+template <class T, bool GRAD, bool ONCE>
+__global__ void __launch_bounds__(kPieceThreads) loss_pieces_kernel(Loss a, const T* logits, T* dlogits)
+{
+    constexpr int V = 16 / sizeof(T);
+    __shared__ float lds[2][kPieceWaves];
+    const int64_t items = GRAD ? a.c.rows * a.pieces : a.c.rows;
+    const float factor = GRAD ? row_factor<kPieceThreads>(a) : 0.0f;
+    for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
+        const int64_t row = GRAD ? item / a.pieces : item;
+        const int piece = GRAD ? (int)(item - row * a.pieces) : 0;
+        const int target = uniform(target_at(a, row)), vocab = (int)a.c.vocab;
+        const T* from = logits + row * a.c.logits_stride;
+        const Grid<const T> in(from, vocab, cell_of(kPieceWaves));
+        T* to = dlogits + row * a.c.dlogits_stride;
+        const Grid<T> out(to, in);
+        const int start = piece * kPiece<T>, first = start + wave_id() * kWave * V;
+        if (target < 0) {
+            if (piece == 0 && threadIdx.x == 0) {
+                if (a.loss) a.loss[row] = 0.0f;
+                a.sums[row] = Sums{0.0, 0};
+            }
+            if (GRAD) {
+                const float none[V] = {};
+#pragma unroll
+                for (int k = 0; k < kPieceVectors; ++k) store_floats_of<ONCE>(out, first + k * kPieceThreads * V, none);
+            }
+            continue;
+        }
+        Words z[kPieceVectors];
+        if (GRAD) {
+#pragma unroll
+            for (int k = 0; k < kPieceVectors; ++k) z[k] = load_words(in, first + k * kPieceThreads * V);
+        }
+        const float2* ends = a.ends + row * a.pieces;
+        float top = -__builtin_inff(), sum = 0.0f;
+        for (int i = threadIdx.x; i < a.pieces; i += kPieceThreads) top = fmaxf(top, ends[i].x);
+        top = group_max<kPieceWaves>(top, lds[0]);
+        for (int i = threadIdx.x; i < a.pieces; i += kPieceThreads) sum = sum + ends[i].y * exp_under(ends[i].x, top);
+        sum = group_sum<kPieceWaves>(sum, lds[1]);
+        const float hit = a.hits[row];
+        if (piece == 0 && threadIdx.x == 0) {
+            const float loss = logf(sum) - (hit - top);
+            if (a.loss) a.loss[row] = loss;
+            a.sums[row] = Sums{(double)loss, 1};
+        }
+        if constexpr (GRAD) {
+            const float share = factor / sum;
+            float x[V];
+#pragma unroll
+            for (int k = 0; k < kPieceVectors; ++k) {
+                as_floats<T>(x, z[k]);
+#pragma unroll
+                for (int i = 0; i < V; ++i) x[i] = exp_under(x[i], top) * share;
+                store_floats_of<ONCE>(out, first + k * kPieceThreads * V, x);
+            }
+            // the lane that wrote the target's element writes it again, less the factor
+            const int at = target + in.head - start;
+            if (at >= 0 && at < kPiece<T> && at / V % kPieceThreads == (int)threadIdx.x)
+                to[target] = (T)(exp_under(hit, top) * share - factor);
+        }
+        __syncthreads();                               // the next piece's reductions write where this one's were read
+    }
+}
+
 // The groups' sums, in their order.
 __global__ void __launch_bounds__(kEndBlock) loss_end_kernel(Loss a, int64_t groups, float* total, int32_t* count)
 {
@@ -363,8 +477,8 @@ int64_t at_most(int64_t n, int64_t most)
     return n < most ? n : most;
 }
 
-// Waves of a row and vectors a lane: the first that holds it, or 16 and 0 where none does.  Few waves with many vectors
-// each: rows of their own work beside each other on a CU, one reading or writing while another reduces.
+// Waves of a row and vectors a lane: the first that holds it, or those of a piece and 0 where none does.  Few waves with
+// many vectors each: rows of their own work beside each other on a CU, one reading or writing while another reduces.
 struct Shape {
     int waves, k;
 };
@@ -399,7 +513,14 @@ Shape shape_of(const ea_token_loss_t& c)
     for (const Shape& s : all)
         // wherever in a cell a row starts
         if (c.vocab + cell_of(s.waves) / 16 * v - 1 <= v * kWave * s.waves * s.k) return s;
-    return {16, 0};
+    return {kPieceWaves, 0};
+}
+
+// Pieces of a row that is not held, wherever in a cell it starts.
+int64_t pieces_of(const ea_token_loss_t& c)
+{
+    const int64_t size = c.type == EA_F32 ? 4 : 2, piece = kPieceThreads * kPieceVectors * 16 / size;
+    return (c.vocab + cell_of(kPieceWaves) / size - 1 + piece - 1) / piece;
 }
 
 // Workgroups of the main pass, and the sums they leave.
@@ -410,7 +531,7 @@ int64_t groups_of(const ea_token_loss_t& c, Shape s)
 
 int64_t sums_of(const ea_token_loss_t& c, Shape s)
 {
-    return groups_of(c, s) * (s.waves == 1 ? 4 : 1);
+    return s.k == 0 ? c.rows : groups_of(c, s) * (s.waves == 1 ? 4 : 1);
 }
 
 int64_t counting_groups(const ea_token_loss_t& c)
@@ -429,16 +550,29 @@ hipError_t start_loss(const Loss& a, Shape s, unsigned groups, const void* logit
         return hipGetLastError();                                                                                 \
     }
     EA_SHAPES
-    EA_SHAPE(16, 0)
 #undef EA_SHAPE
     return hipErrorInvalidValue;
+}
+
+template <class T, bool GRAD, bool ONCE>
+hipError_t start_pieces(const Loss& a, const void* logits, void* dlogits, hipStream_t st)
+{
+    const int64_t items = a.c.rows * a.pieces, most = 1 << 20;
+    hipLaunchKernelGGL(loss_ends_kernel<T>, dim3((unsigned)at_most(items, most)), dim3(kPieceThreads), 0, st, a,
+                       (const T*)logits);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((loss_pieces_kernel<T, GRAD, ONCE>), dim3((unsigned)at_most(GRAD ? items : a.c.rows, most)),
+                       dim3(kPieceThreads), 0, st, a, (const T*)logits, (T*)dlogits);
+    return hipGetLastError();
 }
 
 }  // namespace
 
 int64_t token_loss_workspace_bytes(const ea_token_loss_t& c)
 {
-    return counting_groups(c) * 16 + sums_of(c, shape_of(c)) * 16;
+    const Shape s = shape_of(c);
+    return counting_groups(c) * 16 + sums_of(c, s) * 16 + (s.k == 0 ? c.rows * pieces_of(c) * 8 + c.rows * 4 : 0);
 }
 
 hipError_t launch_token_loss(const ea_token_loss_t& c, const void* logits, const void* targets, float* loss,
@@ -451,6 +585,11 @@ hipError_t launch_token_loss(const ea_token_loss_t& c, const void* logits, const
     a.targets = targets;
     a.loss = loss;
     a.sums = (Sums*)((char*)workspace + parts * 16);
+    if (shape.k == 0) {
+        a.pieces = (int32_t)pieces_of(c);
+        a.ends = (float2*)(a.sums + c.rows);
+        a.hits = (float*)(a.ends + c.rows * a.pieces);
+    }
     hipError_t e = hipSuccess;
     if (dlogits && c.reduction == EA_REDUCE_MEAN && parts > 0) {
         a.counts = (int64_t*)workspace;
@@ -462,9 +601,13 @@ hipError_t launch_token_loss(const ea_token_loss_t& c, const void* logits, const
         e = with_type(c.type, [&](auto t) {
             using T = decltype(t);
             const unsigned groups = (unsigned)groups_of(c, shape);
-            if (!dlogits) return start_loss<T, false, false>(a, shape, groups, logits, dlogits, s);
+            if (!dlogits)
+                return shape.k ? start_loss<T, false, false>(a, shape, groups, logits, dlogits, s)
+                               : start_pieces<T, false, false>(a, logits, dlogits, s);
             return with_bool(past_caches(c.rows * c.vocab, c.type), [&](auto once) {
-                return start_loss<T, true, decltype(once)::value>(a, shape, groups, logits, dlogits, s);
+                constexpr bool O = decltype(once)::value;
+                return shape.k ? start_loss<T, true, O>(a, shape, groups, logits, dlogits, s)
+                               : start_pieces<T, true, O>(a, logits, dlogits, s);
             });
         });
     if (e != hipSuccess) return e;

@@ -11,7 +11,7 @@ if not torch.cuda.is_available():  # pragma: no cover - CPU-only host
 import layer_util as L  # noqa: E402
 import paper_2205_14473_amd as E  # noqa: E402
 import train_util as R  # noqa: E402
-from layer_util import TYPES  # noqa: E402
+from layer_util import TYPES, U32  # noqa: E402
 
 
 def config(rows, vocab, kind, bits=64, gap=0, dgap=0, scale=1.0, mean=True):
@@ -216,3 +216,61 @@ def test_graph_streams_and_the_same_bits():
             call()
             torch.cuda.synchronize()
             assert all(torch.equal(p, q) for p, q in zip(got, every()))
+
+
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("vocab", [135_168, 147_455, 163_841, 250_007])
+def test_rows_in_pieces(vocab, kind):
+    """Rows that no workgroup holds: targets at every piece's ends, wherever the rows begin, pieces without a logit that
+    is not -infinity, rows that do not count between them."""
+    dtype = TYPES[kind]
+    size = torch.empty(0, dtype=dtype).element_size()
+    piece = 32_768 // size
+    rows = 2 * (vocab // piece) + 3
+    z, t = inputs(rows, vocab, dtype)
+    for i in range(rows - 3):
+        t[i] = min(vocab - 1, (i // 2 + 1) * piece - 1 + i % 2 - (i % 3) * 5)
+    t[rows - 3], t[rows - 2], t[rows - 1] = vocab - 1, -100, 0
+    z[1, :piece + 70], z[2, -3 * piece:], z[rows - 1, 1:] = -float("inf"), -float("inf"), -float("inf")
+    t[1], t[2] = vocab - 9, 3
+    for gap, dgap, shift, mean in ((0, 0, 0, True), (7, 3, 1, False)):
+        c = config(rows, vocab, dtype, gap=gap, dgap=dgap, mean=mean, scale=300.0)
+        zw = torch.where(z == -float("inf"), torch.full((), -1e4, dtype=dtype), z)     # as good as -infinity: e^-9000 is 0
+        got = run(z, t, c, shift=shift)
+        check(got, zw, t, c)
+        assert got[0][rows - 1].item() == 0.0 and bool((got[3][1, :piece + 70] == 0).all())
+        again = run(z, t, config(rows, vocab, dtype, gap=gap, dgap=gap, mean=mean, scale=300.0), shift=shift, in_place=True)
+        for a, b in zip(got, again):
+            assert torch.equal(a, b)
+        alone = run(z, t, c, grad=False, shift=shift)
+        for a, b in zip(got[:3], alone[:3]):
+            assert torch.equal(a, b)
+
+
+def test_pieces_in_a_graph_and_many_rows():
+    """More rows than a workgroup counts itself, replayed."""
+    rows, vocab = 4_200, 66_000
+    z = torch.randn((rows, vocab), device="cuda", generator=torch.Generator(device="cuda").manual_seed(3))
+    t = torch.randint(-1, vocab, (rows,), device="cuda", generator=torch.Generator(device="cuda").manual_seed(4))
+    c = config(rows, vocab, torch.float32)
+    dz, loss, total = torch.empty_like(z), torch.empty(rows, device="cuda"), torch.empty(1, device="cuda")
+    count = torch.empty(1, dtype=torch.int32, device="cuda")
+    ws = torch.empty(E.ea_token_loss_workspace_bytes(c), dtype=torch.uint8, device="cuda")
+    E.ea_token_loss(c, z, t, loss, total, count, dz, ws)
+    kept = [v.clone() for v in (loss, total, count, dz[::50])]
+    assert count.item() == int((t >= 0).sum())
+    few = slice(0, rows, 700)
+    want = L.Loss(z[few].double().cpu(), t[few].cpu(), 1.0, False)
+    R.within(loss[few], want.loss, want.loss_bound, "loss")
+    # the gradient's factor is 1 / count: two roundings more
+    R.within(dz[few], want.dz / count.item(), want.dz_bound / count.item() + 2 * U32 * want.dz.abs() / count.item() + 2.0 ** -140,
+             "dlogits")
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        E.ea_token_loss(c, z, t, loss, total, count, dz, ws)
+    for _ in range(3):
+        for v in (loss, total, count, dz, ws):
+            v.view(torch.uint8).fill_(0xA5)
+        graph.replay()
+        assert all(map(torch.equal, (loss, total, count, dz[::50]), kept))
+        torch.cuda.synchronize()
