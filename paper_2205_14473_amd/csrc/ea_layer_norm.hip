@@ -5,8 +5,13 @@
 // read again for each of their sums.
 //
 // The squares are summed of differences from the mean, from the same registers:
-// nothing cancels.  Bound by bytes: 65,536 x 1,024 bfloat16 50 us, 5.4 TB/s, where a
-// copy of as much reaches 5.1.  Few rows are bound by the launch: 16 x 768 3 us.
+// nothing cancels.  The mean is a quotient, not a product with a rounded 1 / dim: a row
+// of one value whose sum is exact has that value as its mean, and gives the bias (as a
+// product the mean is a unit off at some widths, and 1 / sqrt(eps) times that is in the
+// result: up to 0.3 for a row of 10,000s).
+//
+// Bound by bytes: 65,536 x 1,024 bfloat16 50 us, 5.4 TB/s, where a copy of as much
+// reaches 5.1.  Few rows are bound by the launch: 16 x 768 3 us.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -26,10 +31,12 @@ __device__ __forceinline__ float row_sum(float a, float2* lds)
     return a;
 }
 
-// ONCE: the result goes past the caches.
+// n, each: dim and 1 / dim, from the host so that they are scalars (in vector registers one wave less fits a SIMD: 65,536
+// x 1,024 bfloat16 52.7 us, and 50.2 this way).  ONCE: the result goes past the caches.
 template <class X, class Y, bool TAIL, int WAVES, int K, bool ONCE>
 __global__ void __launch_bounds__(WAVES == 1 ? 256 : WAVES * kWave)
-    norm_kernel(ea_layer_norm_t c, const X* x, const void* weight, const void* bias, Y* y, float* mean, float* rstd)
+    norm_kernel(ea_layer_norm_t c, const X* x, const void* weight, const void* bias, Y* y, float* mean, float* rstd,
+                float n, float each)
 {
     constexpr int V = vec_of<X, Y, TAIL>(), kRows = WAVES == 1 ? 4 : 1;          // of a workgroup
     __shared__ float2 lds[WAVES];
@@ -41,7 +48,6 @@ __global__ void __launch_bounds__(WAVES == 1 ? 256 : WAVES * kWave)
         load_weights<V>(w + k * V, weight, c.w_type, at, dim, 1.0f, tail_of<TAIL, WAVES, K>(k));
         load_weights<V>(b + k * V, bias, c.w_type, at, dim, 0.0f, tail_of<TAIL, WAVES, K>(k));
     }
-    const float each = 1.0f / (float)dim;
     for (int64_t row = (int64_t)blockIdx.x * kRows + (WAVES == 1 ? wave_id() : 0); row < c.rows;
          row += (int64_t)gridDim.x * kRows) {
         float v[K * V], sum = 0.0f;
@@ -51,7 +57,7 @@ __global__ void __launch_bounds__(WAVES == 1 ? 256 : WAVES * kWave)
                         tail_of<TAIL, WAVES, K>(k));
 #pragma unroll
         for (int k = 0; k < K * V; ++k) sum = sum + v[k];
-        const float mu = row_sum<WAVES>(sum, lds) * each;
+        const float mu = quotient(row_sum<WAVES>(sum, lds), n, each);
         float squares = 0.0f;
 #pragma unroll
         for (int k = 0; k < K * V; ++k) {
@@ -77,12 +83,11 @@ __global__ void __launch_bounds__(WAVES == 1 ? 256 : WAVES * kWave)
 template <class X, class Y, bool TAIL, bool ONCE>
 __global__ void __launch_bounds__(kLongBlock)
     norm_long_kernel(ea_layer_norm_t c, const X* x, const void* weight, const void* bias, Y* y, float* mean,
-                     float* rstd)
+                     float* rstd, float n, float each)
 {
     constexpr int V = vec_of<X, Y, TAIL>();
     __shared__ float2 lds[kLongBlock / kWave];
     const int dim = (int)c.dim;
-    const float each = 1.0f / (float)dim;
     for (int64_t row = blockIdx.x; row < c.rows; row += gridDim.x) {
         const X* from = x + row * c.x_stride;
         Y* to = y + row * c.y_stride;
@@ -92,7 +97,7 @@ __global__ void __launch_bounds__(kLongBlock)
 #pragma unroll
             for (int k = 0; k < V; ++k) sum = sum + v[k];
         }
-        const float mu = row_sum<kLongBlock / kWave>(sum, lds) * each;
+        const float mu = quotient(row_sum<kLongBlock / kWave>(sum, lds), n, each);
         for (int at = threadIdx.x * V; at < dim; at += kLongBlock * V) {
             load_row<V>(v, from, at, dim, TAIL ? kTail : 0);
 #pragma unroll
@@ -131,6 +136,7 @@ hipError_t launch_layer_norm(const ea_layer_norm_t& c, const void* x, const void
     using namespace norm;
     if (c.rows == 0) return hipSuccess;
     const Shape shape = shape_of(c);
+    const float n = (float)c.dim, each = 1.0f / n;
     return with_type(c.x_type, [&](auto xt) {
         return with_type(c.y_type, [&](auto yt) {
             return with_bool(past_caches(c.rows * c.dim, c.y_type), [&](auto once) {
@@ -140,7 +146,7 @@ hipError_t launch_layer_norm(const ea_layer_norm_t& c, const void* x, const void
                 if (!shape.waves) {
                     auto* kernel = shape.tail ? norm_long_kernel<X, Y, true, O> : norm_long_kernel<X, Y, false, O>;
                     hipLaunchKernelGGL(kernel, dim3((unsigned)at_most(c.rows, 1024)), dim3(kLongBlock), 0, s, c,
-                                       (const X*)x, weight, bias, (Y*)y, mean, rstd);
+                                       (const X*)x, weight, bias, (Y*)y, mean, rstd, n, each);
                     return hipGetLastError();
                 }
                 const unsigned groups = (unsigned)norm_groups_of(c, shape);
@@ -149,7 +155,7 @@ hipError_t launch_layer_norm(const ea_layer_norm_t& c, const void* x, const void
                     constexpr bool T = decltype(t)::value;
                     hipLaunchKernelGGL((norm_kernel<X, Y, T, W, K, O>), dim3(groups),
                                        dim3(W == 1 ? 256 : W * kWave), 0, s, c, (const X*)x, weight, bias, (Y*)y, mean,
-                                       rstd);
+                                       rstd, n, each);
                     return hipGetLastError();
                 });
             });

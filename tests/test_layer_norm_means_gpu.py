@@ -1,0 +1,37 @@
+"""Layer norm's means are quotients, not products with a rounded 1 / dim: where a row's sum is exact, a whole multiple of
+the row's width, so is its mean, and what is left of the row after its subtraction is 0 without any error that 1 / sqrt(eps)
+would enlarge.  Widths of every form whose reciprocal, rounded, times their own multiple is not the multiplicand."""
+import pytest
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+if not torch.cuda.is_available():  # pragma: no cover - CPU-only host
+    pytest.skip("needs a GPU", allow_module_level=True)
+
+import paper_2205_14473_amd as E  # noqa: E402
+from layer_util import TYPES  # noqa: E402
+
+VALUES = [1.0, -3.0, 5.0, 7.0, 19.0, 52.0, 100.0, 120.0, -248.0]     # in every type
+# one wave (whole vectors, with a tail, fewer than one), 4 waves, 16 waves, rows that are not held
+WIDTHS = [7, 41, 120, 488, 953, 1952, 3995, 4067, 7808, 15_616, 16_247, 20_520, 20_655]
+
+
+def config(rows, dim, kind):
+    code = E.ea_type(kind)
+    return E.LayerNorm(rows=rows, dim=dim, x_stride=dim, y_stride=dim, eps=1e-5, x_type=code, y_type=code, w_type=E.EA_F32)
+
+
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("dim", WIDTHS)
+def test_rows_of_one_value_give_the_bias(dim, kind):
+    """Sums of at most 248 x 20,655 are exact in binary32 in any order."""
+    dtype, rows = TYPES[kind], len(VALUES)
+    values = torch.tensor(VALUES, device="cuda")
+    x = values[:, None].expand(rows, dim).to(dtype).contiguous()
+    gen = torch.Generator(device="cuda").manual_seed(dim)
+    w, b = torch.randn(dim, device="cuda", generator=gen) * 50, torch.randn(dim, device="cuda", generator=gen)
+    y, mean, rstd = torch.empty_like(x), torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda")
+    E.ea_layer_norm(config(rows, dim, dtype), x, w, b, y, mean, rstd)
+    assert torch.equal(mean, values)
+    assert torch.equal(y, b.to(dtype).expand(rows, dim))
