@@ -41,11 +41,13 @@ constexpr int grad_waves(int waves, int columns, bool tail)
     return grad_ahead(waves, columns, tail) && columns > 8 ? 3 : 4;
 }
 
-// ONCE: the result goes past the caches.
+// n, each: dim and 1 / dim, from the host so that they are scalars.  The means are subtracted, and what they leave is
+// multiplied by rstd: they are quotients, so that they leave nothing where the sums are exact.  ONCE: the result goes past
+// the caches.
 template <class X, class Y, bool TAIL, int WAVES, int K, bool ONCE>
 __global__ void __launch_bounds__(WAVES == 1 ? 256 : WAVES * kWave, (grad_waves(WAVES, K * kVec<X, Y, TAIL>, TAIL)))
     norm_grad_kernel(ea_layer_norm_t c, const X* x, const Y* dy, const void* weight, const float* mean,
-                     const float* rstd, const X* add, X* dx, float* partial)
+                     const float* rstd, const X* add, X* dx, float* partial, float n, float each)
 {
     constexpr int V = vec_of<X, Y, TAIL>(), kRows = WAVES == 1 ? 4 : 1;
     // The weights wait in LDS then.
@@ -84,7 +86,6 @@ __global__ void __launch_bounds__(WAVES == 1 ? 256 : WAVES * kWave, (grad_waves(
     if (kAhead) __syncthreads();
 #pragma unroll
     for (int k = 0; k < K * V; ++k) dw[k] = db[k] = 0.0f;
-    const float each = 1.0f / (float)dim;
     for (; row < c.rows; row += step) {
         if (!kAhead) load(row);
         const float mu = mean[row], r = rstd[row];
@@ -110,8 +111,9 @@ __global__ void __launch_bounds__(WAVES == 1 ? 256 : WAVES * kWave, (grad_waves(
             second = __builtin_fmaf(d[k], v[k], second);
         }
         row_sums<WAVES>(first, second, lds);
-        first = first * each;
-        second = second * each;
+        // (scalars: in vector registers 16-wave rows spill a hundred others, 4,096 x 16,384 bfloat16 150 us, and 115 so)
+        first = uniform(quotient(first, n, each));
+        second = uniform(quotient(second, n, each));
 #pragma unroll
         for (int k = 0; k < K; ++k) {
             const int at = (k * WAVES * kWave + lane) * V, tail = tail_of<TAIL, WAVES, K>(k);
@@ -159,12 +161,11 @@ __global__ void __launch_bounds__(WAVES == 1 ? 256 : WAVES * kWave, (grad_waves(
 template <class X, class Y, bool TAIL, bool ONCE>
 __global__ void __launch_bounds__(kLongBlock)
     norm_grad_long_kernel(ea_layer_norm_t c, const X* x, const Y* dy, const void* weight, const float* mean,
-                          const float* rstd, const X* add, X* dx)
+                          const float* rstd, const X* add, X* dx, float n, float each)
 {
     constexpr int V = vec_of<X, Y, TAIL>();
     __shared__ float2 lds[kLongBlock / kWave];
     const int dim = (int)c.dim;
-    const float each = 1.0f / (float)dim;
     for (int64_t row = blockIdx.x; row < c.rows; row += gridDim.x) {
         const float mu = mean[row], r = rstd[row];
         const X* from = x + row * c.x_stride;
@@ -181,8 +182,8 @@ __global__ void __launch_bounds__(kLongBlock)
             }
         }
         row_sums<kLongBlock / kWave>(first, second, lds);
-        first = first * each;
-        second = second * each;
+        first = uniform(quotient(first, n, each));
+        second = uniform(quotient(second, n, each));
         for (int at = threadIdx.x * V; at < dim; at += kLongBlock * V) {
             float o[V];
             load_weights<V>(w, weight, c.w_type, at, dim, 1.0f, TAIL ? kTail : 0);
@@ -290,6 +291,7 @@ hipError_t launch_layer_norm_grad(const ea_layer_norm_t& c, const void* x, const
     float* partial = dweight || dbias ? (float*)workspace : nullptr;
     const Shape shape = shape_of(c);
     const int64_t parts = c.rows == 0 ? 0 : shape.waves ? grad_groups_of(c, shape) : runs_of(c);
+    const float n = (float)c.dim, each = 1.0f / n;
     hipError_t e = hipSuccess;
     if (c.rows > 0)
         e = with_type(c.x_type, [&](auto xt) {
@@ -310,7 +312,8 @@ hipError_t launch_layer_norm_grad(const ea_layer_norm_t& c, const void* x, const
                                                dim3(kColumnBlock), 0, s, c, (const X*)x, (const Y*)dy, mean, rstd,
                                                partial, run);
                         hipLaunchKernelGGL(rows, dim3((unsigned)at_most(c.rows, 1024)), dim3(kLongBlock), 0, s, c,
-                                           (const X*)x, (const Y*)dy, weight, mean, rstd, (const X*)add, (X*)dx);
+                                           (const X*)x, (const Y*)dy, weight, mean, rstd, (const X*)add, (X*)dx, n,
+                                           each);
                         return hipGetLastError();
                     }
                     return with_shape<vec_of<X, Y, false>()>(shape, [&](auto t, auto w, auto k) {
@@ -318,7 +321,7 @@ hipError_t launch_layer_norm_grad(const ea_layer_norm_t& c, const void* x, const
                         constexpr bool T = decltype(t)::value;
                         hipLaunchKernelGGL((norm_grad_kernel<X, Y, T, W, K, O>), dim3((unsigned)parts),
                                            dim3(W == 1 ? 256 : W * kWave), 0, s, c, (const X*)x, (const Y*)dy, weight,
-                                           mean, rstd, (const X*)add, (X*)dx, partial);
+                                           mean, rstd, (const X*)add, (X*)dx, partial, n, each);
                         return hipGetLastError();
                     });
                 });

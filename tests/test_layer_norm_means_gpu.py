@@ -35,3 +35,25 @@ def test_rows_of_one_value_give_the_bias(dim, kind):
     E.ea_layer_norm(config(rows, dim, dtype), x, w, b, y, mean, rstd)
     assert torch.equal(mean, values)
     assert torch.equal(y, b.to(dtype).expand(rows, dim))
+
+
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("dim", WIDTHS)
+def test_gradients_along_the_mean_and_the_row_vanish(dim, kind):
+    """For x of 1 and -1 in pairs (0 at an odd end), a mean of 0 and rstd of 1: a gradient of one value c has the mean c, and
+    its sum with x is 0; one of c x has the mean 0, and c as its mean product with x (of an even width).  dx is what is
+    left of them, 0, so that with `add` it is `add`."""
+    dtype = TYPES[kind]
+    sign = torch.where(torch.arange(dim, device="cuda") % 2 == 0, 1.0, -1.0)
+    if dim % 2:
+        sign[-1] = 0
+    along = [torch.ones_like(sign)] + ([sign] if dim % 2 == 0 else [])
+    dy = torch.stack([c * v for v in along for c in VALUES]).to(dtype)
+    rows = len(dy)
+    x = sign.expand(rows, dim).to(dtype).contiguous()
+    mean, rstd = torch.zeros(rows, device="cuda"), torch.ones(rows, device="cuda")
+    add = torch.randn((rows, dim), device="cuda", generator=torch.Generator(device="cuda").manual_seed(dim)).to(dtype)
+    for a in (None, add):
+        dx = torch.empty_like(x)
+        E.ea_layer_norm_grad(config(rows, dim, dtype), x, dy, None, mean, rstd, a, dx, None, None, False, None)
+        assert bool((dx == (0 if a is None else a)).all())
