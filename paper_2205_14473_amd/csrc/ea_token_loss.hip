@@ -494,7 +494,6 @@ struct Shape {
     EA_SHAPE(4, 16)                                                                                                \
     EA_SHAPE(8, 10)                                                                                                \
     EA_SHAPE(8, 12)                                                                                                \
-    EA_SHAPE(8, 13)                                                                                                \
     EA_SHAPE(8, 14)                                                                                                \
     EA_SHAPE(8, 16)                                                                                                \
     EA_SHAPE(16, 10)                                                                                               \
