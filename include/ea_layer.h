@@ -56,9 +56,10 @@ typedef struct ea_layer_norm {
  *   y (device, rows, write; may be x when types and strides are the same),
  *   mean, rstd (device, rows floats each, write; may be NULL, but the gradient
  *   needs them).
- * A row that holds an infinity or NaN, or whose sum overflows binary32, gives
- * NaN, in that row only; one whose squares alone overflow has rstd = 0 and
- * y = bias. */
+ * The mean is the sum's quotient to the nearest: a row of one value whose sum is
+ * exact gives the bias.  A row that holds an infinity or NaN, or whose sum, or
+ * difference from the mean, overflows binary32, gives NaN, in that row only; one
+ * whose squares alone overflow has rstd = 0 and y = bias. */
 int ea_layer_norm(const ea_layer_norm_t *c, const void *x, const void *weight, const void *bias, void *y, float *mean,
                   float *rstd, void *stream);
 
@@ -153,7 +154,9 @@ int64_t ea_recurrence_workspace_bytes(const ea_recurrence_t *c);
  * `length` without lengths.  Steps from n on are not read and y is 0 there.
  * Sequences are cut into pieces whose gates are multiplied: with plain gates
  * a product over some of the steps that leaves binary32's range gives
- * infinities or NaN, or 0, even where the steps one by one would not.
+ * infinities or NaN, or 0, even where the steps one by one would not.  A product
+ * that falls to 0, of any gates, leaves 0 of a finite state and NaN of an infinite
+ * one; the states behind an infinity are infinite or NaN.
  * Pieces hand their states on through the workspace, within one launch, and wait
  * for each other: calls that may run at the same time need a workspace each.  (A
  * state that does not come for a good part of a second is taken as NaN.)

@@ -178,7 +178,7 @@ hipError_t launch_layer_norm_grad(const ea_layer_norm_t& c, const void* x, const
                                   const float* mean, const float* rstd, const void* add, void* dx, void* dweight,
                                   void* dbias, bool accumulate, void* workspace, hipStream_t s);
 
-// residual is NULL for the gradient, whose dy takes x's place (in_type the type of what is read).
+// residual is NULL for the gradient, whose dy takes x's place.
 hipError_t launch_dropout(const ea_dropout_t& c, bool backward, uint32_t t, const uint32_t* t_dev, const void* in,
                           const void* residual, void* out, hipStream_t s);
 

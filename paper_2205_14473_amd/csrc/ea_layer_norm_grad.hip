@@ -6,8 +6,10 @@
 // the sizes alone, so every sum has one order.
 //
 // Bound by bytes: 65,536 x 1,024 bfloat16 with a residual's gradient added 103 us,
-// 5.2 TB/s, of which the partial rows' sum is 6.  Few rows are bound by the two
-// launches: 2,048 x 768 binary32 12 us.
+// 5.2 TB/s, of which the partial rows' sum is 6; 4,096 x 16,384 115 us, 4.7 TB/s.  Few
+// rows are bound by the two launches: 2,048 x 768 binary32 12 us.  Rows that are not
+// held read x and dy three times: 2,048 x 20,000 bfloat16 117 us, 2.8 TB/s of what
+// they have to move (the norm itself, three times x: 42 us, 3.9).
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -25,17 +27,19 @@ __host__ __device__ constexpr int64_t partial_row(int64_t dim)
     return (dim + 7) / 8 * 8;
 }
 
-// Whether the next row's vectors are asked for before this row's sums are formed.  The registers for them pay where a
-// lane holds few columns (131,072 x 256 bfloat16 65 us without, 55 with) and for rows with a tail, whose loads are more
-// and smaller (65,536 x 1,001 119 without, 106 with); not for 16 whole columns a lane (32,768 x 1,024 float32 104
-// without, 112 with; 65,536 x 1,024 bfloat16 107 either way), nor for 16 waves, which have 128 registers each (4,096 x
-// 16,384 149 without, 196 with).
+// Whether the next row's vectors are asked for before this row's sums are formed, `add` in all of these.  The registers for
+// them pay where a lane holds few columns (131,072 x 256 bfloat16 66 us without, 55 with) and for rows with a tail, whose
+// loads are more and smaller (65,536 x 1,001 121 without, 104 with); not for 16 whole columns a lane (32,768 x 1,024
+// binary32 102 without, 107 with; 65,536 x 1,024 bfloat16 103 either way), nor for 16 waves, which have 128 registers each
+// (4,096 x 16,384 bfloat16 115 without, 130 with; binary32 218 and 349).
 constexpr bool grad_ahead(int waves, int columns, bool tail)
 {
     return waves <= 4 && (columns <= 8 || tail);
 }
 
-// Waves of a SIMD that the gradient's registers leave room for (four and spills for 1,001 columns: 230 us).
+// Waves of a SIMD that the gradient's registers leave room for (four and spills for 1,001 columns: 230 us).  Forms of 16
+// columns a lane with a binary32 array still keep 4 to 16 registers in scratch, of 16 waves with a tail and arrays of two
+// sizes 41 to 59.
 constexpr int grad_waves(int waves, int columns, bool tail)
 {
     return grad_ahead(waves, columns, tail) && columns > 8 ? 3 : 4;

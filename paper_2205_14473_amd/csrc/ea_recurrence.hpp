@@ -8,7 +8,8 @@
 // and the state they end with go to LDS, and every wave folds what lies before
 // it, in order, and runs its steps again from the true state.
 //
-// What a chunk starts with comes from the chunks before it through memory.
+// What a chunk starts with comes from the chunks before it through memory, by decoupled
+// look-back (Merrill and Garland, 2016) with a fixed order of the fold.
 // kGroup chunks form a group and kGroup groups a stretch.  A chunk hands out its
 // product and end state as soon as it has them, without waiting for anything; the
 // last chunk of a group folds the group's and hands that out; the last chunk of a
@@ -23,7 +24,10 @@
 // Bound by bytes and by what the exchange costs on top of them.  One sequence of
 // 65,536 steps of 1,024 bfloat16 channels, states saved: 124 us, 3.3 TB/s; the
 // gradient of 32 padded sequences of 2,048 steps (gates in binary32) 160 us, 4.5 TB/s;
-// that of 2 x 16,384 x 768 binary32 with plain gates 117 us, 4.3 TB/s.  Other ways,
+// that of 2 x 16,384 x 768 binary32 with plain gates 117 us, 4.3 TB/s.  A lane is a
+// channel, so that under 64 channels lanes idle and a row is one short load: what
+// bounds is the steps, not the bytes (256 x 3,000 x 16 bfloat16 69 us, 1.1 TB/s;
+// 64 x 8,000 x 32 57, 1.7; x 64 63, 3.1; the gradients 124, 96 and 105).  Other ways,
 // before the results went past the caches (128 / 170 / 122 us then): steps as segments
 // of whole sequences, the ends of which a first pass forms: 220 / 190 / 171.  Groups
 // alone, without stretches: 124 / 168 / 122, but a wait that passes on every 4,096
@@ -43,8 +47,8 @@ constexpr int kMostWaves = 16;
 constexpr int kGroup = 16;                             // chunks; a wave waits for each of those before
 static_assert(kGroup <= kMostWaves, "a group's earlier chunks, and a stretch's earlier groups, have a wave each");
 
-// Division of numbers under 2^31 by a number known to the host: (h + (n - h) / 2) / 2^shift for the high half h of
-// n * factor, in scalar instructions.
+// Division of numbers under 2^31 by a number known to the host (Granlund and Montgomery, 1994): (h + (n - h) / 2) / 2^shift
+// for the high half h of n * factor, in scalar instructions.
 struct Divisor {
     uint32_t factor, shift, by;
     explicit Divisor(uint32_t d = 1) : by(d)

@@ -1,7 +1,7 @@
 // ea_token_loss.hip -- cross-entropy of tokens and its gradient in one pass over
 // the logits.
 //
-// A row is held in registers, as it is stored, by 1, 4 or 16 waves: its largest
+// A row is held in registers, as it is stored, by 1, 4, 8 or 16 waves: its largest
 // logit and the sum of exponentials are reductions, and the gradient leaves the
 // same registers.  Longer rows are cut into pieces and read twice.  The mean's
 // gradient needs the number of tokens that count first: a workgroup counts few
@@ -26,7 +26,7 @@ constexpr float kLog2e = 0x1.715476p+0f;
 constexpr int kCountBlock = 1024;
 constexpr int64_t kMostCounts = 256;                   // workgroups that count
 constexpr int64_t kOwnCount = 16;                      // targets a thread up to which each workgroup counts all itself
-constexpr int64_t kMostWaves = 4096;                   // of the main pass, 16 a CU: each row's waves leave one sum
+constexpr int64_t kMostWaves = 4096;                   // of the main pass, 16 a CU; twice as many where a row is one wave's
 constexpr int kEndBlock = 256;
 
 // Workspace: the counting groups' counts, then each main group's sum and count (for rows in pieces each row's, then
@@ -479,6 +479,8 @@ int64_t at_most(int64_t n, int64_t most)
 
 // Waves of a row and vectors a lane: the first that holds it, or those of a piece and 0 where none does.  Few waves with
 // many vectors each: rows of their own work beside each other on a CU, one reading or writing while another reduces.
+// (From 10 vectors a lane on in steps of two: 13 between 12 and 14 gained 1% at most with the gradient, 2% without.)
+// Without the gradient, many forms of 10 vectors and more keep one or two registers in scratch.
 struct Shape {
     int waves, k;
 };
