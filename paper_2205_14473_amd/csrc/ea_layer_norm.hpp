@@ -123,11 +123,12 @@ __device__ __forceinline__ void row_sums(float& a, float& b, float2* lds)
 }
 
 // sum / n, where each is 1 / n rounded: what the product leaves of the sum comes out of one operation and corrects it to
-// the nearest.  (131,072 x 256 bfloat16, mean and variance by divisions of ten operations each: 31.4 us; without: 28.0.)
+// the nearest.  (Of an infinite sum it leaves NaN, and there is nothing to correct.)
+// (131,072 x 256 bfloat16, mean and variance by divisions of ten operations each: 31.4 us; without: 28.0.)
 __device__ __forceinline__ float quotient(float sum, float n, float each)
 {
-    const float q = sum * each;
-    return __builtin_fmaf(__builtin_fmaf(-q, n, sum), each, q);
+    const float q = sum * each, left = __builtin_fmaf(-q, n, sum);
+    return left == left ? __builtin_fmaf(left, each, q) : q;
 }
 
 // Waves of a row and vectors a lane holds of it (0 waves: the row is not held), the fewest that hold it, so that only a

@@ -57,3 +57,24 @@ def test_gradients_along_the_mean_and_the_row_vanish(dim, kind):
         dx = torch.empty_like(x)
         E.ea_layer_norm_grad(config(rows, dim, dtype), x, dy, None, mean, rstd, a, dx, None, None, False, None)
         assert bool((dx == (0 if a is None else a)).all())
+
+
+@pytest.mark.parametrize("dim", [41, 488, 953, 1952, 16_247, 20_655])
+def test_infinite_sums_have_infinite_means(dim):
+    """A row's mean is its sum's quotient where that is an infinity too; the gradient of a row whose dy holds one is what the
+    formula's operations give: -infinity where nothing else is infinite."""
+    inf = float("inf")
+    x = torch.ones((4, dim), device="cuda")
+    x[0, 5], x[1, dim - 1], x[2, 0], x[2, 1] = inf, -inf, inf, -inf
+    x[3, :2] = 3e38
+    y, mean, rstd = torch.empty_like(x), torch.empty(4, device="cuda"), torch.empty(4, device="cuda")
+    c = config(4, dim, torch.float32)
+    E.ea_layer_norm(c, x, None, None, y, mean, rstd)
+    assert mean[0].item() == inf and mean[1].item() == -inf and mean[2].isnan() and mean[3].item() == inf
+    assert bool(y.isnan().all())
+    # x of 0 with a mean of 0: dx = rstd (dy - mean(dy)), and the mean is infinite
+    dy, dx = torch.ones_like(x), torch.empty_like(x)
+    dy[1, :2] = 3e38
+    E.ea_layer_norm_grad(c, torch.zeros_like(x), dy, None, torch.zeros_like(mean), torch.ones_like(rstd), None, dx, None, None,
+                         False, None)
+    assert bool((dx[1] == -inf).all()) and bool(dx[::2].isfinite().all())
